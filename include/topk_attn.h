@@ -73,12 +73,15 @@ enum {
                                    rint(x * 127 / amax) and one fp32 scale amax / 127 per row
                                    (amax = largest magnitude of the row; rows below 2^-100 are coded
                                    as zero).  16-bit dtypes, head_dim 64, 128 or 256, Hq/Hkv <= 4. */
-    TOPK_ATTN_INDEX_PAGES = 2   /* plus a coarse index over pages of 64 consecutive tokens (the paper's
+    TOPK_ATTN_INDEX_PAGES = 2,  /* plus a coarse index over pages of 64 consecutive tokens (the paper's
                                    sub-linear retrieval; the kind of index is left open there): per page
                                    a centre c (mean of its keys, in the cache dtype) and two fp32 numbers,
                                    a radius r >= |k - c| for every key k of the page and |c|.  A page
                                    cannot hold a key that scores more than q . c + |q| r (Cauchy-Schwarz).
                                    16-bit dtypes, Hq/Hkv <= 4. */
+    TOPK_ATTN_INDEX_BOXES = 4   /* plus the block index of topk_attn_decode_blocks: per page of 64 consecutive tokens the
+                                   smallest and the largest key, channel by channel, in `dtype`.  The top-k
+                                   decodes take the exact path on such a handle.  All dtypes and head groups. */
 };
 
 typedef struct {
@@ -109,7 +112,8 @@ typedef struct {
  * then the scales [layer][seq][kv_head][max_tokens] fp32 follow (each rounded up to 256
  * bytes).  With TOPK_ATTN_INDEX_PAGES the page centres [layer][seq][kv_head][P][head_dim] in
  * `dtype` and then [layer][seq][kv_head][P][2] fp32 (radius, centre norm) follow, P =
- * ceil(max_tokens / 64): 1.6 % of K at head_dim 128.  0 on invalid config. */
+ * ceil(max_tokens / 64): 1.6 % of K at head_dim 128.  With TOPK_ATTN_INDEX_BOXES the boxes
+ * [layer][seq][kv_head][P][2][head_dim] in `dtype` follow (smallest, then largest): 3.1 % of K.  0 on invalid config. */
 size_t topk_attn_kv_bytes(const topk_attn_config* cfg);
 
 /* Bytes of scratch the kernels need (score buffer, candidate lists, partial sums,
@@ -150,6 +154,36 @@ int topk_attn_append_kv(topk_attn_t* h, int layer, int seq, const void* k_new, c
  * enqueued then).  n_new == 0 is a no-op. */
 int topk_attn_append_step(topk_attn_t* h, int layer, const void* k_new, const void* v_new, int64_t n_new,
                           void* hip_stream);
+
+/* New tokens' projections into the cache: the queries and keys of each head are normalised (root mean square, optional), turned by
+ * their rotary position and rounded once to the cache dtype; keys and values are appended, the queries go to q_out, where the decodes
+ * take them from.  One pass over the projections, in place of separate norms and rotations before topk_attn_append_step /
+ * topk_attn_append_kv.
+ *   x' = x / sqrt(mean_c x_c^2 + norm_eps) * norm_c
+ *   pair i < rotary_dim / 2 of channels (a, b):  a' = a cos t - b sin t,  b' = b cos t + a sin t,  t = position * inv_freq[i]
+ * (norms, angles and rotation in 32 bits or more; the angle, which grows with the position, in 64).  Channels from rotary_dim on
+ * are normalised only.  With an index its entries of the new keys are kept as by the other appends. */
+typedef struct {
+    uint32_t struct_size;      /* sizeof(topk_attn_rotary) */
+    int32_t rotary_dim;        /* leading channels of a head that are rotated: even, 0 .. head_dim */
+    int32_t interleaved;       /* 0: pair i is channels (i, i + rotary_dim / 2); otherwise (2 i, 2 i + 1) */
+    float norm_eps;            /* >= 0; used where a norm weight is given */
+    int64_t n_new;             /* tokens per sequence; 0 is a no-op */
+    /* Projections in the cache dtype, device: element (s, t, h, c) of the call's s-th sequence at
+     * base[s * seq_stride + t * token_stride + h * head_dim + c] (strides in elements, rows 16-byte aligned): the three
+     * may be parts of one fused projection.  q and q_out may both be NULL (keys and values only). */
+    const void *q, *k, *v;
+    int64_t q_seq_stride, q_token_stride, k_seq_stride, k_token_stride, v_seq_stride, v_token_stride;
+    void* q_out;               /* device [S, n_new, Hq, d] in the cache dtype (S: sequences of the call); must not overlap the inputs */
+    const void *q_norm, *k_norm;   /* device [d] in the cache dtype, 16-byte aligned, or NULL: not normalised */
+    const float* inv_freq;     /* device [rotary_dim / 2]; may be NULL for rotary_dim 0 */
+    const int32_t* positions;  /* device [S, n_new], or NULL: the cache row each token goes to (its length before the call + t) --
+                                  after topk_attn_evict rows and positions differ */
+} topk_attn_rotary;
+/* seq: one sequence of the layer, or -1: all B of them.  Enqueued on `hip_stream`; like the other appends not to be replayed from a
+ * HIP graph.  Errors: EINVAL (null, range, odd or too large rotary_dim, misaligned, a negative stride, one of q / q_out alone),
+ * ECAPACITY (nothing is enqueued then), EUNSUPPORTED (2^31 or more tokens in a call). */
+int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_rotary* r, void* hip_stream);
 
 /* One decode step of `layer` for all B sequences: steps 1-3 above over all tokens
  * currently cached for (layer, b).  k_eff = min(k, N_b).
@@ -214,6 +248,45 @@ int topk_attn_decode_window(topk_attn_t* h, int layer, const void* q, int k, int
 int topk_attn_decode_multi(topk_attn_t* h, int layer, const void* q, int n_queries, int causal, int k,
                            int window, float* out, int32_t* idx, float* vals, float* lse,
                            void* hip_stream);
+
+/* Dense attention of one new token per sequence over all its cached tokens (the comparison the paper makes, and what layers that keep
+ * full attention call): out = softmax(q K^T / sqrt(d)) V, split over the cache's length and joined.  q, out and lse as in
+ * topk_attn_decode.
+ *   mass  device [B, Hkv, max_tokens] fp32 or NULL, caller-owned: each cached key's softmax weight, summed over the query heads of
+ *         its KV head, is added to mass[b][kv_head][position]; entries behind a sequence's length stay as they are.  No atomics: the
+ *         same call gives the same bits.
+ * A decode recorded into a HIP graph may be replayed as long as no sequence of the layer has grown or shrunk since.
+ * Errors: EINVAL (null h/q/out, layer range, misaligned q, a sequence with no tokens), EUNSUPPORTED (2^31 workgroups or more). */
+int topk_attn_decode_dense(topk_attn_t* h, int layer, const void* q, float* out, float* lse, float* mass, void* hip_stream);
+
+/* Block-sparse attention of one new token per sequence: for every sequence and KV head the n_blocks best pages of 64 tokens, each
+ * attended whole by the heads of the group.  A page's score is the largest raw score any key in its box (TOPK_ATTN_INDEX_BOXES) could
+ * have with any of the group's heads, max_h sum_c max(q_hc lo_c, q_hc hi_c), in 64 bits; ties go to the lower page.  The page of the newest
+ * token is always one of the n_blocks.  A sequence of at most n_blocks pages is attended densely.
+ *   blocks  device [B, Hkv, n_blocks] int32 or NULL: the pages attended, ascending; -1 behind them
+ *   lse     over the attended tokens;  mass as in topk_attn_decode_dense, for the attended tokens
+ * Errors as topk_attn_decode_dense; EINVAL without a block index or if n_blocks < 1. */
+int topk_attn_decode_blocks(topk_attn_t* h, int layer, const void* q, int n_blocks, float* out, int32_t* blocks, float* lse,
+                            float* mass, void* hip_stream);
+
+/* The same accumulation from what a top-k decode of the layer returned: mass[b][h / G][idx] += exp(vals / sqrt(d) - lse) for the k entries of
+ * every head (idx, vals [B, Hq, k], lse [B, Hq]; the positions of a head are distinct; entries with idx < 0 or >= max_tokens are passed over).
+ * With a recent-token window lse covers the window too, whose tokens are not among idx.  No atomics: the same call gives the same bits.
+ * Errors: EINVAL (null, layer range, k < 1). */
+int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const float* vals, const float* lse, int k, float* mass,
+                       void* hip_stream);
+
+/* Eviction by accumulated attention weight: every sequence of `layer` with more than `budget` tokens keeps its `recent` newest ones and, per
+ * KV head, the budget - recent of the older ones with the largest mass (ties to the lower position; a NaN counts as less than any
+ * number).  The kept rows move to the front of the cache in their order, index entries and mass with them; mass behind them, up to the old
+ * length, is cleared.  The length becomes `budget`.  Sequences of at most `budget` tokens stay as they are.
+ *   mass  device [B, Hkv, max_tokens] fp32
+ *   kept  device [B, Hkv, budget] int32 or NULL: the positions the rows had before the call, ascending; -1 behind a shorter sequence
+ * Rows are numbered by their place in the cache from then on (idx, windows, causal chunks); a window or `recent` still means the newest
+ * tokens.  Not to be replayed from a HIP graph (the lengths' host copy changes).
+ * Errors: EINVAL (null h/mass, layer range, budget < 1, budget > max_tokens, recent outside 0 .. budget), ENOMEM (the workspace has no room for
+ * a word per 64 KB of rows: budgets of tens of millions of tokens). */
+int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int64_t recent, int32_t* kept, void* hip_stream);
 
 /* Host-only helper for the paper's layer-wise settings of k ("Layer-Wise Settings for k":
  * a fixed total budget sum_l k_l, spent either uniformly or increasing linearly from the

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtopk_attn.so")
-SOURCES = ["api.hip", "scan.hip", "select.hip", "gather.hip", "attend.hip", "index8.hip", "tail.hip", "pages.hip"]
+SOURCES = ["api.hip", "scan.hip", "select.hip", "gather.hip", "attend.hip", "index8.hip", "tail.hip", "pages.hip",
+           "api_ops.hip", "dense.hip", "blocks.hip", "rotary.hip", "evict.hip"]
 # measurement program of its own (streaming-read ceiling over launch shapes), built beside the library
 PROBE_SRC = "read_probe_sweep.hip"
 PROBE = os.path.join(OBJ_DIR, "read_probe_sweep")

@@ -15,20 +15,13 @@
 #include "../../include/topk_attn.h"
 #include "../../include/topk_attn_debug.h"
 #include "device_utils.h"
+#include "handle.h"
 #include "internal.h"
+#include "page_boxes.h"
 
 using namespace tka;
 
 namespace {
-
-constexpr size_t kAlign = 256;
-inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-inline int elem_bytes(int dtype) { return dtype == TOPK_ATTN_F32 ? 4 : 2; }
-
-struct WsLayout {
-    size_t len, thr, bins, samp, seg_cnt, seg_max, seg_cnt2, flags, hmax, fallback, tailrec, page_mask, page_cnt, page_list, hist, cand, bnd, scores, sel_idx, sel_val, part_acc, part_l, part_m, total;
-    int cand_cap, bnd_cap, n_chunk_cap, hist_cap, page_words, batch_layers;
-};
 
 bool config_ok(const topk_attn_config* c, int* why) {
     *why = TOPK_ATTN_EINVAL;
@@ -37,7 +30,7 @@ bool config_ok(const topk_attn_config* c, int* why) {
     if (c->max_tokens < 1 || c->max_k < 1 || c->device < 0 || c->max_window < 0) return false;
     if (c->max_queries < 0 || c->max_queries > 4096) return false;
     if (c->index_kind != TOPK_ATTN_INDEX_NONE && c->index_kind != TOPK_ATTN_INDEX_INT8 &&
-        c->index_kind != TOPK_ATTN_INDEX_PAGES)
+        c->index_kind != TOPK_ATTN_INDEX_PAGES && c->index_kind != TOPK_ATTN_INDEX_BOXES)
         return false;
     if ((int64_t)c->n_seqs * (c->max_queries > 1 ? c->max_queries : 1) > 65535) return false;   // a grid dimension
     if (c->max_tokens > (int64_t)0x7FFFFF00) return false;   // positions are int32
@@ -57,34 +50,6 @@ bool config_ok(const topk_attn_config* c, int* why) {
         return false;
     *why = TOPK_ATTN_OK;
     return true;
-}
-
-size_t kv_half_bytes(const topk_attn_config* c) {
-    return align_up((size_t)c->n_layers * c->n_seqs * c->n_kv_heads * (size_t)c->max_tokens * c->head_dim *
-                    elem_bytes(c->dtype));
-}
-
-// int8 index behind K and V: codes, then scales
-size_t index_codes_bytes(const topk_attn_config* c) {
-    if (c->index_kind != TOPK_ATTN_INDEX_INT8) return 0;
-    return align_up((size_t)c->n_layers * c->n_seqs * c->n_kv_heads * (size_t)c->max_tokens * c->head_dim);
-}
-size_t index_scales_bytes(const topk_attn_config* c) {
-    if (c->index_kind != TOPK_ATTN_INDEX_INT8) return 0;
-    return align_up((size_t)c->n_layers * c->n_seqs * c->n_kv_heads * (size_t)c->max_tokens * sizeof(float));
-}
-// page index behind K and V: centres, then (radius, centre norm) pairs
-int64_t page_cap_of(const topk_attn_config* c) { return (c->max_tokens + 63) / 64; }
-size_t page_centres_bytes(const topk_attn_config* c) {
-    if (c->index_kind != TOPK_ATTN_INDEX_PAGES) return 0;
-    return align_up((size_t)c->n_layers * c->n_seqs * c->n_kv_heads * (size_t)page_cap_of(c) * c->head_dim * elem_bytes(c->dtype));
-}
-size_t page_balls_bytes(const topk_attn_config* c) {
-    if (c->index_kind != TOPK_ATTN_INDEX_PAGES) return 0;
-    return align_up((size_t)c->n_layers * c->n_seqs * c->n_kv_heads * (size_t)page_cap_of(c) * 2 * sizeof(float));
-}
-size_t kv_total_bytes(const topk_attn_config* c) {
-    return 2 * kv_half_bytes(c) + index_codes_bytes(c) + index_scales_bytes(c) + page_centres_bytes(c) + page_balls_bytes(c);
 }
 
 // batch_layers: layers of a topk_attn_decode_layers call that share their launches, each with per-call buffers of its own (a
@@ -149,6 +114,9 @@ WsLayout ws_layout(const topk_attn_config* c, int batch_layers) {
     w.part_acc = take(BH * (size_t)w.n_chunk_cap * c->head_dim * sizeof(float));
     w.part_l = take(BH * (size_t)w.n_chunk_cap * sizeof(float));
     w.part_m = take(BH * (size_t)w.n_chunk_cap * sizeof(float));
+    const size_t box_pages = c->index_kind == TOPK_ATTN_INDEX_BOXES ? (size_t)c->n_seqs * c->n_kv_heads * (size_t)page_cap_of(c) : 0;
+    w.block_score = take(box_pages * sizeof(double));
+    w.block_list = take(box_pages * sizeof(int32_t));
     w.total = o;
     w.batch_layers = batch_layers;
     return w;
@@ -348,30 +316,6 @@ static int scratch_address(int device, void** out) {
 
 constexpr int kTimingSlots = 512;
 
-struct topk_attn {
-    topk_attn_config cfg;
-    WsLayout ws;
-    WsLayout ws_one;            // the layout without room for further layers (the built-in scratch)
-    size_t kv_half;
-    std::vector<int64_t> len;   // host mirror of the device lengths, [L][B]
-    int path;
-    bool last_fast;
-    bool last_static;           // the last decode used the built-in scratch
-    int force_redo;             // measurement aid, see topk_attn_debug_force_redo: 0, 1, or 2 (chip-wide selection)
-    float page_beta;            // scale of the page radius in the page bound (1 = exact)
-    bool last_paged;            // the last decode went through the page index
-    bool last_tail;             // the last decode used the chip-wide selection (its per-head records are in the workspace)
-    int last_queries;           // queries per sequence of the last decode
-    int last_n_seg, last_seg_cap;   // the split of the last filtered decode's candidate lists (0: not filtered)
-    int last_layer;
-    int last_slot;              // layers of the last call before its last one in the per-call buffers
-    char* scratch_dev;          // this device's copy of the built-in scratch
-    int n_cu;                   // compute units of the device
-    // optional event pairs around the key scan of each decode (measurement only)
-    bool timing;
-    std::vector<hipEvent_t> ev;  // 2 * kTimingSlots once enabled
-    int ev_used;
-};
 
 extern "C" {
 
@@ -540,6 +484,14 @@ int topk_attn_append_kv(topk_attn_t* h, int layer, int seq, const void* k_new, c
                               balls, (hipStream_t)hip_stream) != hipSuccess)
             return TOPK_ATTN_EDEVICE;
     }
+    if (c.index_kind == TOPK_ATTN_INDEX_BOXES) {   // boxes of the pages just touched
+        const int64_t pcap = page_cap_of(&c), stream0 = (int64_t)slot * c.n_kv_heads;
+        char* boxes = static_cast<char*>(c.kv_storage) + 2 * h->kv_half + stream0 * pcap * 2 * row_b;
+        const char* kseq = static_cast<const char*>(c.kv_storage) + stream0 * head_b;
+        if (launch_page_boxes(c.dtype, c.head_dim, kseq, c.max_tokens, pcap, c.n_kv_heads, 1, nullptr, cur, n_new, boxes,
+                              (hipStream_t)hip_stream) != hipSuccess)
+            return TOPK_ATTN_EDEVICE;
+    }
     h->len[slot] = cur + n_new;
     return TOPK_ATTN_OK;
 }
@@ -602,6 +554,12 @@ int topk_attn_append_step(topk_attn_t* h, int layer, const void* k_new, const vo
         float* balls = reinterpret_cast<float*>(base + page_centres_bytes(&c)) + stream0 * pcap * 2;
         if (launch_page_balls(c.dtype, c.head_dim, kdst, c.max_tokens, pcap, c.n_kv_heads, B, len_dev, 0, n_new, centres, balls,
                               st) != hipSuccess)
+            return TOPK_ATTN_EDEVICE;
+    }
+    if (c.index_kind == TOPK_ATTN_INDEX_BOXES) {
+        const int64_t pcap = page_cap_of(&c), stream0 = (int64_t)layer * B * c.n_kv_heads;
+        char* boxes = static_cast<char*>(c.kv_storage) + 2 * h->kv_half + stream0 * pcap * 2 * row_b;
+        if (launch_page_boxes(c.dtype, c.head_dim, kdst, c.max_tokens, pcap, c.n_kv_heads, B, len_dev, 0, n_new, boxes, st) != hipSuccess)
             return TOPK_ATTN_EDEVICE;
     }
     hipLaunchKernelGGL(bump_len_kernel, dim3((unsigned)((B + 255) / 256)), dim3(256), 0, st, len_dev, B, (int32_t)n_new);

@@ -1,0 +1,408 @@
+// Attention of one query per sequence and head over all cached tokens, or over a list of 64-token pages (topk_attn_decode_dense and
+// the last step of topk_attn_decode_blocks): out = sum_i p_i V_i / sum_i p_i with p_i = exp(q . K_i / sqrt(d)), in one pass over K and V.
+//
+//   attend_kernel       splits of a sequence, a workgroup each: running maximum, sum of weights and weighted value sum, per wave
+//   attend_join_kernel  the splits of a head put together; the weights of the keys added to `mass`
+//
+// Bound by the read of K and V: 16 384 bytes per 32 keys and KV head against 2 x 32 MFMA (d = 128, 16 bit), a tenth of the time the read takes.
+#include "device_utils.h"
+#include "internal.h"
+#include "ops.h"
+#include "page_boxes.h"
+#include "scan_tiles.h"
+
+namespace tka {
+
+// A step of the walk: STEP keys against 16 heads.  The products are taken transposed (keys x channels times channels x heads, then
+// channels x keys times keys x heads), so that a lane holds scores and weighted sums of one head, lane % 16, and the running maximum
+// is a number per lane.  The scores come out of the first product in lane (j, head) for keys 4 j .. 4 j + 3 of each 16-key tile; the
+// second product takes its keys in that same order, so the weights are its operand as they are.
+template <int DT, int D> struct AttendTile {
+    static constexpr int SUB = DT == DT_F32 ? 1 : 2;             // 16-key tiles of a step: one contraction of the second product
+    static constexpr int STEP = 16 * SUB, KEYS = 4 * SUB;        // keys of a step, and those whose values a lane holds
+    static constexpr int ROW = D * Elem<DT>::kBytes;
+    static constexpr int KCH = ROW / 64;                         // 16-byte pieces of a key row per lane
+    static constexpr int VLOAD = ROW / 16 < 16 ? ROW / 16 : 16;  // bytes of a value row a lane loads at a time
+    static constexpr int VQ = ROW / 16 / VLOAD;                  // such loads
+    static constexpr int EV = VLOAD / Elem<DT>::kBytes;          // channels of a load
+    static constexpr int T = D / 16;                             // 16-channel tiles
+    // channel of row m of tile t
+    static __device__ __forceinline__ constexpr int channel(int t, int m) { return ((t / EV) * 16 + m) * EV + t % EV; }
+    static constexpr bool kPipelined = ROW <= 256 || (DT == DT_F32 && ROW <= 512);
+    u32x4 k[SUB][KCH];
+    uint32_t v[KEYS][VQ * VLOAD / 4];
+};
+
+template <int BYTES>
+__device__ __forceinline__ void buffer_read(const __amdgpu_buffer_rsrc_t rsrc, int off, uint32_t* to) {
+    if constexpr (BYTES == 16) {
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
+        to[0] = x.x; to[1] = x.y; to[2] = x.z; to[3] = x.w;
+    } else if constexpr (BYTES == 8) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b64(rsrc, off, 0, 0);
+        to[0] = x[0]; to[1] = x[1];
+    } else {
+        to[0] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, off, 0, 0);
+    }
+}
+
+__device__ __forceinline__ float max_over_rows(float v) {      // largest of lanes l, l ^ 16, l ^ 32, l ^ 48
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Weights of 16-bit caches are the operand of an MFMA and go in as two parts, the rounding to the type and what it left: 16 (bf16) or 22
+// (fp16) bits of each weight, errors of at most 2^-18 of it.  (One part alone: 2^-9, a hundred times what the sums' roundings make.)
+// fp16 has no numbers below 2^-24, so there the weights are relative to the maximum less 13 powers of two.
+template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
+
+// Waves per SIMD: two (256 registers) where the buffers leave room for it.
+template <int DT, int D> constexpr int kAttendWaves = AttendTile<DT, D>::ROW <= 512 ? 2 : 1;
+
+template <int DT, int D, bool LIST, bool MASS>
+__global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(AttendCall a) {
+    using Tile = AttendTile<DT, D>;
+    constexpr int SUB = Tile::SUB, STEP = Tile::STEP, KEYS = Tile::KEYS, KCH = Tile::KCH, T = Tile::T, ROW = Tile::ROW, EV = Tile::EV;
+    constexpr int SPP = 64 / STEP;
+    __shared__ float red[4][16][D + 4];
+    __shared__ float red_m[4][16], red_l[4][16];
+    const int lane = lane_id(), j = lane >> 4, n = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // The head blocks of one split follow each other eight workgroups apart: on the same XCD, whose L2 holds the keys for them.
+    int unit = (int)blockIdx.x, rb = 0;
+    if (a.row_blocks > 1) {
+        const int group = unit / (8 * a.row_blocks), in = unit - group * 8 * a.row_blocks;
+        rb = in >> 3;
+        unit = group * 8 + (in & 7);
+    }
+    const int stream = unit / a.n_split, split = unit - stream * a.n_split;
+    if (stream >= a.B * a.Hkv) return;                        // (the last group of eight may be cut short)
+    const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
+    const int64_t N = a.len[b];
+    const int64_t pages_b = (N + 63) / 64;
+    const int64_t pages = LIST ? (a.n_list < pages_b ? a.n_list : pages_b) : pages_b;
+    const int64_t p0 = (int64_t)split * a.chunk;
+    if (p0 >= pages) return;                                  // (the join knows how many splits a sequence has)
+    const int64_t p1 = p0 + a.chunk < pages ? p0 + a.chunk : pages;
+    const int n_steps = (int)(p1 - p0) * SPP;
+    const int heads = a.G - 16 * rb < 16 ? a.G - 16 * rb : 16;
+    const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G + 16 * rb;
+    const char* const Kh = a.K + (int64_t)stream * a.Ncap * ROW;
+    const char* const Vh = a.V + (int64_t)stream * a.Ncap * ROW;
+    const int32_t* const list = LIST ? a.list + (int64_t)stream * a.list_stride + p0 : nullptr;
+
+    // queries: lane (j, head) holds the channels its lane (j, key) holds of a key row
+    u32x4 q[KCH];
+    {
+        const char* p = static_cast<const char*>(a.q) + (head0 + (n < heads ? n : 0)) * ROW + j * 16;
+#pragma unroll
+        for (int s = 0; s < KCH; ++s) {
+            q[s] = *reinterpret_cast<const u32x4*>(p + 64 * s);
+            if (n >= heads) q[s] = u32x4{0, 0, 0, 0};
+        }
+    }
+    uint32_t k_off[SUB], v_off[SUB];
+#pragma unroll
+    for (int g = 0; g < SUB; ++g) {
+        k_off[g] = (uint32_t)((16 * g + n) * ROW + j * 16);
+        v_off[g] = (uint32_t)((16 * g + 4 * j) * ROW + n * Tile::VLOAD);
+        asm volatile("" : "+v"(k_off[g]), "+v"(v_off[g]));
+    }
+    uint32_t pages_ahead = 0;                                 // LIST: lane i holds the page of the wave's step i (of the next 64)
+    // First row of the wave's step i (steps wave, wave + 4, ... of the split), asked for in order.
+    auto row_of = [&](int i) -> int64_t {
+        const int s = wave + 4 * i;
+        if (!LIST) return p0 * 64 + (int64_t)s * STEP;
+        if ((i & 63) == 0) {
+            const int at = wave + 4 * (i + lane);
+            pages_ahead = (uint32_t)list[at < n_steps ? at / SPP : 0];
+        }
+        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages_ahead, i & 63);
+        return (int64_t)page * 64 + (s % SPP) * STEP;
+    };
+    auto rows_from = [&](int64_t row0, bool live) -> int {      // rows of the step that the cache holds
+        const int64_t left = live ? N - row0 : 0;
+        int r = (int)(left < 0 ? 0 : left > STEP ? STEP : left);
+        r = __builtin_amdgcn_readfirstlane(r);
+        asm("" : "+s"(r));
+        return r;
+    };
+    auto load = [&](Tile& t, int i, int& rows) {
+        const int64_t row0 = row_of(i);
+        rows = rows_from(row0, wave + 4 * i < n_steps);
+        // what lies behind the rows there are reads as zero and is not fetched: no weight of zero meets a value of infinity
+        const int64_t at = rows > 0 ? row0 * ROW : 0;
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(Kh + at), 0, rows * ROW, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(Vh + at), 0, rows * ROW, 0x00020000);
+#pragma unroll
+        for (int g = 0; g < SUB; ++g) {
+#pragma unroll
+            for (int s = 0; s < KCH; ++s) t.k[g][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, (int)k_off[g] + 64 * s, 0, 0));
+        }
+#pragma unroll
+        for (int e = 0; e < KEYS; ++e) {
+#pragma unroll
+            for (int c = 0; c < Tile::VQ; ++c)
+                buffer_read<Tile::VLOAD>(rv, (int)v_off[e / 4] + (e % 4) * ROW + 256 * c, &t.v[e][c * (Tile::VLOAD / 4)]);
+        }
+    };
+    f32x4 acc[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;                              // (m: raw score times scale; l: this lane's keys)
+    auto use = [&](const Tile& t, int i, int rows) {
+        f32x4 s[SUB];
+#pragma unroll
+        for (int g = 0; g < SUB; ++g) {
+            s[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KCH; ++c) {
+                if constexpr (DT == DT_F32) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[g][c][x]), __uint_as_float(q[c][x]), s[g], 0, 0, 0);
+                } else {
+                    using v8 = typename Mfma<DT>::v8;
+                    s[g] = Mfma<DT>::mac(__builtin_bit_cast(v8, t.k[g][c]), __builtin_bit_cast(v8, q[c]), s[g]);
+                }
+            }
+        }
+        if (MASS) {
+            // kept in the order of the walk; a head's four scores of neighbouring keys in one store
+            float* to = a.scores + (head0 + n) * a.score_stride + p0 * 64 + (int64_t)(wave + 4 * i) * STEP + 4 * j;
+#pragma unroll
+            for (int g = 0; g < SUB; ++g) {
+                if (n < heads) {
+                    if (16 * g + 4 * j + 3 < rows) {
+                        __builtin_memcpy(to + 16 * g, &s[g], 16);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (16 * g + 4 * j + r < rows) to[16 * g + r] = s[g][r];
+                    }
+                }
+            }
+        }
+        float p[KEYS];
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < KEYS; ++e) {
+            p[e] = s[e / 4][e % 4];
+            if (rows < STEP && 16 * (e / 4) + 4 * j + e % 4 >= rows) p[e] = -INFINITY;
+            top = fmaxf(top, p[e]);
+        }
+        const float m_new = fmaxf(m, max_over_rows(top) * a.scale_log2e);
+        const float ref = (m_new == -INFINITY ? 0.f : m_new) - WeightShift<DT>::value;      // (nothing but -inf so far: weights of zero)
+        const float alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.f : m_new));
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int e = 0; e < KEYS; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2e, -ref));
+            l += p[e];
+        }
+#pragma unroll
+        for (int c = 0; c < T; ++c) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[c][r] *= alpha;
+        }
+        if constexpr (DT == DT_F32) {
+#pragma unroll
+            for (int c = 0; c < T; ++c) {
+#pragma unroll
+                for (int e = 0; e < KEYS; ++e) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[e][c]), p[e], acc[c], 0, 0, 0);
+            }
+        } else {
+            using v8 = typename Mfma<DT>::v8;
+            v8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                hi[e] = (decltype(+hi[0]))p[e];
+                lo[e] = (decltype(+lo[0]))(p[e] - (float)hi[e]);
+            }
+#pragma unroll
+            for (int c = 0; c < T; ++c) {
+                // channel column of the lane's eight keys: pairs of rows, one 16-bit half each
+                const int w = (c / EV) * (Tile::VLOAD / 4) + (c % EV) / 2;
+                const uint32_t half = c % 2 ? 0x07060302u : 0x05040100u;
+                u32x4 col;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) col[x] = __builtin_amdgcn_perm(t.v[2 * x + 1][w], t.v[2 * x][w], half);
+                acc[c] = Mfma<DT>::mac(__builtin_bit_cast(v8, col), hi, acc[c]);
+                acc[c] = Mfma<DT>::mac(__builtin_bit_cast(v8, col), lo, acc[c]);
+            }
+        }
+    };
+    const int mine = n_steps > wave ? (n_steps - wave + 3) / 4 : 0;
+    if constexpr (Tile::kPipelined) {
+        Tile ta, tb;
+        int ra = 0, rb_ = 0;
+        if (mine > 0) load(ta, 0, ra);
+        for (int i = 0; i < mine; i += 2) {
+            load(tb, i + 1, rb_);
+            __builtin_amdgcn_sched_barrier(0);
+            use(ta, i, ra);
+            if (i + 1 >= mine) break;
+            load(ta, i + 2, ra);
+            __builtin_amdgcn_sched_barrier(0);
+            use(tb, i + 1, rb_);
+        }
+    } else {
+        Tile t;
+        int r = 0;
+        for (int i = 0; i < mine; ++i) {
+            load(t, i, r);
+            __builtin_amdgcn_sched_barrier(0);
+            use(t, i, r);
+        }
+    }
+    l = add_lanes_32(add_lanes_16(l));
+    // the four waves' sums, relative to the largest of their maxima
+    if (j == 0) { red_m[wave][n] = m; red_l[wave][n] = l; }
+    if (n < heads) {
+#pragma unroll
+        for (int c = 0; c < T; ++c) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[wave][n][Tile::channel(c, 4 * j + r)] = acc[c][r];
+        }
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < heads * D; i += 256) {
+        const int h = i / D, c = i - h * D;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, red_m[w][h]);
+        float sum = 0.f, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = red_m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[w][h] - top);
+            if (f != 0.f) { sum = fmaf(f, red[w][h][c], sum); total = fmaf(f, red_l[w][h], total); }
+        }
+        const int64_t bh = head0 + h;
+        if (a.n_split == 1) {
+            a.out[bh * D + c] = sum / total;
+            if (c == 0 && a.lse) a.lse[bh] = (top - WeightShift<DT>::value) * 0.69314718055994531f + logf(total);
+        } else {
+            a.part_acc[(bh * a.n_split + split) * D + c] = sum;
+        }
+        if (c == 0) {
+            a.part_lm[(bh * a.n_split + split) * 2] = total;
+            a.part_lm[(bh * a.n_split + split) * 2 + 1] = top;
+        }
+    }
+}
+
+// Splits of sequence b.
+__device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t N) {
+    int64_t pages = (N + 63) / 64;
+    if (a.list && a.n_list < pages) pages = a.n_list;
+    return (int)((pages + a.chunk - 1) / a.chunk);
+}
+// log2 of the sum of a head's weights (not shifted), over its splits; one wave.  `top`: what its partial sums are relative to the largest of.
+__device__ __forceinline__ float head_log2_sum(const AttendCall& a, int64_t bh, int n_split, float shift, float* top_out) {
+    const float* lm = a.part_lm + bh * a.n_split * 2;
+    float top = -INFINITY;
+    for (int i = lane_id(); i < n_split; i += kWave) top = fmaxf(top, lm[2 * i + 1]);
+    top = wave_max(top);
+    float sum = 0.f;
+    for (int i = lane_id(); i < n_split; i += kWave) {
+        const float f = lm[2 * i + 1] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lm[2 * i + 1] - top);
+        if (f != 0.f) sum = fmaf(f, lm[2 * i], sum);
+    }
+    sum = group_reduce<AddOp, 64>(sum);
+    *top_out = top;
+    return (top - shift) + log2f(sum);
+}
+
+constexpr int kMassPerBlock = 1024;      // keys whose weights one workgroup adds up
+
+// The first B * Hq workgroups put a head's splits together; the others (with `mass`) add each key's weights, the heads of the group in
+// order, from the scores that the walk left: 4 bytes per key and head written and read, where a second walk over the keys reads 2 d / G.
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendCall a, float shift, int n_join) {
+    __shared__ float lg[128];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if ((int)blockIdx.x < n_join) {
+        __shared__ float f[1024];
+        const int64_t bh = blockIdx.x;
+        const int ns = attend_splits(a, a.len[bh / a.Hq]);
+        float top;
+        const float lg2 = head_log2_sum(a, bh, ns, shift, &top);      // (every wave: no exchange)
+        const float* lm = a.part_lm + bh * a.n_split * 2;
+        for (int i = (int)threadIdx.x; i < ns; i += 256)
+            f[i] = lm[2 * i + 1] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lm[2 * i + 1] - top - (lg2 - (top - shift)));
+        __syncthreads();
+        for (int c = (int)threadIdx.x; c < a.D; c += 256) {
+            const float* p = a.part_acc + bh * a.n_split * a.D + c;
+            float sum = 0.f;
+#pragma unroll 8
+            for (int i = 0; i < ns; ++i)
+                if (f[i] != 0.f) sum = fmaf(f[i], p[(int64_t)i * a.D], sum);
+            a.out[bh * a.D + c] = sum;
+        }
+        if (threadIdx.x == 0 && a.lse) a.lse[bh] = lg2 * 0.69314718055994531f;
+        return;
+    }
+    const int per_stream = (int)((a.walk + kMassPerBlock - 1) / kMassPerBlock);
+    const int stream = ((int)blockIdx.x - n_join) / per_stream, part = ((int)blockIdx.x - n_join) - stream * per_stream;
+    const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
+    const int64_t N = a.len[b];
+    const int64_t i0 = (int64_t)part * kMassPerBlock;
+    const int64_t pages_b = (N + 63) / 64, pages = a.list && a.n_list < pages_b ? a.n_list : pages_b;
+    if (i0 >= pages * 64) return;
+    const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G;
+    const int ns = attend_splits(a, N);
+    for (int g = wave; g < a.G; g += 4) {
+        float top;
+        const float v = head_log2_sum(a, head0 + g, ns, shift, &top);
+        if (lane_id() == 0) lg[g] = v;
+    }
+    __syncthreads();
+    const float* const s0 = a.scores + head0 * a.score_stride;
+    float* const mass = a.mass + (int64_t)stream * a.Ncap;
+    constexpr int U = kMassPerBlock / 256;
+    int64_t at[U], pos[U];
+    float w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        at[u] = i0 + u * 256 + (int)threadIdx.x;
+        pos[u] = at[u];
+        if (at[u] >= pages * 64) pos[u] = N;
+        else if (a.list) pos[u] = (int64_t)a.list[(int64_t)stream * a.list_stride + at[u] / 64] * 64 + at[u] % 64;
+        if (pos[u] >= N) at[u] = i0;                              // (nothing to add: any score)
+        w[u] = 0.f;
+    }
+#pragma unroll 4
+    for (int g = 0; g < a.G; ++g) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] += __builtin_amdgcn_exp2f(fmaf(s0[g * a.score_stride + at[u]], a.scale_log2e, -lg[g]));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (pos[u] < N) mass[pos[u]] += w[u];
+}
+
+hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
+    const int64_t units = (int64_t)a.B * a.Hkv * a.n_split;
+    const int64_t blocks = a.row_blocks > 1 ? (units + 7) / 8 * 8 * a.row_blocks : units;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+#define TKA_ATTEND(DT_, D_)                                                                                                               \
+    do {                                                                                                                                  \
+        if (a.list && a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);       \
+        else if (a.list) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, false>), dim3((unsigned)blocks), dim3(256), 0, st, a);           \
+        else if (a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, false, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);           \
+        else hipLaunchKernelGGL((attend_kernel<DT_, D_, false, false>), dim3((unsigned)blocks), dim3(256), 0, st, a);                      \
+    } while (0)
+    TKA_BY_TYPE_AND_DIM(TKA_ATTEND, a.dtype, a.D);
+#undef TKA_ATTEND
+    hipError_t e = hipGetLastError();
+    const int n_join = a.n_split > 1 ? a.B * a.Hq : 0;
+    const int64_t n_mass = a.mass ? (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock) : 0;
+    if (n_join + n_mass > INT32_MAX) return hipErrorInvalidValue;
+    if (e != hipSuccess || n_join + n_mass == 0) return e;
+    hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, n_join);
+    return hipGetLastError();
+}
+
+}  // namespace tka

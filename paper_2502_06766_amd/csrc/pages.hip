@@ -15,6 +15,7 @@
 // pattern of the pages kept (scan.hip), and leaves their numbers, ascending, and their count per key stream to be held against the mask.
 #include "device_utils.h"
 #include "internal.h"
+#include "ops.h"
 #include "scan_tiles.h"
 
 namespace tka {
@@ -30,8 +31,8 @@ page_ball_kernel(const char* __restrict__ K, int64_t Ncap, int64_t Pcap, int Hkv
     constexpr int EPL = 8;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     const int kvh = blockIdx.y, b = blockIdx.z;
-    const int64_t row0 = len_dev ? (int64_t)len_dev[b] : row0_host;      // a batched append reads each sequence's length
-    const int64_t n_total = row0 + n_new;
+    const int64_t at = len_dev ? (int64_t)len_dev[b] : row0_host;        // a batched append reads each sequence's length
+    const int64_t row0 = n_new < 0 ? 0 : at, n_total = n_new < 0 ? at : at + n_new;      // (n_new < 0: all rows below the length)
     const int64_t page = row0 / 64 + (int64_t)blockIdx.x * 4 + wave;
     if (page * 64 >= n_total) return;
     const int64_t first = page * 64;
@@ -170,10 +171,8 @@ __global__ void __launch_bounds__(256) page_filter_kernel(Shape sh, Bufs bf, flo
     if (lane == 0) *out = m;
 }
 
-hipError_t launch_page_balls(int dtype, int D, const void* K, int64_t Ncap, int64_t Pcap, int Hkv, int B,
-                             const int32_t* len_dev, int64_t row0, int64_t n_new, void* centres, float* balls, hipStream_t st) {
-    if (n_new <= 0) return hipSuccess;
-    const int64_t pages = (n_new + 63) / 64 + 1;                      // the first page touched may be a partly filled one
+static hipError_t enqueue_page_balls(int dtype, int D, const void* K, int64_t Ncap, int64_t Pcap, int Hkv, int B, int64_t pages,
+                                     const int32_t* len_dev, int64_t row0, int64_t n_new, void* centres, float* balls, hipStream_t st) {
     const dim3 grid((unsigned)((pages + 3) / 4), (unsigned)Hkv, (unsigned)B);
 #define TKA_PB(DT_, D_)                                                                                                  \
     hipLaunchKernelGGL((page_ball_kernel<DT_, D_>), grid, dim3(256), 0, st, static_cast<const char*>(K), Ncap, Pcap, Hkv, \
@@ -189,6 +188,20 @@ hipError_t launch_page_balls(int dtype, int D, const void* K, int64_t Ncap, int6
     else return hipErrorInvalidValue;
 #undef TKA_PB
     return hipGetLastError();
+}
+
+hipError_t launch_page_balls(int dtype, int D, const void* K, int64_t Ncap, int64_t Pcap, int Hkv, int B,
+                             const int32_t* len_dev, int64_t row0, int64_t n_new, void* centres, float* balls, hipStream_t st) {
+    if (n_new <= 0) return hipSuccess;
+    // (one more than the rows fill: the first page touched may be a partly filled one)
+    return enqueue_page_balls(dtype, D, K, Ncap, Pcap, Hkv, B, (n_new + 63) / 64 + 1, len_dev, row0, n_new, centres, balls, st);
+}
+
+// The balls of all pages below the device lengths (of which none exceeds `rows`).
+hipError_t launch_balls_again(int dtype, int D, const void* K, int64_t Ncap, int64_t Pcap, int Hkv, int B, const int32_t* len_dev,
+                              int64_t rows, void* centres, float* balls, hipStream_t st) {
+    if (rows <= 0) return hipSuccess;
+    return enqueue_page_balls(dtype, D, K, Ncap, Pcap, Hkv, B, (rows + 63) / 64, len_dev, 0, -1, centres, balls, st);
 }
 
 bool pages_supported(int dtype, int D, int G) {

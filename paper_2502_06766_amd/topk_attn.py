@@ -17,10 +17,11 @@ LIB_PATH = os.path.join(_HERE, "libtopk_attn.so")
 OK, EINVAL, ECAPACITY, EUNSUPPORTED, EDEVICE, ENOMEM, ESCRATCH = range(7)
 F32, F16, BF16 = 0, 1, 2
 PATH_AUTO, PATH_FULL, PATH_FILTER, PATH_INDEX, PATH_PAGES = 0, 1, 2, 3, 4
-INDEX_NONE, INDEX_INT8, INDEX_PAGES = 0, 1, 2
+INDEX_NONE, INDEX_INT8, INDEX_PAGES, INDEX_BOXES = 0, 1, 2, 4
 
 EXPORTS = [
-    "topk_attn_kv_bytes", "topk_attn_workspace_bytes", "topk_attn_layers_workspace_bytes", "topk_attn_create", "topk_attn_append_kv", "topk_attn_append_step",
+    "topk_attn_kv_bytes", "topk_attn_workspace_bytes", "topk_attn_layers_workspace_bytes", "topk_attn_create", "topk_attn_append_kv", "topk_attn_append_step", "topk_attn_append_rotary",
+    "topk_attn_decode_dense", "topk_attn_decode_blocks", "topk_attn_add_mass", "topk_attn_evict",
     "topk_attn_decode", "topk_attn_decode_static", "topk_attn_decode_window", "topk_attn_decode_multi", "topk_attn_decode_layers", "topk_attn_k_schedule", "topk_attn_scores", "topk_attn_length", "topk_attn_reset", "topk_attn_set_path",
     "topk_attn_last_fallbacks", "topk_attn_set_page_bound_scale", "topk_attn_last_pages_read", "topk_attn_last_selection_records", "topk_attn_debug_read_workspace", "topk_attn_debug_read_workspace_dims", "topk_attn_debug_force_redo", "topk_attn_set_scan_timing", "topk_attn_scan_time", "topk_attn_read_probe", "topk_attn_build_id", "topk_attn_strerror", "topk_attn_destroy",
 ]
@@ -46,6 +47,31 @@ class Config(ctypes.Structure):
         ("kv_bytes", ctypes.c_size_t),
         ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class Rotary(ctypes.Structure):
+    """Mirror of topk_attn_rotary."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("norm_eps", ctypes.c_float),
+        ("n_new", ctypes.c_int64),
+        ("q", ctypes.c_void_p),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("q_seq_stride", ctypes.c_int64),
+        ("q_token_stride", ctypes.c_int64),
+        ("k_seq_stride", ctypes.c_int64),
+        ("k_token_stride", ctypes.c_int64),
+        ("v_seq_stride", ctypes.c_int64),
+        ("v_token_stride", ctypes.c_int64),
+        ("q_out", ctypes.c_void_p),
+        ("q_norm", ctypes.c_void_p),
+        ("k_norm", ctypes.c_void_p),
+        ("inv_freq", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
     ]
 
 
@@ -78,6 +104,16 @@ def lib() -> ctypes.CDLL:
         L.topk_attn_append_kv.restype = i32
         L.topk_attn_append_step.argtypes = [vp, i32, vp, vp, i64, vp]
         L.topk_attn_append_step.restype = i32
+        L.topk_attn_append_rotary.argtypes = [vp, i32, i32, ctypes.POINTER(Rotary), vp]
+        L.topk_attn_append_rotary.restype = i32
+        L.topk_attn_decode_dense.argtypes = [vp, i32, vp, vp, vp, vp, vp]
+        L.topk_attn_decode_dense.restype = i32
+        L.topk_attn_decode_blocks.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp]
+        L.topk_attn_decode_blocks.restype = i32
+        L.topk_attn_add_mass.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp]
+        L.topk_attn_add_mass.restype = i32
+        L.topk_attn_evict.argtypes = [vp, i32, vp, i64, i64, vp, vp]
+        L.topk_attn_evict.restype = i32
         L.topk_attn_decode.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp]
         L.topk_attn_decode.restype = i32
         L.topk_attn_decode_static.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp]
@@ -185,6 +221,29 @@ def topk_attn_append_kv(h, layer, seq, k_new_ptr, v_new_ptr, n_new, token_stride
 
 def topk_attn_append_step(h, layer, k_new_ptr, v_new_ptr, n_new, stream=0):
     _check(lib().topk_attn_append_step(h, layer, k_new_ptr, v_new_ptr, n_new, stream), "topk_attn_append_step")
+
+
+def topk_attn_append_rotary(h, layer, seq, rotary: Rotary, stream=0):
+    """seq: a sequence, or -1 for all of the layer's."""
+    _check(lib().topk_attn_append_rotary(h, layer, seq, ctypes.byref(rotary), stream), "topk_attn_append_rotary")
+
+
+def topk_attn_decode_dense(h, layer, q_ptr, out_ptr, lse_ptr=0, mass_ptr=0, stream=0):
+    _check(lib().topk_attn_decode_dense(h, layer, q_ptr, out_ptr, lse_ptr or None, mass_ptr or None, stream),
+           "topk_attn_decode_dense")
+
+
+def topk_attn_decode_blocks(h, layer, q_ptr, n_blocks, out_ptr, blocks_ptr=0, lse_ptr=0, mass_ptr=0, stream=0):
+    _check(lib().topk_attn_decode_blocks(h, layer, q_ptr, n_blocks, out_ptr, blocks_ptr or None, lse_ptr or None,
+                                         mass_ptr or None, stream), "topk_attn_decode_blocks")
+
+
+def topk_attn_add_mass(h, layer, idx_ptr, vals_ptr, lse_ptr, k, mass_ptr, stream=0):
+    _check(lib().topk_attn_add_mass(h, layer, idx_ptr, vals_ptr, lse_ptr, k, mass_ptr, stream), "topk_attn_add_mass")
+
+
+def topk_attn_evict(h, layer, mass_ptr, budget, recent=0, kept_ptr=0, stream=0):
+    _check(lib().topk_attn_evict(h, layer, mass_ptr, budget, recent, kept_ptr or None, stream), "topk_attn_evict")
 
 
 def topk_attn_decode(h, layer, q_ptr, k, out_ptr, idx_ptr=0, vals_ptr=0, lse_ptr=0, stream=0):
@@ -353,6 +412,79 @@ class TopkAttnCache:
         assert k_new.is_cuda and v_new.is_cuda and k_new.dtype == self.torch_dtype()
         assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.shape == v_new.shape
         topk_attn_append_step(self.h, layer, k_new.data_ptr(), v_new.data_ptr(), k_new.shape[1], self._stream())
+
+    def append_rotary(self, layer, q, k, v, inv_freq, positions=None, q_norm=None, k_norm=None, eps=1e-6, interleaved=False, seq=-1):
+        """q [S, n, Hq, d] (or None), k, v [S, n, Hkv, d] device tensors whose heads lie together (views of a fused projection will do):
+        the keys and queries normalised (by weights [d], or not) and rotated by inv_freq [rotary / 2] fp32, keys and values appended to
+        all sequences of the layer, or to `seq` (S = 1).  positions [S, n] int32, by default the cache rows.  -> q [S, n, Hq, d]."""
+        t = self.torch
+        B, n, Hkv, d = k.shape
+        dt = self.torch_dtype()
+        for x, heads in ((q, self.shape[2]), (k, self.shape[3]), (v, self.shape[3])):
+            if x is not None:
+                assert x.device == self.device and x.dtype == dt and x.shape == (B, n, heads, self.shape[4])
+                assert x.stride(3) == 1 and (heads == 1 or x.stride(2) == d)
+        assert B == (self.shape[1] if seq < 0 else 1)
+        assert inv_freq.device == self.device and inv_freq.dtype == t.float32 and inv_freq.is_contiguous()
+        for w in (q_norm, k_norm):
+            assert w is None or (w.device == self.device and w.dtype == dt and w.shape == (d,) and w.is_contiguous())
+        if positions is not None:
+            assert positions.device == self.device and positions.dtype == t.int32 and positions.shape == (B, n) and positions.is_contiguous()
+        out = None if q is None else t.empty((B, n, self.shape[2], d), dtype=dt, device=self.device)
+        ptr = lambda x: None if x is None else x.data_ptr()
+        step = lambda x: (0, 0) if x is None else (x.stride(0) if B > 1 else 0, x.stride(1) if n > 1 else 0)      # (one of them: any stride)
+        topk_attn_append_rotary(self.h, layer, seq, Rotary(
+            ctypes.sizeof(Rotary), 2 * inv_freq.numel(), 1 if interleaved else 0, eps, n, ptr(q), ptr(k), ptr(v), *step(q), *step(k), *step(v),
+            ptr(out), ptr(q_norm), ptr(k_norm), ptr(inv_freq), ptr(positions)), self._stream())
+        return out
+
+    def _mass_ptr(self, mass):
+        if mass is None:
+            return 0
+        t = self.torch
+        assert mass.device == self.device and mass.dtype == t.float32 and mass.is_contiguous()
+        assert mass.shape == (self.shape[1], self.shape[3], self.shape[5])
+        return mass.data_ptr()
+
+    def decode_dense(self, layer, q, want_lse=True, mass=None):
+        """q [B, Hq, d] -> (out, lse) over all cached tokens; their weights are added to mass [B, Hkv, max_tokens] fp32."""
+        t = self.torch
+        assert q.device == self.device and q.is_contiguous() and q.dtype == self.torch_dtype()
+        assert q.shape == (self.shape[1], self.shape[2], self.shape[4])
+        out = t.empty(q.shape, dtype=t.float32, device=self.device)
+        lse = t.empty(q.shape[:2], dtype=t.float32, device=self.device) if want_lse else None
+        topk_attn_decode_dense(self.h, layer, q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, self._mass_ptr(mass),
+                               self._stream())
+        return out, lse
+
+    def decode_blocks(self, layer, q, n_blocks, want_blocks=True, want_lse=True, mass=None):
+        """q [B, Hq, d] -> (out, blocks [B, Hkv, n_blocks], lse) over the n_blocks best pages of each KV head (index_kind INDEX_BOXES)."""
+        t = self.torch
+        assert q.device == self.device and q.is_contiguous() and q.dtype == self.torch_dtype()
+        assert q.shape == (self.shape[1], self.shape[2], self.shape[4])
+        out = t.empty(q.shape, dtype=t.float32, device=self.device)
+        blocks = t.empty((self.shape[1], self.shape[3], max(n_blocks, 0)), dtype=t.int32, device=self.device) if want_blocks else None
+        lse = t.empty(q.shape[:2], dtype=t.float32, device=self.device) if want_lse else None
+        topk_attn_decode_blocks(self.h, layer, q.data_ptr(), n_blocks, out.data_ptr(), blocks.data_ptr() if want_blocks else 0,
+                                lse.data_ptr() if want_lse else 0, self._mass_ptr(mass), self._stream())
+        return out, blocks, lse
+
+    def add_mass(self, layer, idx, vals, lse, mass):
+        """Adds the weights of a top-k decode's selection (its idx, vals, lse) to mass [B, Hkv, max_tokens] fp32."""
+        t = self.torch
+        assert idx.dtype == t.int32 and vals.dtype == t.float32 and lse.dtype == t.float32
+        assert all(x.device == self.device and x.is_contiguous() and x.shape[:2] == self.shape[1:3] for x in (idx, vals, lse))
+        assert idx.dim() == 3 and vals.shape == idx.shape and lse.dim() == 2
+        topk_attn_add_mass(self.h, layer, idx.data_ptr(), vals.data_ptr(), lse.data_ptr(), idx.shape[2], self._mass_ptr(mass),
+                           self._stream())
+
+    def evict(self, layer, mass, budget, recent=0, want_kept=True):
+        """Cuts every sequence of the layer to `budget` tokens: the `recent` newest and, per KV head, those with the largest mass.
+        -> the positions kept [B, Hkv, budget] (or None)."""
+        t = self.torch
+        kept = t.empty((self.shape[1], self.shape[3], max(budget, 0)), dtype=t.int32, device=self.device) if want_kept else None
+        topk_attn_evict(self.h, layer, self._mass_ptr(mass), budget, recent, kept.data_ptr() if want_kept else 0, self._stream())
+        return kept
 
     def decode(self, layer, q, k, want_idx=True, want_vals=True, want_lse=True, window=0):
         """q [B, Hq, d] device tensor -> (out, idx, vals, lse) device tensors (None if not wanted)."""
