@@ -211,8 +211,9 @@ int topk_attn_decode(topk_attn_t* h, int layer, const void* q, int k, float* out
  * library: a device array of TOPK_ATTN_STATIC_SCRATCH_BYTES that every GPU the library runs on
  * holds until the process ends.  Only the cache lengths are still read from the handle's
  * workspace.  The call allocates and frees nothing and enqueues kernels only.
- * Limit: ESCRATCH (nothing enqueued) if topk_attn_workspace_bytes(cfg) minus the lengths' share
- * (n_layers * n_seqs * 4, rounded up to 256) exceeds TOPK_ATTN_STATIC_SCRATCH_BYTES -- one
+ * Limit: ESCRATCH (nothing enqueued) if topk_attn_workspace_bytes(cfg) minus the share of the
+ * lengths (n_layers * n_seqs * 4, rounded up to 256) and of the dense decode's counters (4 bytes per sequence and 16 heads
+ * of a KV head, rounded up) exceeds TOPK_ATTN_STATIC_SCRATCH_BYTES -- one
  * Llama-8B-shaped layer of 128k tokens at k = 2048 fits, a million-token layer does not.
  * All calls on one GPU, from whatever handle, share the one array: the call clears the words
  * that must start at zero itself, and two such calls that overlap in time on one GPU race. */

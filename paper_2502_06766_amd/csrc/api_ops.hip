@@ -54,7 +54,6 @@ T* scratch_at(const topk_attn* h, size_t offset) { return reinterpret_cast<T*>(s
 
 // Pages that one workgroup of the walk takes, two workgroups to a compute unit in all: a workgroup's waves need a few steps each to keep
 // their loads in flight, and a part of a round at the end costs as much as a whole one.  At least two pages: a step per wave.
-constexpr int64_t kMaxSplits = 1024;             // weights of a head's splits in LDS (attend_join_kernel)
 int64_t pages_per_split(const topk_attn* h, int64_t total_pages, int64_t longest, int64_t max_splits) {
     const int64_t wgs = 2 * (int64_t)h->n_cu;
     int64_t chunk = std::max<int64_t>(2, (total_pages + wgs - 1) / wgs);
@@ -110,6 +109,7 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     a.n_split = (int)((pages + a.chunk - 1) / a.chunk);
     a.part_acc = scratch_at<float>(h, h->ws.cand);
     a.part_lm = a.part_acc + (size_t)a.B * a.Hq * a.n_split * a.D;
+    a.arrive = scratch_at<uint32_t>(h, h->ws.arrive);
     a.out = out; a.lse = lse; a.mass = mass;
     a.scale_log2e = 1.4426950408889634f / sqrtf((float)c.head_dim);
     const hipError_t e = launch_attend(a, st);

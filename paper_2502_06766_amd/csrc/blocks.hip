@@ -79,21 +79,130 @@ __device__ __forceinline__ uint64_t ord_of(double v) {
 // One workgroup per key stream.  The page that ends the selection (its score, and among equal scores its number: lower ones first) is
 // found from a linear histogram between the smallest and the largest score, whose one bin in question is ranked by direct comparison,
 // or, where that bin is crowded or the scores are not finite, byte by byte of their ordered bits.  Then the pages up to it are written in
-// their order.  Each thread has `per` neighbouring pages; their scores are read again in each pass (L2: 8 bytes a page).
-constexpr int kPickThreads = 1024, kPickBins = 1024, kPickList = 2048;
-__global__ void __launch_bounds__(kPickThreads) block_select_kernel(BlockCall a) {
+// their order.  Each thread has `per` neighbouring pages: up to 16 of them stay in its registers (16384 pages, a million tokens: 37 us
+// when each of the five passes reads them again), and beyond they are read again.
+constexpr int kPickThreads = 1024, kPickBins = 1024, kPickList = 2048, kPickHeld = 16;
+struct PickShared {
+    uint32_t tot[2][16];
+    float red[2][2][16];
+    uint32_t hist[kPickBins];
+    uint64_t key[kPickList];
+    uint32_t page[kPickList];
+    uint32_t n_list, bin, need;
+    uint64_t edge_key, prefix;
+    uint32_t edge_page;
+};
+template <bool HELD>
+__device__ __forceinline__ void pick_pages(const double* score, int32_t* list, int64_t n, uint32_t want, PickShared& sm) {
     using Team = WorkgroupTeam<kPickThreads>;
-    struct SM {
-        uint32_t tot[2][16];
-        float red[2][2][16];
-        uint32_t hist[kPickBins];
-        uint64_t key[kPickList];
-        uint32_t page[kPickList];
-        uint32_t n_list, bin, need;
-        uint64_t edge_key, prefix;
-        uint32_t edge_page;
+    const int tid = (int)threadIdx.x;
+    const int64_t per = (n + kPickThreads - 1) / kPickThreads;
+    const int64_t i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
+    double held[HELD ? kPickHeld : 1];
+    if (HELD) {
+#pragma unroll
+        for (int u = 0; u < kPickHeld; ++u) held[u] = i0 + u < i1 ? score[i0 + u] : 0.0;
+    }
+    auto each = [&](auto f) {                                  // f(page, its score) for the thread's pages in order
+        if (HELD) {
+#pragma unroll
+            for (int u = 0; u < kPickHeld; ++u)
+                if (i0 + u < i1) f(i0 + u, held[u]);
+        } else {
+            for (int64_t i = i0; i < i1; ++i) f(i, score[i]);
+        }
     };
-    __shared__ SM sm;
+    // range of the scores, in 32 bits (a histogram edge needs no more)
+    float lo = INFINITY, hi = -INFINITY;
+    bool bad = false;
+    each([&](int64_t, double s) {
+        const float v = (float)s;
+        bad |= !(fabsf(v) < INFINITY);
+        lo = fminf(lo, v); hi = fmaxf(hi, v);
+    });
+    if (bad) { lo = -INFINITY; hi = INFINITY; }
+    for (int i = tid; i < kPickBins; i += kPickThreads) sm.hist[i] = 0;
+    if (tid == 0) sm.n_list = 0;
+    team_range<Team>(lo, hi, sm, 0);
+    const float inv = (float)kPickBins / (hi - lo);
+    bool listed = hi < INFINITY && lo > -INFINITY && hi > lo && inv < INFINITY;
+    // (monotone: a rounding, a difference and a product with a positive number)
+    auto bin_of = [&](double s) { const int x = (int)(((float)s - lo) * inv); return x < kPickBins - 1 ? x : kPickBins - 1; };
+    if (listed) {
+        each([&](int64_t, double s) { atomicAdd(&sm.hist[bin_of(s)], 1u); });
+        __syncthreads();
+        // thread t looks at bin 1023 - t: the bin in which the want-th score from above lies
+        const uint32_t c = sm.hist[kPickBins - 1 - tid];
+        uint32_t total;
+        const uint32_t above = team_prefix<Team>(c, total, sm, 0);
+        if (above < want && above + c >= want) { sm.bin = (uint32_t)(kPickBins - 1 - tid); sm.need = want - above; }
+        __syncthreads();
+        const int bin = (int)sm.bin;
+        listed = sm.hist[bin] <= kPickList;
+        if (listed) {
+            each([&](int64_t i, double s) {
+                if (bin_of(s) == bin) {
+                    const uint32_t at = atomicAdd(&sm.n_list, 1u);      // (in any order: they are ranked by score and number)
+                    sm.key[at] = ord_of(s); sm.page[at] = (uint32_t)i;
+                }
+            });
+            __syncthreads();
+            const uint32_t have = sm.n_list, need = sm.need;
+            for (uint32_t x = (uint32_t)tid; x < have; x += kPickThreads) {
+                const uint64_t kx = sm.key[x];
+                const uint32_t px = sm.page[x];
+                uint32_t rank = 0;
+                for (uint32_t y = 0; y < have; ++y) rank += sm.key[y] > kx || (sm.key[y] == kx && sm.page[y] < px);
+                if (rank == need - 1) { sm.edge_key = kx; sm.edge_page = px; }
+            }
+        }
+    }
+    if (!listed) {
+        // byte by byte: the key of the want-th page, then among the pages of that key the want-th of what is left
+        uint64_t prefix = 0;
+        uint32_t need = want;
+        for (int shift = 56; shift >= 0; shift -= 8) {
+            __syncthreads();
+            for (int i = tid; i < 256; i += kPickThreads) sm.hist[i] = 0;
+            __syncthreads();
+            const uint64_t mask = shift == 56 ? 0ull : ~0ull << (shift + 8);
+            each([&](int64_t, double s) {
+                const uint64_t k = ord_of(s);
+                if ((k & mask) == prefix) atomicAdd(&sm.hist[(k >> shift) & 255], 1u);
+            });
+            __syncthreads();
+            const uint32_t c = tid < 256 ? sm.hist[255 - tid] : 0u;
+            uint32_t total;
+            const uint32_t above = team_prefix<Team>(c, total, sm, 0);
+            if (above < need && above + c >= need) { sm.prefix = prefix | ((uint64_t)(255 - tid) << shift); sm.need = need - above; }
+            __syncthreads();
+            prefix = sm.prefix; need = sm.need;
+        }
+        uint32_t same = 0;
+        each([&](int64_t, double s) { same += ord_of(s) == prefix; });
+        uint32_t total;
+        uint32_t before = team_prefix<Team>(same, total, sm, 1);
+        each([&](int64_t i, double s) {
+            if (ord_of(s) == prefix && ++before == need) { sm.edge_key = prefix; sm.edge_page = (uint32_t)i; }
+        });
+    }
+    __syncthreads();
+    const uint64_t edge_key = sm.edge_key;                     // selected: key > edge_key, or equal and page <= edge_page
+    const uint32_t edge_page = sm.edge_page;
+    auto picked = [&](int64_t i, double s) {
+        const uint64_t k = ord_of(s);
+        return k > edge_key || (k == edge_key && (uint32_t)i <= edge_page);
+    };
+    uint32_t mine = 0;
+    each([&](int64_t i, double s) { mine += picked(i, s); });
+    uint32_t total;
+    uint32_t at = team_prefix<Team>(mine, total, sm, 0);
+    each([&](int64_t i, double s) {
+        if (picked(i, s)) list[at++] = (int32_t)i;
+    });
+}
+__global__ void __launch_bounds__(kPickThreads) block_select_kernel(BlockCall a) {
+    __shared__ PickShared sm;
     const int tid = (int)threadIdx.x;
     const int64_t stream = blockIdx.x;
     const int64_t P = ((int64_t)a.len[stream / a.Hkv] + 63) / 64;
@@ -103,107 +212,11 @@ __global__ void __launch_bounds__(kPickThreads) block_select_kernel(BlockCall a)
         return;
     }
     const double* const score = a.score + stream * a.Pcap;
-    const int64_t n = P - 1;                                   // the newest page is in without a search
-    const uint32_t want = (uint32_t)a.n_blocks - 1;            // 0 <= want < n
-    const int64_t per = (n + kPickThreads - 1) / kPickThreads;
-    const int64_t i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
-    uint64_t edge_key = ~0ull;                                 // selected: key > edge_key, or equal and page <= edge_page
-    uint32_t edge_page = 0;
-    if (want > 0) {
-        // range of the scores, in 32 bits (a histogram edge needs no more)
-        float lo = INFINITY, hi = -INFINITY;
-        bool bad = false;
-        for (int64_t i = i0; i < i1; ++i) {
-            const float v = (float)score[i];
-            bad |= !(fabsf(v) < INFINITY);
-            lo = fminf(lo, v); hi = fmaxf(hi, v);
-        }
-        if (bad) { lo = -INFINITY; hi = INFINITY; }
-        for (int i = tid; i < kPickBins; i += kPickThreads) sm.hist[i] = 0;
-        if (tid == 0) { sm.n_list = 0; sm.bin = kPickBins; }
-        team_range<Team>(lo, hi, sm, 0);
-        const float inv = (float)kPickBins / (hi - lo);
-        bool listed = hi < INFINITY && lo > -INFINITY && hi > lo && inv < INFINITY;
-        // (monotone: a rounding, a difference and a product with a positive number)
-        auto bin_of = [&](double s) { const int x = (int)(((float)s - lo) * inv); return x < kPickBins - 1 ? x : kPickBins - 1; };
-        if (listed) {
-            for (int64_t i = i0; i < i1; ++i) atomicAdd(&sm.hist[bin_of(score[i])], 1u);
-            __syncthreads();
-            // thread t looks at bin 1023 - t: the bin in which the want-th score from above lies
-            const uint32_t c = sm.hist[kPickBins - 1 - tid];
-            uint32_t total;
-            const uint32_t above = team_prefix<Team>(c, total, sm, 0);
-            if (above < want && above + c >= want) { sm.bin = (uint32_t)(kPickBins - 1 - tid); sm.need = want - above; }
-            __syncthreads();
-            const int bin = (int)sm.bin;
-            listed = sm.hist[bin] <= kPickList;
-            if (listed) {
-                for (int64_t i = i0; i < i1; ++i) {
-                    const double s = score[i];
-                    if (bin_of(s) == bin) {
-                        const uint32_t at = atomicAdd(&sm.n_list, 1u);      // (in any order: they are ranked by score and number)
-                        sm.key[at] = ord_of(s); sm.page[at] = (uint32_t)i;
-                    }
-                }
-                __syncthreads();
-                const uint32_t have = sm.n_list, need = sm.need;
-                for (uint32_t x = (uint32_t)tid; x < have; x += kPickThreads) {
-                    const uint64_t kx = sm.key[x];
-                    const uint32_t px = sm.page[x];
-                    uint32_t rank = 0;
-                    for (uint32_t y = 0; y < have; ++y) rank += sm.key[y] > kx || (sm.key[y] == kx && sm.page[y] < px);
-                    if (rank == need - 1) { sm.edge_key = kx; sm.edge_page = px; }
-                }
-                __syncthreads();
-                edge_key = sm.edge_key; edge_page = sm.edge_page;
-            }
-        }
-        if (!listed) {
-            // byte by byte: the key of the want-th page, then among the pages of that key the want-th of what is left
-            uint64_t prefix = 0;
-            uint32_t need = want;
-            for (int shift = 56; shift >= 0; shift -= 8) {
-                __syncthreads();
-                for (int i = tid; i < 256; i += kPickThreads) sm.hist[i] = 0;
-                __syncthreads();
-                const uint64_t mask = shift == 56 ? 0ull : ~0ull << (shift + 8);
-                for (int64_t i = i0; i < i1; ++i) {
-                    const uint64_t k = ord_of(score[i]);
-                    if ((k & mask) == prefix) atomicAdd(&sm.hist[(k >> shift) & 255], 1u);
-                }
-                __syncthreads();
-                const uint32_t c = tid < 256 ? sm.hist[255 - tid] : 0u;
-                uint32_t total;
-                const uint32_t above = team_prefix<Team>(c, total, sm, 0);
-                if (above < need && above + c >= need) { sm.prefix = prefix | ((uint64_t)(255 - tid) << shift); sm.need = need - above; }
-                __syncthreads();
-                prefix = sm.prefix; need = sm.need;
-            }
-            edge_key = prefix;
-            uint32_t same = 0;
-            for (int64_t i = i0; i < i1; ++i) same += ord_of(score[i]) == edge_key;
-            uint32_t total;
-            uint32_t before = team_prefix<Team>(same, total, sm, 1);
-            for (int64_t i = i0; i < i1; ++i)
-                if (ord_of(score[i]) == edge_key && ++before == need) sm.edge_page = (uint32_t)i;
-            __syncthreads();
-            edge_page = sm.edge_page;
-        }
-    }
-    auto picked = [&](int64_t i) {
-        const uint64_t k = ord_of(score[i]);
-        return k > edge_key || (k == edge_key && (uint32_t)i <= edge_page);
-    };
-    uint32_t mine = 0;
-    if (want > 0)
-        for (int64_t i = i0; i < i1; ++i) mine += picked(i);
-    __syncthreads();
-    uint32_t total;
-    uint32_t at = team_prefix<Team>(mine, total, sm, 0);
-    if (mine)
-        for (int64_t i = i0; i < i1; ++i)
-            if (picked(i)) list[at++] = (int32_t)i;
-    if (tid == 0) list[want] = (int32_t)n;
+    const uint32_t want = (uint32_t)a.n_blocks - 1;            // 0 <= want < P - 1: the newest page is in without a search
+    if (tid == 0) list[want] = (int32_t)(P - 1);
+    if (want == 0) return;
+    if (P - 1 <= kPickHeld * kPickThreads) pick_pages<true>(score, list, P - 1, want, sm);
+    else pick_pages<false>(score, list, P - 1, want, sm);
 }
 
 hipError_t launch_block_scores(const BlockCall& a, hipStream_t st) {

@@ -1,8 +1,9 @@
 // Attention of one query per sequence and head over all cached tokens, or over a list of 64-token pages (topk_attn_decode_dense and
 // the last step of topk_attn_decode_blocks): out = sum_i p_i V_i / sum_i p_i with p_i = exp(q . K_i / sqrt(d)), in one pass over K and V.
 //
-//   attend_kernel       splits of a sequence, a workgroup each: running maximum, sum of weights and weighted value sum, per wave
-//   attend_join_kernel  the splits of a head put together; the weights of the keys added to `mass`
+//   attend_kernel       splits of a sequence, a workgroup each: running maximum, sum of weights and weighted value sum, per wave; the
+//                       last workgroup of a key stream to finish puts the splits together
+//   attend_mass_kernel  with `mass`: the splits put together there, and the weights of the keys added up
 //
 // Bound by the read of K and V: 16 384 bytes per 32 keys and KV head against 2 x 32 MFMA (d = 128, 16 bit), a tenth of the time the read takes.
 #include "device_utils.h"
@@ -58,6 +59,101 @@ __device__ __forceinline__ float max_over_rows(float v) {      // largest of lan
 // fp16 has no numbers below 2^-24, so there the weights are relative to the maximum less 13 powers of two.
 template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
 
+// Splits of a sequence of N tokens.
+__device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t N) {
+    int64_t pages = (N + 63) / 64;
+    if (a.list && a.n_list < pages) pages = a.n_list;
+    return (int)((pages + a.chunk - 1) / a.chunk);
+}
+// What the splits leave is read by a workgroup of the same launch, maybe on another XCD: written and read past the caches that are not shared.
+__device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float2 get2(const float* p) {
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+// log2 of the sum of a head's weights (not shifted), over its splits; one wave.  `f` (or null) gets the factor of each split's weighted sum.
+__device__ __forceinline__ float head_log2_sum(const AttendCall& a, int64_t bh, int n_split, float shift, float* f) {
+    const float* lm = a.part_lm + bh * a.n_split * 2;
+    constexpr int U = kMaxSplits / kWave;
+    float2 v[U];
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = u * kWave + lane_id();
+        v[u] = make_float2(0.f, -INFINITY);
+        if (u * kWave < n_split && i < n_split) v[u] = get2(lm + 2 * i);
+        top = fmaxf(top, v[u].y);
+    }
+    top = wave_max(top);
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        v[u].y = v[u].y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v[u].y - top);     // (nothing but -inf: no part in the sum)
+        if (v[u].y != 0.f) sum = fmaf(v[u].y, v[u].x, sum);
+    }
+    sum = group_reduce<AddOp, 64>(sum);
+    const float inv = 1.0f / sum;
+    if (f) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u * kWave + lane_id() < n_split) f[u * kWave + lane_id()] = v[u].y * inv;
+    }
+    return (top - shift) + log2f(sum);
+}
+// out and lse of `heads` neighbouring heads (at most 16) from their splits; a workgroup of 256 threads, f: [heads][n_split] in LDS.
+__device__ __forceinline__ void join_splits(const AttendCall& a, int64_t head0, int heads, int n_split, float shift, float* f, float2* part) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    for (int h = wave; h < heads; h += 4) {
+        const float lg2 = head_log2_sum(a, head0 + h, n_split, shift, f + h * n_split);
+        if (lane_id() == 0 && a.lse) a.lse[head0 + h] = lg2 * 0.69314718055994531f;
+    }
+    __syncthreads();
+    // Pairs of channels; with few of them two or four threads share a pair's splits.  Four sums, by split modulo four, whoever takes them: the
+    // result does not depend on how many heads are joined at a time.
+    const int half = a.D / 2, pairs = heads * half;
+    const int shares = pairs <= 64 ? 4 : pairs <= 128 ? 2 : 1;
+    const int share = (int)threadIdx.x / pairs;
+    for (int i = shares > 1 ? (int)threadIdx.x % pairs : (int)threadIdx.x; i < pairs; i += 256) {
+        if (shares > 1 && share >= shares) break;
+        const int h = i / half, c = 2 * (i - h * half);
+        const float* p = a.part_acc + (head0 + h) * a.n_split * a.D + c;
+        const float* fh = f + h * n_split;
+        float2 sum[4] = {};
+        const int first = shares > 1 ? share : 0;
+        for (int x0 = 0; x0 < n_split; x0 += 8) {
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const bool mine = x0 + u < n_split && ((u & 3) & (shares - 1)) == first;
+                v[u] = make_float2(0.f, 0.f);
+                if (mine) v[u] = get2(p + (int64_t)(x0 + u) * a.D);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float w = x0 + u < n_split ? fh[x0 + u] : 0.f;
+                if (w != 0.f) { sum[u & 3].x = fmaf(w, v[u].x, sum[u & 3].x); sum[u & 3].y = fmaf(w, v[u].y, sum[u & 3].y); }
+            }
+        }
+        if (shares > 1) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if ((x & (shares - 1)) == first) part[x * pairs + i] = sum[x];
+        } else {
+            a.out[(head0 + h) * a.D + c] = (sum[0].x + sum[1].x) + (sum[2].x + sum[3].x);
+            a.out[(head0 + h) * a.D + c + 1] = (sum[0].y + sum[1].y) + (sum[2].y + sum[3].y);
+        }
+    }
+    if (shares > 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < pairs) {
+            const float2 *q = part + threadIdx.x;
+            const int64_t at = (head0 + (int)threadIdx.x / half) * a.D + 2 * ((int)threadIdx.x % half);
+            a.out[at] = (q[0].x + q[pairs].x) + (q[2 * pairs].x + q[3 * pairs].x);
+            a.out[at + 1] = (q[0].y + q[pairs].y) + (q[2 * pairs].y + q[3 * pairs].y);
+        }
+    }
+}
+
 // Waves per SIMD: two (256 registers) where the buffers leave room for it.
 template <int DT, int D> constexpr int kAttendWaves = AttendTile<DT, D>::ROW <= 512 ? 2 : 1;
 
@@ -66,8 +162,11 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
     using Tile = AttendTile<DT, D>;
     constexpr int SUB = Tile::SUB, STEP = Tile::STEP, KEYS = Tile::KEYS, KCH = Tile::KCH, T = Tile::T, ROW = Tile::ROW, EV = Tile::EV;
     constexpr int SPP = 64 / STEP;
-    __shared__ float red[4][16][D + 4];
+    constexpr int RED = 4 * 16 * (D + 4), JOIN = 16 * kMaxSplits + 1024;
+    __shared__ float lds[RED > JOIN || MASS ? RED : JOIN];
+    float (*const red)[16][D + 4] = reinterpret_cast<float (*)[16][D + 4]>(lds);
     __shared__ float red_m[4][16], red_l[4][16];
+    __shared__ uint32_t arrived;
     const int lane = lane_id(), j = lane >> 4, n = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     // The head blocks of one split follow each other eight workgroups apart: on the same XCD, whose L2 holds the keys for them.
@@ -269,6 +368,7 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
         }
     }
     __syncthreads();
+    const bool whole = MASS ? a.n_split == 1 : pages <= a.chunk;        // the sequence's only split (with `mass` the join does all or none)
     for (int i = (int)threadIdx.x; i < heads * D; i += 256) {
         const int h = i / D, c = i - h * D;
         float top = -INFINITY;
@@ -281,67 +381,41 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
             if (f != 0.f) { sum = fmaf(f, red[w][h][c], sum); total = fmaf(f, red_l[w][h], total); }
         }
         const int64_t bh = head0 + h;
-        if (a.n_split == 1) {
-            a.out[bh * D + c] = sum / total;
-            if (c == 0 && a.lse) a.lse[bh] = (top - WeightShift<DT>::value) * 0.69314718055994531f + logf(total);
+        if (whole) {
+            a.out[bh * D + c] = sum * (1.0f / total);              // (as join_splits() has it)
+            if (c == 0 && a.lse) a.lse[bh] = ((top - WeightShift<DT>::value) + log2f(total)) * 0.69314718055994531f;
         } else {
-            a.part_acc[(bh * a.n_split + split) * D + c] = sum;
+            put(&a.part_acc[(bh * a.n_split + split) * D + c], sum);
         }
-        if (c == 0) {
-            a.part_lm[(bh * a.n_split + split) * 2] = total;
-            a.part_lm[(bh * a.n_split + split) * 2 + 1] = top;
+        if (c == 0 && (MASS || !whole)) {
+            put(&a.part_lm[(bh * a.n_split + split) * 2], total);
+            put(&a.part_lm[(bh * a.n_split + split) * 2 + 1], top);
         }
     }
-}
-
-// Splits of sequence b.
-__device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t N) {
-    int64_t pages = (N + 63) / 64;
-    if (a.list && a.n_list < pages) pages = a.n_list;
-    return (int)((pages + a.chunk - 1) / a.chunk);
-}
-// log2 of the sum of a head's weights (not shifted), over its splits; one wave.  `top`: what its partial sums are relative to the largest of.
-__device__ __forceinline__ float head_log2_sum(const AttendCall& a, int64_t bh, int n_split, float shift, float* top_out) {
-    const float* lm = a.part_lm + bh * a.n_split * 2;
-    float top = -INFINITY;
-    for (int i = lane_id(); i < n_split; i += kWave) top = fmaxf(top, lm[2 * i + 1]);
-    top = wave_max(top);
-    float sum = 0.f;
-    for (int i = lane_id(); i < n_split; i += kWave) {
-        const float f = lm[2 * i + 1] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lm[2 * i + 1] - top);
-        if (f != 0.f) sum = fmaf(f, lm[2 * i], sum);
-    }
-    sum = group_reduce<AddOp, 64>(sum);
-    *top_out = top;
-    return (top - shift) + log2f(sum);
+    if (MASS || whole) return;
+    // the last split of the stream's head block to get here joins them (and leaves the counter at zero for the next call)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    uint32_t* const counter = a.arrive + (int64_t)stream * a.row_blocks + rb;
+    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const int ns = (int)((pages + a.chunk - 1) / a.chunk);
+    if (arrived + 1u != (uint32_t)ns) return;
+    if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    join_splits(a, head0, heads, ns, WeightShift<DT>::value, lds, reinterpret_cast<float2*>(lds + 16 * kMaxSplits));
 }
 
 constexpr int kMassPerBlock = 1024;      // keys whose weights one workgroup adds up
 
-// The first B * Hq workgroups put a head's splits together; the others (with `mass`) add each key's weights, the heads of the group in
-// order, from the scores that the walk left: 4 bytes per key and head written and read, where a second walk over the keys reads 2 d / G.
-__global__ void __launch_bounds__(256) attend_join_kernel(AttendCall a, float shift, int n_join) {
+// The first B * Hq workgroups put a head's splits together; the others add each key's weights, the heads of the group in order, from the
+// scores that the walk left: 4 bytes per key and head written and read, where a second walk over the keys reads 2 d / G.
+__global__ void __launch_bounds__(256) attend_mass_kernel(AttendCall a, float shift, int n_join) {
     __shared__ float lg[128];
+    __shared__ float f[kMaxSplits];
+    __shared__ float2 sums[512];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if ((int)blockIdx.x < n_join) {
-        __shared__ float f[1024];
-        const int64_t bh = blockIdx.x;
-        const int ns = attend_splits(a, a.len[bh / a.Hq]);
-        float top;
-        const float lg2 = head_log2_sum(a, bh, ns, shift, &top);      // (every wave: no exchange)
-        const float* lm = a.part_lm + bh * a.n_split * 2;
-        for (int i = (int)threadIdx.x; i < ns; i += 256)
-            f[i] = lm[2 * i + 1] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lm[2 * i + 1] - top - (lg2 - (top - shift)));
-        __syncthreads();
-        for (int c = (int)threadIdx.x; c < a.D; c += 256) {
-            const float* p = a.part_acc + bh * a.n_split * a.D + c;
-            float sum = 0.f;
-#pragma unroll 8
-            for (int i = 0; i < ns; ++i)
-                if (f[i] != 0.f) sum = fmaf(f[i], p[(int64_t)i * a.D], sum);
-            a.out[bh * a.D + c] = sum;
-        }
-        if (threadIdx.x == 0 && a.lse) a.lse[bh] = lg2 * 0.69314718055994531f;
+        join_splits(a, blockIdx.x, 1, attend_splits(a, a.len[blockIdx.x / a.Hq]), shift, f, sums);
         return;
     }
     const int per_stream = (int)((a.walk + kMassPerBlock - 1) / kMassPerBlock);
@@ -354,8 +428,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendCall a, float sh
     const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G;
     const int ns = attend_splits(a, N);
     for (int g = wave; g < a.G; g += 4) {
-        float top;
-        const float v = head_log2_sum(a, head0 + g, ns, shift, &top);
+        const float v = head_log2_sum(a, head0 + g, ns, shift, nullptr);
         if (lane_id() == 0) lg[g] = v;
     }
     __syncthreads();
@@ -397,11 +470,11 @@ hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
     TKA_BY_TYPE_AND_DIM(TKA_ATTEND, a.dtype, a.D);
 #undef TKA_ATTEND
     hipError_t e = hipGetLastError();
-    const int n_join = a.n_split > 1 ? a.B * a.Hq : 0;
-    const int64_t n_mass = a.mass ? (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock) : 0;
+    if (e != hipSuccess || !a.mass) return e;
+    const int64_t n_join = a.n_split > 1 ? (int64_t)a.B * a.Hq : 0;
+    const int64_t n_mass = (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock);
     if (n_join + n_mass > INT32_MAX) return hipErrorInvalidValue;
-    if (e != hipSuccess || n_join + n_mass == 0) return e;
-    hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, n_join);
+    hipLaunchKernelGGL(attend_mass_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, (int)n_join);
     return hipGetLastError();
 }
 

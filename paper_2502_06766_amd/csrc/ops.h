@@ -4,6 +4,8 @@
 
 namespace tka {
 
+constexpr int kMaxSplits = 256;  // splits of a sequence (their factors sit in LDS when they are joined)
+
 // Attention of one query per sequence and head over all cached tokens, or over a list of pages of 64 tokens.
 struct AttendCall {
     const char* K;              // this layer's keys and values [B][Hkv][Ncap][D]
@@ -15,6 +17,7 @@ struct AttendCall {
     int n_list;                 // pages of a list (a sequence of fewer pages: all of its own)
     float* part_acc;            // [B*Hq][n_split][D] weighted sums of the splits
     float* part_lm;             // [B*Hq][n_split][2] their sums of weights, and the score the weights are relative to (times log2(e) / sqrt(D))
+    uint32_t* arrive;           // [B][Hkv][row_blocks] splits that are done; zero between calls
     float* scores;              // [B*Hq][score_stride] raw scores in the order of the walk, kept for `mass`
     int64_t score_stride;
     float* out;                 // [B*Hq][D]

