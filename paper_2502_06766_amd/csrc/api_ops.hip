@@ -52,25 +52,56 @@ Layer layer_of(const topk_attn* h, int layer) {
 template <class T>
 T* scratch_at(const topk_attn* h, size_t offset) { return reinterpret_cast<T*>(static_cast<char*>(h->cfg.workspace) + offset); }
 
-// Pages that one workgroup of the walk takes, two workgroups to a compute unit in all: a workgroup's waves need a few steps each to keep
-// their loads in flight, and a part of a round at the end costs as much as a whole one.  At least two pages: a step per wave.
-int64_t pages_per_split(const topk_attn* h, int64_t total_pages, int64_t longest, int64_t max_splits) {
-    const int64_t wgs = 2 * (int64_t)h->n_cu;
-    int64_t chunk = std::max<int64_t>(2, (total_pages + wgs - 1) / wgs);
-    chunk = std::max(chunk, (longest + max_splits - 1) / max_splits);
+// Pages that one workgroup of the walk takes: the split with the least estimated time.  The estimate, in microseconds, for key streams of
+// pages[i] pages (each standing for `weight` streams), from measurements with 8 KV heads of d = 128 in 16 bits (32 KB a page):
+//   - a page takes a workgroup 0.5 on an empty chip and 1.42 with one on every compute unit (5.9 TB/s), between them as the root of their number;
+//   - more workgroups than compute units take whole rounds if all are alike, else their share of the work and a part of one at the end;
+//   - a workgroup costs 1 in itself, 1.7 where others follow it, putting splits together 3.2, and 0.05 a split.
+// One sequence of 500 / 1000 / 2000 / 16384 / 131072 tokens takes 8.3 / 8.8 / 9.6 / 17.8 / 93 us with 8 (one split), 2, 2, 8 and 64 pages a
+// workgroup; with 2, 16 (one split), 16, 4 and 32 pages 8.7 / 12.5 / 15.5 / 21.8 / 99.  24 sequences of 400 to 8192 tokens, 64 heads: 103 / 92 / 92
+// / 84 / 113 with 4 / 8 / 16 / 32 / 64 pages; 5 of 1600 to 32768: 80 / 75 / 73 / 76 / 107.
+int64_t pages_per_split(const int64_t* pages, int n, double weight, int64_t longest, int64_t max_splits, int n_cu, double row_bytes) {
+    double best = 1e30, all = 0.0;
+    int64_t chunk = longest;                                 // (max_splits >= 1)
+    const double scale = row_bytes / 256.0;
+    for (int i = 0; i < n; ++i) all += (double)pages[i];
+    all *= weight / n_cu;
+    const auto consider = [&](int64_t splits) {              // of the longest sequence
+        const int64_t c = std::max<int64_t>(2, (longest + splits - 1) / splits);
+        double wgs = 0.0;
+        const float inv = 1.0f / (float)c;
+        for (int i = 0; i < n; ++i) wgs += (double)(int64_t)((float)(pages[i] + c - 1) * inv);
+        wgs *= weight / n_cu;                                // to a compute unit
+        double cost = splits > 1 ? 3.2 + 0.05 * (double)splits : 0.0;
+        if (wgs <= 1.0) cost += 1.0 + scale * (double)c * std::max(0.5, 1.42 * sqrt(wgs));
+        else cost += 1.7 * wgs + scale * 1.42 * std::min(ceil(wgs) * (double)c, all + 0.25 * (double)c);
+        if (cost < best) { best = cost; chunk = c; }
+    };
+    // powers of two, one number between each two of them, and what fills whole rounds if all sequences are as long
+    for (int64_t k = 1; k <= max_splits && k <= longest; k *= 2) {
+        consider(k);
+        if (k >= 2 && k + k / 2 <= max_splits) consider(k + k / 2);
+    }
+    for (int r = 1; r <= 4; ++r) {
+        const int64_t k = (int64_t)(r * n_cu / (n * weight));
+        if (k >= 1 && k <= max_splits) consider(k);
+    }
     return chunk;
 }
+// Beyond this many bytes of a head block's partial sums the one workgroup that would put them together takes longer than a launch that has a
+// workgroup per head: 8 heads, 32 splits (128 KB) of 128k tokens 95 us joined in the walk's launch, 98 after it; 16 heads, 252 splits (2 MB) of
+// 64k tokens 45 and 18.
+constexpr int64_t kJoinBytes = 192 << 10;
 
 int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* out, int32_t* blocks, float* lse, float* mass,
                void* hip_stream) {
     const topk_attn_config& c = h->cfg;
     const Layer l = layer_of(h, layer);
-    int64_t longest = 0, total = 0;
+    int64_t longest = 0;
     for (int b = 0; b < c.n_seqs; ++b) {
         const int64_t n = h->len[(size_t)layer * c.n_seqs + b];
         if (n < 1) return TOPK_ATTN_EINVAL;
         longest = std::max(longest, n);
-        total += n_blocks ? std::min<int64_t>((n + 63) / 64, n_blocks) : (n + 63) / 64;
     }
     const DeviceOf device(h);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
@@ -105,8 +136,18 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     // partial sums in the candidate lists' place
     const size_t room = (size_t)h->ws.cand_cap * sizeof(uint64_t) / ((size_t)c.head_dim * sizeof(float) + 2 * sizeof(float));
     const int64_t max_splits = std::min<int64_t>(kMaxSplits, (int64_t)room);
-    a.chunk = (int)pages_per_split(h, total * a.Hkv * a.row_blocks, pages, max_splits);
+    int64_t sample[16];                          // (of a larger batch some sequences stand for all)
+    const int n_sample = std::min(c.n_seqs, 16);
+    for (int i = 0; i < n_sample; ++i) {
+        const int64_t n = h->len[(size_t)layer * c.n_seqs + (size_t)((int64_t)i * c.n_seqs / n_sample)];
+        sample[i] = std::min((n + 63) / 64, pages);
+    }
+    a.chunk = (int)pages_per_split(sample, n_sample, (double)c.n_seqs / n_sample * a.Hkv * a.row_blocks, pages, max_splits, h->n_cu,
+                                   (double)l.row);
     a.n_split = (int)((pages + a.chunk - 1) / a.chunk);
+    const bool many = (int64_t)a.n_split * std::min(a.G, 16) * a.D * 4 > kJoinBytes;
+    a.join_later = mass || many;
+    a.join_heads = many ? 1 : 16;
     a.part_acc = scratch_at<float>(h, h->ws.cand);
     a.part_lm = a.part_acc + (size_t)a.B * a.Hq * a.n_split * a.D;
     a.arrive = scratch_at<uint32_t>(h, h->ws.arrive);
@@ -170,10 +211,19 @@ int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int6
         add(l.index + index_codes_bytes(&c) + l.stream0 * c.max_tokens * sizeof(float), sizeof(float), false);
     }
     add(mass, sizeof(float), true);
-    const size_t streams = (size_t)c.n_seqs * c.n_kv_heads, words = 1 + streams * a.units + c.n_seqs;
+    a.longest = longest - recent;
+    a.chunk = std::max<int64_t>(kEvictHeldTokens, (a.longest + kEvictChunks - 1) / kEvictChunks);
+    // scratch in the candidate lists' place
+    const size_t streams = (size_t)c.n_seqs * c.n_kv_heads;
+    size_t words = 0;
+    const auto take = [&](size_t n) { uint32_t* p = scratch_at<uint32_t>(h, h->ws.cand) + words; words += (n + 3) / 4 * 4; return p; };
+    if (a.longest > kEvictHeldTokens) {
+        a.hist = take(streams * 2 * kEvictChunks * kEvictBins);
+        a.pick = take(streams * kEvictPick);
+    }
+    a.state = take(1 + streams * a.units);
+    a.old_len = reinterpret_cast<int32_t*>(take(c.n_seqs));
     if (words * 4 > (size_t)c.n_seqs * c.n_q_heads * h->ws.cand_cap * sizeof(uint64_t)) return TOPK_ATTN_ENOMEM;
-    a.state = scratch_at<uint32_t>(h, h->ws.cand);
-    a.old_len = reinterpret_cast<int32_t*>(a.state + 1 + streams * a.units);
     const DeviceOf device(h);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -241,9 +291,13 @@ int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_
     }
     a.Ncap = c.max_tokens; a.n = r->n_new; a.B = B; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.D = c.head_dim; a.dtype = c.dtype;
     a.rotary = r->rotary_dim; a.interleaved = r->interleaved != 0; a.eps = r->norm_eps;
-    // the kernel advances the length where one workgroup sees the whole sequence and no index kernel needs the old one
-    const bool paged = c.index_kind == TOPK_ATTN_INDEX_PAGES || c.index_kind == TOPK_ATTN_INDEX_BOXES;
-    a.bump = r->n_new == 1 && !paged;
+    // Sequences of one length: passed by value, so that no workgroup reads what another one advances.  (A launch that advances the lengths
+    // costs 5 us of a prompt's 56, a counter of the tokens done 50.)
+    a.base = h->len[slot];
+    for (int b = 1; b < B; ++b)
+        if (h->len[slot + b] != a.base) a.base = -1;
+    // the kernel advances the lengths unless an index kernel after it needs the old ones
+    a.advance = c.index_kind != TOPK_ATTN_INDEX_PAGES && c.index_kind != TOPK_ATTN_INDEX_BOXES && (a.base >= 0 || r->n_new == 1);
     if (launch_rotary(a, st) != hipSuccess) return TOPK_ATTN_EDEVICE;
     if (c.index_kind == TOPK_ATTN_INDEX_PAGES &&
         launch_page_balls(c.dtype, c.head_dim, a.K, c.max_tokens, pcap, c.n_kv_heads, B, a.len, 0, r->n_new, l.index + stream0 * pcap * l.row,
@@ -253,7 +307,7 @@ int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_
         launch_page_boxes(c.dtype, c.head_dim, a.K, c.max_tokens, pcap, c.n_kv_heads, B, a.len, 0, r->n_new,
                           l.index + stream0 * pcap * 2 * l.row, st) != hipSuccess)
         return TOPK_ATTN_EDEVICE;
-    if (!a.bump) hipLaunchKernelGGL(advance_len_kernel, dim3((unsigned)((B + 255) / 256)), dim3(256), 0, st, a.len, B, (int32_t)r->n_new);
+    if (!a.advance) hipLaunchKernelGGL(advance_len_kernel, dim3((unsigned)((B + 255) / 256)), dim3(256), 0, st, a.len, B, (int32_t)r->n_new);
     if (hipGetLastError() != hipSuccess) return TOPK_ATTN_EDEVICE;
     for (int b = 0; b < B; ++b) h->len[slot + b] += r->n_new;
     return TOPK_ATTN_OK;

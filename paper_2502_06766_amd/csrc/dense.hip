@@ -3,7 +3,7 @@
 //
 //   attend_kernel       splits of a sequence, a workgroup each: running maximum, sum of weights and weighted value sum, per wave; the
 //                       last workgroup of a key stream to finish puts the splits together
-//   attend_mass_kernel  with `mass`: the splits put together there, and the weights of the keys added up
+//   attend_later_kernel with `mass`: the splits put together there, and the weights of the keys added up; also for many splits of many heads
 //
 // Bound by the read of K and V: 16 384 bytes per 32 keys and KV head against 2 x 32 MFMA (d = 128, 16 bit), a tenth of the time the read takes.
 #include "device_utils.h"
@@ -100,72 +100,79 @@ __device__ __forceinline__ float head_log2_sum(const AttendCall& a, int64_t bh, 
     }
     return (top - shift) + log2f(sum);
 }
-// out and lse of `heads` neighbouring heads (at most 16) from their splits; a workgroup of 256 threads, f: [heads][n_split] in LDS.
-__device__ __forceinline__ void join_splits(const AttendCall& a, int64_t head0, int heads, int n_split, float shift, float* f, float2* part) {
+// Weighted sum of the splits of `quads` groups of four channels.  Four sums, by split modulo four, whichever thread takes them: the result does
+// not depend on how many heads are joined at a time.
+template <int NT, int SHARES>
+__device__ __forceinline__ void sum_splits(const AttendCall& a, int64_t head0, int quads, int n_split, const float* f, f32x4* part) {
+    constexpr int U = 16, SUMS = 4 / SHARES;                       // splits in flight (a trip to memory each otherwise); sums of a thread
+    const __amdgpu_buffer_rsrc_t rsrc =
+        __builtin_amdgcn_make_buffer_rsrc(a.part_acc + head0 * a.n_split * a.D, 0, 16 * a.n_split * a.D * 4, 0x00020000);
+    const int quarter = a.D / 4, first = SHARES > 1 ? (int)threadIdx.x / quads : 0;
+    for (int i = SHARES > 1 ? (int)threadIdx.x % quads : (int)threadIdx.x; i < quads && first < SHARES; i += NT) {
+        const int h = i / quarter, c = 4 * (i - h * quarter);
+        const float* const fh = f + h * n_split;
+        const uint32_t off = (uint32_t)(h * a.n_split * a.D + c) * 4;
+        f32x4 sum[SUMS] = {};
+        for (int x0 = first; x0 < n_split; x0 += U * SHARES) {
+            f32x4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {                          // (sc1: past the L2 of this XCD)
+                const int x = x0 + u * SHARES < n_split ? x0 + u * SHARES : x0;
+                v[u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(off + (uint32_t)(x * a.D) * 4), 0, 16));
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float w = x0 + u * SHARES < n_split ? fh[x0 + u * SHARES] : 0.f;
+                if (w != 0.f) {                                     // (a split of nothing but -inf may hold anything)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) sum[u % SUMS][y] = fmaf(w, v[u][y], sum[u % SUMS][y]);
+                }
+            }
+        }
+        if (SHARES > 1) {
+#pragma unroll
+            for (int y = 0; y < SUMS; ++y) part[(first + y * SHARES) * quads + i] = sum[y];
+        } else {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) a.out[(head0 + h) * a.D + c + y] = (sum[0][y] + sum[1 % SUMS][y]) + (sum[2 % SUMS][y] + sum[3 % SUMS][y]);
+        }
+    }
+    if (SHARES > 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < quads) {
+            const f32x4* q = part + threadIdx.x;
+            const f32x4 sum = (q[0] + q[quads]) + (q[2 * quads] + q[3 * quads]);
+            float* out = a.out + (head0 + (int)threadIdx.x / quarter) * a.D + 4 * ((int)threadIdx.x % quarter);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) out[y] = sum[y];
+        }
+    }
+}
+// out and lse of `heads` neighbouring heads (at most 16) from their splits; a workgroup of NT threads, f: [heads][n_split] in LDS.
+template <int NT>
+__device__ __forceinline__ void join_splits(const AttendCall& a, int64_t head0, int heads, int n_split, float shift, float* f, f32x4* part) {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    for (int h = wave; h < heads; h += 4) {
+    for (int h = wave; h < heads; h += NT / kWave) {
         const float lg2 = head_log2_sum(a, head0 + h, n_split, shift, f + h * n_split);
         if (lane_id() == 0 && a.lse) a.lse[head0 + h] = lg2 * 0.69314718055994531f;
     }
     __syncthreads();
-    // Pairs of channels; with few of them two or four threads share a pair's splits.  Four sums, by split modulo four, whoever takes them: the
-    // result does not depend on how many heads are joined at a time.
-    const int half = a.D / 2, pairs = heads * half;
-    const int shares = pairs <= 64 ? 4 : pairs <= 128 ? 2 : 1;
-    const int share = (int)threadIdx.x / pairs;
-    for (int i = shares > 1 ? (int)threadIdx.x % pairs : (int)threadIdx.x; i < pairs; i += 256) {
-        if (shares > 1 && share >= shares) break;
-        const int h = i / half, c = 2 * (i - h * half);
-        const float* p = a.part_acc + (head0 + h) * a.n_split * a.D + c;
-        const float* fh = f + h * n_split;
-        float2 sum[4] = {};
-        const int first = shares > 1 ? share : 0;
-        for (int x0 = 0; x0 < n_split; x0 += 8) {
-            float2 v[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const bool mine = x0 + u < n_split && ((u & 3) & (shares - 1)) == first;
-                v[u] = make_float2(0.f, 0.f);
-                if (mine) v[u] = get2(p + (int64_t)(x0 + u) * a.D);
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float w = x0 + u < n_split ? fh[x0 + u] : 0.f;
-                if (w != 0.f) { sum[u & 3].x = fmaf(w, v[u].x, sum[u & 3].x); sum[u & 3].y = fmaf(w, v[u].y, sum[u & 3].y); }
-            }
-        }
-        if (shares > 1) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if ((x & (shares - 1)) == first) part[x * pairs + i] = sum[x];
-        } else {
-            a.out[(head0 + h) * a.D + c] = (sum[0].x + sum[1].x) + (sum[2].x + sum[3].x);
-            a.out[(head0 + h) * a.D + c + 1] = (sum[0].y + sum[1].y) + (sum[2].y + sum[3].y);
-        }
-    }
-    if (shares > 1) {
-        __syncthreads();
-        if ((int)threadIdx.x < pairs) {
-            const float2 *q = part + threadIdx.x;
-            const int64_t at = (head0 + (int)threadIdx.x / half) * a.D + 2 * ((int)threadIdx.x % half);
-            a.out[at] = (q[0].x + q[pairs].x) + (q[2 * pairs].x + q[3 * pairs].x);
-            a.out[at + 1] = (q[0].y + q[pairs].y) + (q[2 * pairs].y + q[3 * pairs].y);
-        }
-    }
+    // Four channels a thread; with few of them two or four threads share a group's splits.
+    const int quads = heads * (a.D / 4);
+    if (quads <= NT / 4) sum_splits<NT, 4>(a, head0, quads, n_split, f, part);
+    else if (quads <= NT / 2) sum_splits<NT, 2>(a, head0, quads, n_split, f, part);
+    else sum_splits<NT, 1>(a, head0, quads, n_split, f, part);
 }
 
-// Waves per SIMD: two (256 registers) where the buffers leave room for it.
-template <int DT, int D> constexpr int kAttendWaves = AttendTile<DT, D>::ROW <= 512 ? 2 : 1;
-
 template <int DT, int D, bool LIST, bool MASS>
-__global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(AttendCall a) {
+__global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) attend_kernel(AttendCall a) {
     using Tile = AttendTile<DT, D>;
     constexpr int SUB = Tile::SUB, STEP = Tile::STEP, KEYS = Tile::KEYS, KCH = Tile::KCH, T = Tile::T, ROW = Tile::ROW, EV = Tile::EV;
     constexpr int SPP = 64 / STEP;
-    constexpr int RED = 4 * 16 * (D + 4), JOIN = 16 * kMaxSplits + 1024;
-    __shared__ float lds[RED > JOIN || MASS ? RED : JOIN];
+    constexpr int NW = 4, NT = NW * kWave, RED = NW * 16 * (D + 4), JOIN = 16 * kMaxSplits + 8 * NT;
+    __shared__ __align__(16) float lds[RED > JOIN ? RED : JOIN];
     float (*const red)[16][D + 4] = reinterpret_cast<float (*)[16][D + 4]>(lds);
-    __shared__ float red_m[4][16], red_l[4][16];
+    __shared__ float red_m[NW][16], red_l[NW][16];
     __shared__ uint32_t arrived;
     const int lane = lane_id(), j = lane >> 4, n = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -176,8 +183,14 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
         rb = in >> 3;
         unit = group * 8 + (in & 7);
     }
-    const int stream = unit / a.n_split, split = unit - stream * a.n_split;
-    if (stream >= a.B * a.Hkv) return;                        // (the last group of eight may be cut short)
+    // Splits of one rank follow each other, stream after stream, beginning a stream later with each rank.  (Workgroups go to the XCDs in turn:
+    // with the splits of a stream next to each other, eight or sixteen of them, each XCD had the same ranks of all sequences, and those of the
+    // last ranks, which short sequences do not have, stood idle: 24 sequences of 400 to 8192
+    // tokens in splits of 8 pages 124 us, now 92.)
+    const int streams = a.B * a.Hkv, split = unit / streams;
+    if (split >= a.n_split) return;                           // (the last group of eight may be cut short)
+    int stream = unit - split * streams - split % streams;
+    if (stream < 0) stream += streams;
     const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
     const int64_t N = a.len[b];
     const int64_t pages_b = (N + 63) / 64;
@@ -210,12 +223,12 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
         asm volatile("" : "+v"(k_off[g]), "+v"(v_off[g]));
     }
     uint32_t pages_ahead = 0;                                 // LIST: lane i holds the page of the wave's step i (of the next 64)
-    // First row of the wave's step i (steps wave, wave + 4, ... of the split), asked for in order.
+    // First row of the wave's step i (steps wave, wave + NW, ... of the split), asked for in order.
     auto row_of = [&](int i) -> int64_t {
-        const int s = wave + 4 * i;
+        const int s = wave + NW * i;
         if (!LIST) return p0 * 64 + (int64_t)s * STEP;
         if ((i & 63) == 0) {
-            const int at = wave + 4 * (i + lane);
+            const int at = wave + NW * (i + lane);
             pages_ahead = (uint32_t)list[at < n_steps ? at / SPP : 0];
         }
         const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages_ahead, i & 63);
@@ -230,7 +243,7 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
     };
     auto load = [&](Tile& t, int i, int& rows) {
         const int64_t row0 = row_of(i);
-        rows = rows_from(row0, wave + 4 * i < n_steps);
+        rows = rows_from(row0, wave + NW * i < n_steps);
         // what lies behind the rows there are reads as zero and is not fetched: no weight of zero meets a value of infinity
         const int64_t at = rows > 0 ? row0 * ROW : 0;
         const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(Kh + at), 0, rows * ROW, 0x00020000);
@@ -270,7 +283,7 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
         }
         if (MASS) {
             // kept in the order of the walk; a head's four scores of neighbouring keys in one store
-            float* to = a.scores + (head0 + n) * a.score_stride + p0 * 64 + (int64_t)(wave + 4 * i) * STEP + 4 * j;
+            float* to = a.scores + (head0 + n) * a.score_stride + p0 * 64 + (int64_t)(wave + NW * i) * STEP + 4 * j;
 #pragma unroll
             for (int g = 0; g < SUB; ++g) {
                 if (n < heads) {
@@ -334,7 +347,7 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
             }
         }
     };
-    const int mine = n_steps > wave ? (n_steps - wave + 3) / 4 : 0;
+    const int mine = n_steps > wave ? (n_steps - wave + NW - 1) / NW : 0;
     if constexpr (Tile::kPipelined) {
         Tile ta, tb;
         int ra = 0, rb_ = 0;
@@ -358,7 +371,7 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
         }
     }
     l = add_lanes_32(add_lanes_16(l));
-    // the four waves' sums, relative to the largest of their maxima
+    // the waves' sums, relative to the largest of their maxima
     if (j == 0) { red_m[wave][n] = m; red_l[wave][n] = l; }
     if (n < heads) {
 #pragma unroll
@@ -368,15 +381,15 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
         }
     }
     __syncthreads();
-    const bool whole = MASS ? a.n_split == 1 : pages <= a.chunk;        // the sequence's only split (with `mass` the join does all or none)
-    for (int i = (int)threadIdx.x; i < heads * D; i += 256) {
+    const bool whole = a.join_later ? a.n_split == 1 : pages <= a.chunk;        // the sequence's only split (a later join does all or none)
+    for (int i = (int)threadIdx.x; i < heads * D; i += NT) {
         const int h = i / D, c = i - h * D;
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, red_m[w][h]);
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, red_m[w][h]);
         float sum = 0.f, total = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float f = red_m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[w][h] - top);
             if (f != 0.f) { sum = fmaf(f, red[w][h][c], sum); total = fmaf(f, red_l[w][h], total); }
         }
@@ -392,7 +405,7 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
             put(&a.part_lm[(bh * a.n_split + split) * 2 + 1], top);
         }
     }
-    if (MASS || whole) return;
+    if (a.join_later || whole) return;
     // the last split of the stream's head block to get here joins them (and leaves the counter at zero for the next call)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -402,20 +415,22 @@ __global__ void __launch_bounds__(256, (kAttendWaves<DT, D>)) attend_kernel(Atte
     const int ns = (int)((pages + a.chunk - 1) / a.chunk);
     if (arrived + 1u != (uint32_t)ns) return;
     if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    join_splits(a, head0, heads, ns, WeightShift<DT>::value, lds, reinterpret_cast<float2*>(lds + 16 * kMaxSplits));
+    join_splits<NT>(a, head0, heads, ns, WeightShift<DT>::value, lds, reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits));
 }
 
 constexpr int kMassPerBlock = 1024;      // keys whose weights one workgroup adds up
 
-// The first B * Hq workgroups put a head's splits together; the others add each key's weights, the heads of the group in order, from the
+// The first workgroups put a head's, or a block of heads', splits together; the others add each key's weights, the heads of the group in order, from the
 // scores that the walk left: 4 bytes per key and head written and read, where a second walk over the keys reads 2 d / G.
-__global__ void __launch_bounds__(256) attend_mass_kernel(AttendCall a, float shift, int n_join) {
+__global__ void __launch_bounds__(256) attend_later_kernel(AttendCall a, float shift, int n_join) {
     __shared__ float lg[128];
-    __shared__ float f[kMaxSplits];
-    __shared__ float2 sums[512];
+    __shared__ float f[16 * kMaxSplits];
+    __shared__ f32x4 sums[512];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if ((int)blockIdx.x < n_join) {
-        join_splits(a, blockIdx.x, 1, attend_splits(a, a.len[blockIdx.x / a.Hq]), shift, f, sums);
+        const int blocks = a.join_heads == 1 ? a.G : a.row_blocks, group = (int)blockIdx.x / blocks, in = (int)blockIdx.x - group * blocks;
+        const int left = a.G - in * a.join_heads, heads = left < a.join_heads ? left : a.join_heads;
+        join_splits<256>(a, (int64_t)group * a.G + in * a.join_heads, heads, attend_splits(a, a.len[group / a.Hkv]), shift, f, sums);
         return;
     }
     const int per_stream = (int)((a.walk + kMassPerBlock - 1) / kMassPerBlock);
@@ -434,47 +449,52 @@ __global__ void __launch_bounds__(256) attend_mass_kernel(AttendCall a, float sh
     __syncthreads();
     const float* const s0 = a.scores + head0 * a.score_stride;
     float* const mass = a.mass + (int64_t)stream * a.Ncap;
-    constexpr int U = kMassPerBlock / 256;
-    int64_t at[U], pos[U];
-    float w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        at[u] = i0 + u * 256 + (int)threadIdx.x;
-        pos[u] = at[u];
-        if (at[u] >= pages * 64) pos[u] = N;
-        else if (a.list) pos[u] = (int64_t)a.list[(int64_t)stream * a.list_stride + at[u] / 64] * 64 + at[u] % 64;
-        if (pos[u] >= N) at[u] = i0;                              // (nothing to add: any score)
-        w[u] = 0.f;
-    }
-#pragma unroll 4
+    // four neighbouring keys a thread (of one page)
+    const int64_t at = i0 + 4 * (int)threadIdx.x;
+    if (at >= pages * 64) return;
+    const int64_t pos = a.list ? (int64_t)a.list[(int64_t)stream * a.list_stride + at / 64] * 64 + at % 64 : at;
+    const int left = N - pos < 4 ? (int)(N - pos) : 4;
+    if (left <= 0) return;
+    float w[4] = {0.f, 0.f, 0.f, 0.f}, old[4];
+    if (left == 4) __builtin_memcpy(old, mass + pos, 16);
+#pragma unroll 8
     for (int g = 0; g < a.G; ++g) {
+        float s[4];
+        // (a row's room ends with the cache, which may be within the last four)
+        if (left == 4) __builtin_memcpy(s, s0 + g * a.score_stride + at, 16);
+        else for (int u = 0; u < 4; ++u) s[u] = u < left ? s0[g * a.score_stride + at + u] : 0.f;
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] += __builtin_amdgcn_exp2f(fmaf(s0[g * a.score_stride + at[u]], a.scale_log2e, -lg[g]));
+        for (int u = 0; u < 4; ++u) w[u] += __builtin_amdgcn_exp2f(fmaf(s[u], a.scale_log2e, -lg[g]));
     }
+    if (left == 4) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (pos[u] < N) mass[pos[u]] += w[u];
+        for (int u = 0; u < 4; ++u) old[u] += w[u];
+        __builtin_memcpy(mass + pos, old, 16);
+    } else {
+        for (int u = 0; u < left; ++u) mass[pos + u] += w[u];
+    }
 }
 
 hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
     const int64_t units = (int64_t)a.B * a.Hkv * a.n_split;
     const int64_t blocks = a.row_blocks > 1 ? (units + 7) / 8 * 8 * a.row_blocks : units;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-#define TKA_ATTEND(DT_, D_)                                                                                                               \
-    do {                                                                                                                                  \
-        if (a.list && a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);       \
-        else if (a.list) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, false>), dim3((unsigned)blocks), dim3(256), 0, st, a);           \
-        else if (a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, false, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);           \
-        else hipLaunchKernelGGL((attend_kernel<DT_, D_, false, false>), dim3((unsigned)blocks), dim3(256), 0, st, a);                      \
+#define TKA_ATTEND(DT_, D_)                                                                                             \
+    do {                                                                                                                \
+        const dim3 grid((unsigned)blocks), wg(256);                                                                     \
+        if (a.list && a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, true>), grid, wg, 0, st, a);             \
+        else if (a.list) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, false>), grid, wg, 0, st, a);                 \
+        else if (a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, false, true>), grid, wg, 0, st, a);                 \
+        else hipLaunchKernelGGL((attend_kernel<DT_, D_, false, false>), grid, wg, 0, st, a);                            \
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_ATTEND, a.dtype, a.D);
 #undef TKA_ATTEND
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !a.mass) return e;
-    const int64_t n_join = a.n_split > 1 ? (int64_t)a.B * a.Hq : 0;
-    const int64_t n_mass = (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock);
+    const int64_t n_join = a.join_later && a.n_split > 1 ? (int64_t)a.B * a.Hkv * (a.join_heads == 1 ? a.G : a.row_blocks) : 0;
+    const int64_t n_mass = !a.mass ? 0 : (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock);
     if (n_join + n_mass > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(attend_mass_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, (int)n_join);
+    if (e != hipSuccess || n_join + n_mass == 0) return e;
+    hipLaunchKernelGGL(attend_later_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, (int)n_join);
     return hipGetLastError();
 }
 

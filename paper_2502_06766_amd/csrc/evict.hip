@@ -1,7 +1,8 @@
 // Accumulated attention weight of the cached tokens: eviction by it (topk_attn_evict), and its accumulation from a top-k selection
 // (topk_attn_add_mass; dense.hip adds it up in the dense and block-sparse decodes).
 //
-//   evict_select_kernel  survivors of each key stream, ascending: the newest tokens and the heaviest of the older ones
+//   evict_select_kernel, evict_step_kernel
+//                        survivors of each key stream, ascending: the newest tokens and the heaviest of the older ones
 //   evict_move_kernel    their rows to the front of the cache, in place: keys, values, accumulators, int8 codes and scales
 //   add_mass_kernel      mass[position] += exp(score / sqrt(d) - lse)
 #include "device_utils.h"
@@ -15,114 +16,237 @@ namespace tka {
 __device__ __forceinline__ uint32_t mass_key(float v) { return v == v ? ord_from_bits(__float_as_uint(v + 0.0f)) : 0u; }
 constexpr uint32_t kZeroMass = 0x80000000u;      // of zero: tokens no query has attended to, often most of a cache
 
-// One workgroup per key stream: the weight of the last survivor by 11, 11 and 10 bits of its key from the top, then the survivors in
-// order, a stretch of the cache per wave.  Reads the weights five times, from L2 but for the first (4 bytes a token; a moved token is
-// 4 d e of them): one compute unit's share of L2, 64 bytes a clock, is what bounds it.
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave, kEvictBins = 2048;
-__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictCall a) {
-    using Team = WorkgroupTeam<kEvictThreads>;
-    struct SM {
-        uint32_t tot[2][16];
-        uint32_t hist[kEvictBins];
-        uint32_t prefix, need;
-        uint32_t above[kEvictWaves], equal[kEvictWaves];
-    };
-    __shared__ SM sm;
-    const int tid = (int)threadIdx.x, lane = lane_id();
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int64_t stream = blockIdx.x;
-    const int b = (int)(stream / a.Hkv);
-    const int64_t N = a.len[b];
-    int32_t* const kept = a.kept + stream * a.budget;
-    for (int i = tid; i < a.units; i += kEvictThreads) a.state[1 + stream * a.units + i] = 0u;
-    if (tid == 0) {
-        if (stream == 0) a.state[0] = 0u;
-        if (stream == (int64_t)b * a.Hkv) a.old_len[b] = (int32_t)N;
-    }
-    if (N <= a.budget) {                                       // all stay
-        for (int64_t i = tid; i < a.budget; i += kEvictThreads) kept[i] = i < N ? (int32_t)i : -1;
-        return;
-    }
-    const float* const mass = a.mass + stream * a.Ncap;
-    const int64_t n = N - a.recent;                            // older tokens
-    const uint32_t want = (uint32_t)(a.budget - a.recent);     // of them survive; want < n
-    for (int64_t i = tid; i < a.recent; i += kEvictThreads) kept[want + i] = (int32_t)(n + i);
-    if (want == 0) return;
-    uint32_t prefix = 0, need = want;
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        const uint32_t mask = pass == 0 ? 0u : ~0u << (shift + bits);
-        for (int i = tid; i < kEvictBins; i += kEvictThreads) sm.hist[i] = 0;
-        __syncthreads();
-        uint32_t zeros = 0;                                    // (counted apart: thousands of additions to one counter otherwise)
-        auto count = [&](uint32_t k) {
-            if (k == kZeroMass) ++zeros;
-            else if ((k & mask) == prefix) atomicAdd(&sm.hist[(k >> shift) & ((1u << bits) - 1)], 1u);
-        };
-        int64_t i = tid;
-        for (; i + 7 * kEvictThreads < n; i += 8 * kEvictThreads) {
-            float v[8];
+// The weight of the last survivor is found from the top of the keys' bits: 11 of them by a histogram in LDS, then 11 and 10 more among the keys
+// that share the ones before (or, where at most 512 keys do after the first, those compared with each other); then the survivors are written
+// in order, a stretch of the cache per wave.  One workgroup has up to 16384 tokens of a key stream in its registers and does it all
+// (8065 tokens 16 us).  Longer streams are cut into up to eight chunks and take a launch per step, each workgroup adding up the chunks'
+// histograms of the step before for itself (32 streams of 5k to 100k tokens: 84 us in one
+// workgroup each, 45 in four launches); chunks of more than 16384 tokens are read again by each step.
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave, kEvictList = 512, kEvictHeld = 16;
+struct EvictShared {
+    uint32_t tot[2][16];
+    uint32_t hist[kEvictBins];
+    uint32_t list[kEvictList];
+    uint32_t n_list, prefix, need;
+    uint32_t above[kEvictWaves], equal[kEvictWaves];
+};
+using EvictTeam = WorkgroupTeam<kEvictThreads>;
+// position of step `pass` among a key's bits
+__device__ __forceinline__ constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
+
+// The keys of tokens [c0, c1), c1 > c0: each wave has a stretch of `steps` times 64 neighbouring ones.
+template <bool HELD> struct KeyWalk {
+    const float* mass;
+    int64_t c1, s0, steps;
+    uint32_t held[HELD ? kEvictHeld : 1];
+    __device__ __forceinline__ KeyWalk(const float* m, int64_t c0, int64_t c1_) : mass(m), c1(c1_) {
+        steps = (c1 - c0 + kEvictThreads - 1) / kEvictThreads;
+        s0 = c0 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * steps * kWave + lane_id();
+        if (HELD) {
+            float v[HELD ? kEvictHeld : 1];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = mass[i + u * kEvictThreads];
+            for (int u = 0; u < (HELD ? kEvictHeld : 1); ++u) v[u] = u < steps ? mass[s0 + u * kWave < c1 ? s0 + u * kWave : c1 - 1] : 0.f;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) count(mass_key(v[u]));
-        }
-        for (; i < n; i += kEvictThreads) count(mass_key(mass[i]));
-        if (zeros && (kZeroMass & mask) == prefix) atomicAdd(&sm.hist[(kZeroMass >> shift) & ((1u << bits) - 1)], zeros);
-        __syncthreads();
-        // thread t looks at the two bins from 2047 - 2 t down
-        const uint32_t c1 = sm.hist[kEvictBins - 1 - 2 * tid], c0 = sm.hist[kEvictBins - 2 - 2 * tid];
-        uint32_t total;
-        const uint32_t above = team_prefix<Team>(c1 + c0, total, sm, pass & 1);
-        if (above < need && above + c1 + c0 >= need) {
-            const bool upper = above + c1 >= need;
-            sm.prefix = prefix | ((uint32_t)(kEvictBins - 1 - 2 * tid - (upper ? 0 : 1)) << shift);
-            sm.need = need - above - (upper ? 0 : c1);
-        }
-        __syncthreads();
-        prefix = sm.prefix; need = sm.need;
-    }
-    // survivors: a key above `prefix`, or the first `need` equal to it
-    const int64_t stretch = ((n + kEvictWaves - 1) / kEvictWaves + kWave - 1) / kWave * kWave;
-    const int64_t s0 = wave * stretch < n ? wave * stretch : n, s1 = s0 + stretch < n ? s0 + stretch : n;
-    uint32_t above = 0, equal = 0;
-    constexpr int U = 8;
-    for (int64_t i = s0; i < s1; i += U * kWave) {
-        float v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = mass[i + u * kWave + lane < s1 ? i + u * kWave + lane : s1 - 1];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool in = i + u * kWave + lane < s1;
-            const uint32_t k = mass_key(v[u]);
-            above += (uint32_t)__popcll(__ballot(in && k > prefix));
-            equal += (uint32_t)__popcll(__ballot(in && k == prefix));
+            for (int u = 0; u < (HELD ? kEvictHeld : 1); ++u) held[u] = mass_key(v[u]);
         }
     }
-    if (lane == 0) { sm.above[wave] = above; sm.equal[wave] = equal; }
+    // f(position, key, there is such a token) for 64 neighbouring tokens at a time, in order
+    template <class F> __device__ __forceinline__ void each(F f) const {
+        if (HELD) {
+#pragma unroll
+            for (int u = 0; u < (HELD ? kEvictHeld : 1); ++u)
+                if (u < steps) f(s0 + u * kWave, held[u], s0 + u * kWave < c1);
+        } else {
+            constexpr int U = 16;
+            for (int64_t u0 = 0; u0 < steps; u0 += U) {
+                const int64_t i = s0 + u0 * kWave;
+                float v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = mass[i + u * kWave < c1 ? i + u * kWave : c1 - 1];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u0 + u < steps) f(i + u * kWave, mass_key(v[u]), i + u * kWave < c1);
+            }
+        }
+    }
+};
+// Histogram of step `pass` of the keys whose higher bits are those of `prefix`, in sm.hist (the caller waits).
+template <class Walk>
+__device__ __forceinline__ void digit_histogram(const Walk& keys, int pass, uint32_t prefix, EvictShared& sm) {
+    const int shift = digit_shift(pass), bits = digit_bits(pass);
+    const uint32_t mask = pass == 0 ? 0u : ~0u << (shift + bits);
+    for (int i = (int)threadIdx.x; i < kEvictBins; i += kEvictThreads) sm.hist[i] = 0;
     __syncthreads();
-    uint32_t at = 0, equal_before = 0;
+    uint32_t zeros = 0;                                        // (counted apart: thousands of additions to one counter otherwise)
+    keys.each([&](int64_t, uint32_t k, bool there) {
+        if (!there) return;
+        if (k == kZeroMass) ++zeros;
+        else if ((k & mask) == prefix) atomicAdd(&sm.hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+    });
+    if (zeros && (kZeroMass & mask) == prefix) atomicAdd(&sm.hist[(kZeroMass >> shift) & ((1u << bits) - 1)], zeros);
+}
+// Thread t brings the counts of bins 2047 - 2 t and 2046 - 2 t.  `prefix` grows by the bin that the need-th key from above lies in, `need` becomes
+// its rank there.  (The caller waits before sm.prefix and sm.need are used again.)
+__device__ __forceinline__ void digit_pick(uint32_t c1, uint32_t c0, int pass, uint32_t& prefix, uint32_t& need, EvictShared& sm) {
+    const int tid = (int)threadIdx.x;
+    uint32_t total;
+    const uint32_t above = team_prefix<EvictTeam>(c1 + c0, total, sm, pass & 1);
+    if (above < need && above + c1 + c0 >= need) {
+        const bool upper = above + c1 >= need;
+        sm.prefix = prefix | ((uint32_t)(kEvictBins - 1 - 2 * tid - (upper ? 0 : 1)) << digit_shift(pass));
+        sm.need = need - above - (upper ? 0 : c1);
+    }
+    __syncthreads();
+    prefix = sm.prefix; need = sm.need;
+}
+// Survivors among the walk's tokens: a key above `edge`, or one of the first `need` equal to it, counting `equal_before` of them before; the first
+// one goes to kept[at].
+template <class Walk>
+__device__ __forceinline__ void write_survivors(const Walk& keys, uint32_t edge, uint32_t need, uint32_t at, uint32_t equal_before, int32_t* kept,
+                                                EvictShared& sm) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    uint32_t above = 0, equal = 0;
+    keys.each([&](int64_t, uint32_t k, bool there) {
+        above += (uint32_t)__popcll(__ballot(there && k > edge));
+        equal += (uint32_t)__popcll(__ballot(there && k == edge));
+    });
+    if (lane_id() == 0) { sm.above[wave] = above; sm.equal[wave] = equal; }
+    __syncthreads();
     for (int w = 0; w < wave; ++w) {
         const uint32_t left = equal_before < need ? need - equal_before : 0u;
         at += sm.above[w] + (sm.equal[w] < left ? sm.equal[w] : left);
         equal_before += sm.equal[w];
     }
-    for (int64_t i = s0; i < s1; i += U * kWave) {
-        float v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = mass[i + u * kWave + lane < s1 ? i + u * kWave + lane : s1 - 1];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool in = i + u * kWave + lane < s1;
-            const uint32_t k = mass_key(v[u]);
-            const uint64_t eq = __ballot(in && k == prefix);
-            const bool keep = in && (k > prefix || (k == prefix && equal_before + (uint32_t)mask_rank(eq) < need));
-            const uint64_t m = __ballot(keep);
-            if (keep) kept[at + (uint32_t)mask_rank(m)] = (int32_t)(i + u * kWave + lane);
-            at += (uint32_t)__popcll(m);
-            equal_before += (uint32_t)__popcll(eq);
+    keys.each([&](int64_t i, uint32_t k, bool there) {
+        const uint64_t eq = __ballot(there && k == edge);
+        const bool keep = there && (k > edge || (k == edge && equal_before + (uint32_t)mask_rank(eq) < need));
+        const uint64_t m = __ballot(keep);
+        if (keep) kept[at + (uint32_t)mask_rank(m)] = (int32_t)i;
+        at += (uint32_t)__popcll(m);
+        equal_before += (uint32_t)__popcll(eq);
+    });
+}
+
+// What there is to select of a stream: `want` of the first n tokens (0: nothing).  With `first` also what needs no selection: the newest tokens,
+// or all, and the scratch of the move.
+__device__ __forceinline__ uint32_t evict_task(const EvictCall& a, int64_t stream, bool first, int64_t& n) {
+    const int tid = (int)threadIdx.x, b = (int)(stream / a.Hkv);
+    const int64_t N = a.len[b];
+    int32_t* const kept = a.kept + stream * a.budget;
+    if (first) {
+        for (int i = tid; i < a.units; i += kEvictThreads) a.state[1 + stream * a.units + i] = 0u;
+        if (tid == 0) {
+            if (stream == 0) a.state[0] = 0u;
+            if (stream == (int64_t)b * a.Hkv) a.old_len[b] = (int32_t)N;
         }
     }
+    if (N <= a.budget) {                                       // all stay
+        if (first)
+            for (int64_t i = tid; i < a.budget; i += kEvictThreads) kept[i] = i < N ? (int32_t)i : -1;
+        return 0;
+    }
+    n = N - a.recent;                                          // older tokens
+    const uint32_t want = (uint32_t)(a.budget - a.recent);     // of them survive; want < n
+    if (first)
+        for (int64_t i = tid; i < a.recent; i += kEvictThreads) kept[want + i] = (int32_t)(n + i);
+    return want;
+}
+
+__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictCall a) {
+    __shared__ EvictShared sm;
+    const int64_t stream = blockIdx.x;
+    const int tid = (int)threadIdx.x;
+    int64_t n = 0;
+    uint32_t need = evict_task(a, stream, true, n), prefix = 0;
+    if (need == 0) return;
+    const KeyWalk<true> keys(a.mass + stream * a.Ncap, 0, n);
+    for (int pass = 0; pass < 3; ++pass) {
+        digit_histogram(keys, pass, prefix, sm);
+        if (tid == 0) sm.n_list = 0;
+        __syncthreads();
+        digit_pick(sm.hist[kEvictBins - 1 - 2 * tid], sm.hist[kEvictBins - 2 - 2 * tid], pass, prefix, need, sm);
+        const uint32_t have = sm.hist[prefix >> digit_shift(0)];
+        if (pass == 0 && have <= kEvictList) {
+            keys.each([&](int64_t, uint32_t k, bool there) {
+                if (there && (k >> digit_shift(0)) == (prefix >> digit_shift(0))) sm.list[atomicAdd(&sm.n_list, 1u)] = k;
+            });
+            __syncthreads();
+            if (tid < (int)have) {
+                const uint32_t k = sm.list[tid];
+                uint32_t more = 0, same = 0;
+                for (uint32_t y = 0; y < have; ++y) { more += sm.list[y] > k; same += sm.list[y] == k; }
+                if (more < need && more + same >= need) { sm.prefix = k; sm.need = need - more; }      // (all that are equal say the same)
+            }
+            __syncthreads();
+            prefix = sm.prefix; need = sm.need;
+            break;
+        }
+        __syncthreads();
+    }
+    write_survivors(keys, prefix, need, 0, 0, a.kept + stream * a.budget, sm);
+}
+
+// The same in steps, a launch each; grid (chunks, streams).  pick: per stream the prefix and rank after the steps so far, and per chunk the keys
+// above the second step's prefix.  The histograms of a step lie in one of two places, those of the step before in the other.
+template <int PASS, bool HELD>
+__global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) {
+    __shared__ EvictShared sm;
+    const int64_t stream = blockIdx.y;
+    const int tid = (int)threadIdx.x, chunk = (int)blockIdx.x, lane = lane_id();
+    int64_t n = 0;
+    uint32_t need = evict_task(a, stream, PASS == 0 && chunk == 0, n), prefix = 0;
+    const int64_t c0 = chunk * a.chunk;
+    if (need == 0 || c0 >= n) return;
+    const int n_chunks = (int)((n + a.chunk - 1) / a.chunk);
+    const KeyWalk<HELD> keys(a.mass + stream * a.Ncap, c0, c0 + a.chunk < n ? c0 + a.chunk : n);
+    uint32_t* const pick = a.pick + stream * kEvictPick;
+    if (PASS > 0) {
+        if (PASS > 1) { prefix = pick[2 * (PASS - 2)]; need = pick[2 * (PASS - 2) + 1]; }
+        const uint32_t* before = a.hist + (stream * 2 + ((PASS - 1) & 1)) * kEvictChunks * kEvictBins;
+        uint32_t c1 = 0, c0_ = 0;
+        for (int x = 0; x < n_chunks; ++x) {
+            const uint2 v = *reinterpret_cast<const uint2*>(before + x * kEvictBins + kEvictBins - 2 - 2 * tid);
+            c0_ += v.x; c1 += v.y;
+        }
+        digit_pick(c1, c0_, PASS - 1, prefix, need, sm);
+        if (chunk == 0 && tid == 0) { pick[2 * (PASS - 1)] = prefix; pick[2 * (PASS - 1) + 1] = need; }
+    }
+    if (PASS < 3) {
+        digit_histogram(keys, PASS, prefix, sm);
+        if (PASS == 2) {
+            uint32_t above = 0;
+            keys.each([&](int64_t, uint32_t k, bool there) { above += (uint32_t)__popcll(__ballot(there && (k >> digit_shift(1)) > (prefix >> digit_shift(1)))); });
+            if (lane == 0) sm.above[tid >> 6] = above;
+        }
+        __syncthreads();
+        uint32_t* mine = a.hist + ((stream * 2 + (PASS & 1)) * kEvictChunks + chunk) * kEvictBins;
+        for (int i = tid; i < kEvictBins; i += kEvictThreads) mine[i] = sm.hist[i];
+        if (PASS == 2 && tid == 0) {
+            uint32_t above = 0;
+            for (int w = 0; w < kEvictWaves; ++w) above += sm.above[w];
+            pick[6 + chunk] = above;
+        }
+        return;
+    }
+    // survivors in the chunks before: above the second step's prefix, above it in the third digit, equal to it
+    const uint32_t* last = a.hist + (stream * 2) * kEvictChunks * kEvictBins;
+    const uint32_t digit = prefix & ((1u << digit_bits(2)) - 1);
+    const int wave = tid >> 6;
+    if (wave < chunk) {
+        uint32_t more = 0;
+        for (uint32_t i = digit + 1 + (uint32_t)lane; i < (1u << digit_bits(2)); i += kWave) more += last[wave * kEvictBins + i];
+        more = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(more), kWave - 1);
+        if (lane == 0) { sm.list[2 * wave] = pick[6 + wave] + more; sm.list[2 * wave + 1] = last[wave * kEvictBins + digit]; }
+    }
+    __syncthreads();
+    uint32_t at = 0, equal_before = 0;
+    for (int x = 0; x < chunk; ++x) {
+        const uint32_t left = equal_before < need ? need - equal_before : 0u, same = sm.list[2 * x + 1];
+        at += sm.list[2 * x] + (same < left ? same : left);
+        equal_before += same;
+    }
+    write_survivors(keys, prefix, need, at, equal_before, a.kept + stream * a.budget, sm);
 }
 
 // Row j of the cache becomes row kept[j] >= j, for all j of a stream, in place.  A workgroup holds a unit of neighbouring rows j in
@@ -228,7 +352,19 @@ __global__ void __launch_bounds__(kMassThreads) add_mass_kernel(MassCall a) {
 hipError_t launch_evict(const EvictCall& a, hipStream_t st) {
     const int64_t streams = (int64_t)a.B * a.Hkv;
     if (streams * a.units > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)streams), dim3(kEvictThreads), 0, st, a);
+    if (a.longest <= kEvictHeldTokens) {
+        hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)streams), dim3(kEvictThreads), 0, st, a);
+    } else {
+        if (streams > 65535) return hipErrorInvalidValue;
+        const dim3 grid((unsigned)((a.longest + a.chunk - 1) / a.chunk), (unsigned)streams);
+#define TKA_STEP(PASS_)                                                                                                            \
+    do {                                                                                                                          \
+        if (a.chunk <= kEvictHeldTokens) hipLaunchKernelGGL((evict_step_kernel<PASS_, true>), grid, dim3(kEvictThreads), 0, st, a); \
+        else hipLaunchKernelGGL((evict_step_kernel<PASS_, false>), grid, dim3(kEvictThreads), 0, st, a);                            \
+    } while (0)
+        TKA_STEP(0); TKA_STEP(1); TKA_STEP(2); TKA_STEP(3);
+#undef TKA_STEP
+    }
     hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(streams * a.units)), dim3(256), 0, st, a);
     return hipGetLastError();
 }

@@ -27,6 +27,8 @@ struct AttendCall {
     int64_t walk;               // most keys a sequence's walk covers, whole pages
     int B, Hq, Hkv, G, D, dtype;
     int chunk;                  // pages per split
+    int join_later;             // the splits are put together in a launch of its own,
+    int join_heads;             // by a workgroup per head (1) or per block of heads (16)
     int n_split;                // splits of the longest sequence
     int row_blocks;             // blocks of 16 heads of a group
     float scale_log2e;          // log2(e) / sqrt(D)
@@ -65,8 +67,9 @@ struct RotaryCall {
     int8_t* codes;              // int8 index of the first sequence [B][Hkv][Ncap][D], or null
     float* scales;
     int64_t Ncap, n;
+    int64_t base;               // length of all sequences before the call, or -1: as the device has it
+    int advance;                // the kernel advances the lengths itself (for base >= 0, or n = 1)
     int B, Hq, Hkv, D, dtype, rotary, interleaved;
-    int bump;                   // the kernel advances the lengths itself (a workgroup per sequence)
     float eps;
 };
 hipError_t launch_rotary(const RotaryCall& a, hipStream_t st);
@@ -80,6 +83,9 @@ struct EvictArray {
     int cleared;                // rows behind the survivors are cleared
 };
 constexpr int kEvictArrays = 5; // keys, values, mass, codes, scales
+constexpr int kEvictBins = 2048, kEvictChunks = 8;     // bins of a step of the selection, chunks of a key stream
+constexpr int64_t kEvictHeldTokens = 16384;            // tokens one workgroup holds
+constexpr int kEvictPick = 16;
 struct EvictCall {
     EvictArray array[kEvictArrays];
     int n_arrays, units;        // units per key stream over all arrays
@@ -88,7 +94,11 @@ struct EvictCall {
     int32_t* kept;              // [B][Hkv][budget], or scratch of the same shape
     uint32_t* state;            // scratch: one word for the next unit, then a flag per unit and key stream
     int32_t* old_len;           // scratch [B]
+    uint32_t* hist;             // scratch [B * Hkv][2][kEvictChunks][kEvictBins], for streams of more than kEvictHeldTokens
+    uint32_t* pick;             // scratch [B * Hkv][kEvictPick]
     int64_t Ncap, budget, recent;
+    int64_t longest;            // older tokens of the longest sequence
+    int64_t chunk;              // tokens of a chunk
     int B, Hkv;
 };
 constexpr int kEvictPieces = 16;                       // 16-byte pieces a thread of a unit holds

@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryCall a) {
     const int b = (int)(blockIdx.x / a.n);
     const int c = (int)threadIdx.x % LPR, slot = (int)threadIdx.x / LPR;
     const int heads_q = a.q ? a.Hq : 0, rows = heads_q + 2 * a.Hkv;
-    const int64_t at = (int64_t)a.len[b] + t;                       // row of the cache
+    const int64_t at = (a.base >= 0 ? a.base : (int64_t)a.len[b]) + t;      // row of the cache
     const int half = a.rotary / 2;
     u32x4 raw[U];
     // rows of the token: query heads, key heads, value heads
@@ -137,9 +137,10 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryCall a) {
             }
         }
     }
-    if (a.bump) {
-        __syncthreads();                                            // every thread has used the length
-        if (threadIdx.x == 0) a.len[b] = (int32_t)(at + 1);
+    // the length, where no workgroup reads it but this one
+    if (a.base >= 0 ? t == 0 : a.n == 1) {
+        __syncthreads();
+        if (threadIdx.x == 0 && a.advance) a.len[b] = (int32_t)(at - t + a.n);
     }
 }
 

@@ -420,23 +420,29 @@ class TopkAttnCache:
         all sequences of the layer, or to `seq` (S = 1).  positions [S, n] int32, by default the cache rows.  -> q [S, n, Hq, d]."""
         t = self.torch
         B, n, Hkv, d = k.shape
-        dt = self.torch_dtype()
-        for x, heads in ((q, self.shape[2]), (k, self.shape[3]), (v, self.shape[3])):
-            if x is not None:
-                assert x.device == self.device and x.dtype == dt and x.shape == (B, n, heads, self.shape[4])
-                assert x.stride(3) == 1 and (heads == 1 or x.stride(2) == d)
+        dt, dev, Hq = self.torch_dtype(), self.device, self.shape[2]
+
+        def rows(x, heads):
+            st = x.stride()
+            assert x.device == dev and x.dtype == dt and x.shape == (B, n, heads, self.shape[4])
+            assert st[3] == 1 and (heads == 1 or st[2] == d)
+            return x.data_ptr(), st[0] if B > 1 else 0, st[1] if n > 1 else 0      # (of one sequence or token: any stride)
+
+        def flat(x, dtype, shape):
+            if x is None:
+                return None
+            assert x.device == dev and x.dtype == dtype and x.shape == shape and x.is_contiguous()
+            return x.data_ptr()
         assert B == (self.shape[1] if seq < 0 else 1)
-        assert inv_freq.device == self.device and inv_freq.dtype == t.float32 and inv_freq.is_contiguous()
-        for w in (q_norm, k_norm):
-            assert w is None or (w.device == self.device and w.dtype == dt and w.shape == (d,) and w.is_contiguous())
-        if positions is not None:
-            assert positions.device == self.device and positions.dtype == t.int32 and positions.shape == (B, n) and positions.is_contiguous()
-        out = None if q is None else t.empty((B, n, self.shape[2], d), dtype=dt, device=self.device)
-        ptr = lambda x: None if x is None else x.data_ptr()
-        step = lambda x: (0, 0) if x is None else (x.stride(0) if B > 1 else 0, x.stride(1) if n > 1 else 0)      # (one of them: any stride)
+        q_ptr, q_seq, q_token = (None, 0, 0) if q is None else rows(q, Hq)
+        k_ptr, k_seq, k_token = rows(k, self.shape[3])
+        v_ptr, v_seq, v_token = rows(v, self.shape[3])
+        half = inv_freq.shape[0]
+        out = None if q is None else t.empty((B, n, Hq, d), dtype=dt, device=dev)
         topk_attn_append_rotary(self.h, layer, seq, Rotary(
-            ctypes.sizeof(Rotary), 2 * inv_freq.numel(), 1 if interleaved else 0, eps, n, ptr(q), ptr(k), ptr(v), *step(q), *step(k), *step(v),
-            ptr(out), ptr(q_norm), ptr(k_norm), ptr(inv_freq), ptr(positions)), self._stream())
+            ctypes.sizeof(Rotary), 2 * half, 1 if interleaved else 0, eps, n, q_ptr, k_ptr, v_ptr, q_seq, q_token, k_seq, k_token, v_seq,
+            v_token, None if q is None else out.data_ptr(), flat(q_norm, dt, (d,)), flat(k_norm, dt, (d,)),
+            flat(inv_freq, t.float32, (half,)), flat(positions, t.int32, (B, n))), self._stream())
         return out
 
     def _mass_ptr(self, mass):

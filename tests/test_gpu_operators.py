@@ -369,6 +369,9 @@ EVICT = [  # dtype, Hkv, d, lens, cap, budget, recent, index
     (wl.BF16, 1, 128, [3000, 64], 3001, 1000, 1000, ta.INDEX_BOXES),
     (wl.F32, 2, 64, [900], 900, 64, 3, ta.INDEX_BOXES),
     (wl.F16, 4, 128, [60000, 59000], 60000, 30000, 500, ta.INDEX_NONE),
+    (wl.F16, 2, 32, [200001, 16500, 30, 49999], 200001, 16000, 100, ta.INDEX_NONE),      # chunks of more tokens than registers
+    (wl.BF16, 1, 64, [16385, 32769, 16384], 32770, 16383, 0, ta.INDEX_INT8),
+    (wl.F32, 1, 32, [131073, 131072], 131073, 131072, 1, ta.INDEX_NONE),
 ]
 
 
@@ -435,6 +438,21 @@ def test_evict(dtype, Hkv, d, lens, cap, budget, recent, index):
         cache.close()
         if other is not None:
             other.close()
+
+
+@pytest.mark.parametrize("n,budget", [(3000, 1500), (16500, 400), (40000, 39990), (140000, 70000)])
+@pytest.mark.parametrize("value", [0.0, 1.5])
+def test_evict_among_equals_keeps_the_oldest(n, budget, value):
+    """All weights equal but a few above and a few below, at the ends of waves and chunks."""
+    cache, _, _ = make([n], 1, 1, 32, n, wl.F16, seed=n)
+    try:
+        mass0 = np.full((1, 1, n), value, np.float32)
+        mass0[0, 0, [63, 64, n // 2, n - 1]] = 9.0
+        mass0[0, 0, [0, 65, n // 3]] = -1.0
+        kept = cache.evict(0, torch.from_numpy(mass0).to(DEV), budget, 7)
+        assert np.array_equal(kept[0, 0].cpu().numpy(), ref.survivors(mass0[0], n, budget, 7)[0])
+    finally:
+        cache.close()
 
 
 def test_evict_orders_unusual_weights():
