@@ -256,7 +256,7 @@ int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_
     if (!h || !r || r->struct_size != sizeof(topk_attn_rotary)) return TOPK_ATTN_EINVAL;
     const topk_attn_config& c = h->cfg;
     if (layer < 0 || layer >= c.n_layers || seq < -1 || seq >= c.n_seqs || r->n_new < 0) return TOPK_ATTN_EINVAL;
-    if (r->rotary_dim < 0 || r->rotary_dim > c.head_dim || (r->rotary_dim & 1) || !(r->norm_eps >= 0.f)) return TOPK_ATTN_EINVAL;
+    if (r->rotary_dim < 0 || r->rotary_dim > c.head_dim || (r->rotary_dim & 1) || !(r->norm_eps >= 0.f) || isinf(r->norm_eps)) return TOPK_ATTN_EINVAL;
     if (r->n_new == 0) return TOPK_ATTN_OK;
     if (!r->k || !r->v || !r->q != !r->q_out || (r->rotary_dim && !r->inv_freq)) return TOPK_ATTN_EINVAL;
     const int e = elem_bytes(c.dtype);

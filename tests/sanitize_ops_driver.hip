@@ -1,0 +1,148 @@
+// Host-side walk through the entry points beside the top-k decode for the sanitizer run (tests/test_operators_cpu.py): api_ops.hip is linked
+// with stand-ins for the kernel launchers, which check what they are handed and report success, over handles that are put together here.
+// Every check that fails prints a line and makes the exit status 1.
+#include <math.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <vector>
+
+#include "../include/topk_attn.h"
+#include "../paper_2502_06766_amd/csrc/handle.h"
+#include "../paper_2502_06766_amd/csrc/internal.h"
+#include "../paper_2502_06766_amd/csrc/ops.h"
+
+static int failures = 0, launches = 0;
+#define CHECK(cond)                                                      \
+    do {                                                                 \
+        if (!(cond)) {                                                   \
+            printf("ops driver: line %d: %s\n", __LINE__, #cond);        \
+            ++failures;                                                  \
+        }                                                                \
+    } while (0)
+
+// stands in for the device: none, or one that is always current
+static bool have_device = false;
+extern "C" hipError_t hipGetDevice(int* d) { *d = 0; return have_device ? hipSuccess : hipErrorNoDevice; }
+static size_t cand_bytes;
+
+namespace tka {
+hipError_t launch_attend(const AttendCall& a, hipStream_t) {
+    ++launches;
+    CHECK(a.chunk >= 1 && a.n_split >= 1 && a.n_split <= kMaxSplits && (int64_t)a.n_split * a.chunk * 64 >= a.walk);
+    CHECK((int64_t)(a.n_split - 1) * a.chunk * 64 < a.walk);
+    // partial sums and their factors fit the place they are given
+    CHECK((size_t)a.B * a.Hq * a.n_split * ((size_t)a.D + 2) * 4 <= cand_bytes);
+    CHECK(a.walk <= (a.list ? a.Ncap : a.Ncap + 63) && a.score_stride == a.Ncap);
+    return hipSuccess;
+}
+hipError_t launch_block_scores(const BlockCall& a, hipStream_t) { ++launches; CHECK(a.pages <= a.Pcap && a.n_blocks >= 1); return hipSuccess; }
+hipError_t launch_block_select(const BlockCall& a, hipStream_t) { ++launches; CHECK(a.list_stride >= 1); return hipSuccess; }
+hipError_t launch_rotary(const RotaryCall& a, hipStream_t) { ++launches; CHECK(a.n >= 1 && a.B >= 1); return hipSuccess; }
+hipError_t launch_add_mass(const MassCall&, hipStream_t) { ++launches; return hipSuccess; }
+hipError_t launch_evict(const EvictCall& a, hipStream_t) {
+    ++launches;
+    int units = 0;
+    for (int x = 0; x < a.n_arrays; ++x) {
+        units += a.array[x].units;
+        CHECK((int64_t)a.array[x].units * a.array[x].unit_rows >= (a.array[x].cleared ? a.longest + a.recent : a.budget));
+        CHECK(a.array[x].unit_rows * (a.array[x].row >= 16 ? a.array[x].row / 16 : 1) == 256 * kEvictPieces);
+    }
+    CHECK(units == a.units && a.n_arrays <= kEvictArrays);
+    CHECK(a.longest <= kEvictHeldTokens || ((a.longest + a.chunk - 1) / a.chunk <= kEvictChunks && a.hist && a.pick));
+    return hipSuccess;
+}
+hipError_t launch_balls_again(int, int, const void*, int64_t, int64_t, int, int, const int32_t*, int64_t, void*, float*, hipStream_t) { ++launches; return hipSuccess; }
+hipError_t launch_page_balls(int, int, const void*, int64_t, int64_t, int, int, const int32_t*, int64_t, int64_t, void*, float*, hipStream_t) { ++launches; return hipSuccess; }
+}  // namespace tka
+
+// a handle as topk_attn_create() leaves it, over memory that nothing here touches
+static topk_attn handle(int B, int Hq, int Hkv, int D, int64_t cap, int dtype, int index, std::vector<int64_t> lens) {
+    topk_attn h{};
+    topk_attn_config& c = h.cfg;
+    c.struct_size = sizeof c;
+    c.n_layers = 2; c.n_seqs = B; c.n_q_heads = Hq; c.n_kv_heads = Hkv; c.head_dim = D; c.max_tokens = cap; c.max_k = 64; c.dtype = dtype;
+    c.index_kind = index;
+    c.kv_storage = reinterpret_cast<void*>(0x10000);
+    c.workspace = reinterpret_cast<void*>(0x20000);
+    h.ws.cand_cap = 32768;
+    h.kv_half = tka::kv_half_bytes(&c);
+    h.len.assign((size_t)2 * B, 0);
+    for (int b = 0; b < B; ++b) h.len[B + b] = lens[b % lens.size()];       // (layer 1)
+    h.n_cu = 256;
+    cand_bytes = (size_t)B * Hq * h.ws.cand_cap * 8;
+    return h;
+}
+
+int main() {
+    float f[4] = {};
+    void* p = reinterpret_cast<void*>(0x40000);
+    float* fp = reinterpret_cast<float*>(p);
+    int32_t* ip = reinterpret_cast<int32_t*>(p);
+    // no device is visible: a call that passes its checks ends at the device, and enqueues nothing
+    {
+        topk_attn h = handle(2, 8, 2, 64, 1000, TOPK_ATTN_F16, TOPK_ATTN_INDEX_BOXES, {100, 900});
+        CHECK(topk_attn_decode_dense(&h, 1, p, fp, nullptr, nullptr, nullptr) == TOPK_ATTN_EDEVICE);
+        CHECK(topk_attn_decode_dense(&h, 0, p, fp, nullptr, nullptr, nullptr) == TOPK_ATTN_EINVAL);        // empty sequences
+        CHECK(topk_attn_decode_dense(&h, 2, p, fp, nullptr, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(topk_attn_decode_dense(&h, -1, p, fp, nullptr, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(topk_attn_decode_dense(&h, 1, f + 1, fp, nullptr, nullptr, nullptr) == TOPK_ATTN_EINVAL || ((uintptr_t)(f + 1) & 15) == 0);
+        CHECK(topk_attn_decode_blocks(&h, 1, p, 0, fp, nullptr, nullptr, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(topk_attn_decode_blocks(&h, 1, p, 3, fp, nullptr, nullptr, nullptr, nullptr) == TOPK_ATTN_EDEVICE);
+        CHECK(topk_attn_add_mass(&h, 1, ip, fp, fp, 0, fp, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(topk_attn_add_mass(&h, 1, ip, fp, fp, 5, fp, nullptr) == TOPK_ATTN_EDEVICE);
+        CHECK(topk_attn_evict(&h, 1, fp, 901, 0, nullptr, nullptr) == TOPK_ATTN_OK);                       // nothing to do
+        CHECK(topk_attn_evict(&h, 1, fp, 500, 0, nullptr, nullptr) == TOPK_ATTN_EDEVICE);
+        CHECK(topk_attn_evict(&h, 1, fp, 500, 501, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(topk_attn_evict(&h, 1, fp, INT64_MAX, 0, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(topk_attn_evict(&h, 1, fp, INT64_MIN, 0, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        h.cfg.index_kind = TOPK_ATTN_INDEX_NONE;
+        CHECK(topk_attn_decode_blocks(&h, 1, p, 3, fp, nullptr, nullptr, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(h.len[2] == 100 && h.len[3] == 900 && launches == 0);
+    }
+    {
+        topk_attn h = handle(2, 8, 2, 64, 1000, TOPK_ATTN_F16, TOPK_ATTN_INDEX_NONE, {100, 900});
+        topk_attn_rotary r{};
+        r.struct_size = sizeof r; r.rotary_dim = 64; r.n_new = 1; r.k = r.v = p; r.inv_freq = fp;
+        CHECK(topk_attn_append_rotary(&h, 1, -1, &r, nullptr) == TOPK_ATTN_EDEVICE);
+        CHECK(topk_attn_append_rotary(&h, 1, -1, nullptr, nullptr) == TOPK_ATTN_EINVAL);
+        for (int64_t n : {(int64_t)101, INT64_MAX, (int64_t)1 << 40}) {
+            r.n_new = n;
+            CHECK(topk_attn_append_rotary(&h, 1, -1, &r, nullptr) == TOPK_ATTN_ECAPACITY);
+        }
+        r.n_new = 1;
+        for (int64_t s : {INT64_MAX, INT64_MAX - 7, INT64_MIN, (int64_t)-8, (int64_t)4}) {
+            r.k_seq_stride = s;
+            CHECK(topk_attn_append_rotary(&h, 1, -1, &r, nullptr) == TOPK_ATTN_EINVAL);
+        }
+        r.k_seq_stride = 0;
+        r.q = p;
+        CHECK(topk_attn_append_rotary(&h, 1, -1, &r, nullptr) == TOPK_ATTN_EINVAL);
+        r.q = nullptr; r.norm_eps = INFINITY;
+        CHECK(topk_attn_append_rotary(&h, 1, 0, &r, nullptr) == TOPK_ATTN_EINVAL);
+        CHECK(h.len[2] == 100 && h.len[3] == 900 && launches == 0);
+    }
+    // plans over shapes and lengths: what is handed to the launchers is checked there
+    have_device = true;
+    uint32_t seed = 12345;
+    const auto rnd = [&](uint32_t n) { seed = seed * 1664525u + 1013904223u; return (seed >> 8) % n; };
+    for (int i = 0; i < 3000; ++i) {
+        const int Hkv = 1 + (int)rnd(9), G = rnd(4) ? 1 + (int)rnd(16) : 1 + (int)rnd(128), B = rnd(3) ? 1 + (int)rnd(4) : 1 + (int)rnd(200);
+        const int dtype = G <= 16 ? (int)rnd(3) : 1 + (int)rnd(2), D = 32 << rnd(4);
+        const int64_t cap = rnd(8) ? 1 + rnd(200000) : 1 + (int64_t)rnd(1 << 24) * 100;
+        std::vector<int64_t> lens;
+        for (int b = 0; b < B; ++b) lens.push_back(rnd(2) ? cap : 1 + (int64_t)(rnd(1 << 24) / 16777216.0 * (double)cap));
+        topk_attn h = handle(B, Hkv * G, Hkv, D, cap, dtype, i & 1 ? TOPK_ATTN_INDEX_BOXES : TOPK_ATTN_INDEX_NONE, lens);
+        float* mass = rnd(2) ? fp : nullptr;
+        CHECK(topk_attn_decode_dense(&h, 1, p, fp, nullptr, mass, nullptr) == TOPK_ATTN_OK);
+        if (i & 1) CHECK(topk_attn_decode_blocks(&h, 1, p, 1 + (int)rnd(3000), fp, rnd(2) ? ip : nullptr, fp, mass, nullptr) == TOPK_ATTN_OK);
+        h.cfg.index_kind = rnd(2) ? TOPK_ATTN_INDEX_NONE : TOPK_ATTN_INDEX_INT8;
+        const int64_t budget = 1 + (int64_t)(rnd(1 << 24) / 16777216.0 * (double)cap), recent = (int64_t)(rnd(1 << 24) / 16777216.0 * (double)budget);
+        const int rc = topk_attn_evict(&h, 1, fp, budget, recent, rnd(2) ? ip : nullptr, nullptr);
+        CHECK(rc == TOPK_ATTN_OK || (rc == TOPK_ATTN_ENOMEM && cap > 1000000));
+        for (int b = 0; b < B; ++b) CHECK(h.len[B + b] == (rc == TOPK_ATTN_OK && lens[b] > budget ? budget : lens[b]));
+    }
+    CHECK(launches > 6000);
+    if (failures == 0) printf("ops driver: all checks passed\n");
+    return failures ? 1 : 0;
+}

@@ -83,3 +83,26 @@ def test_no_mfma_result_is_read_early_in_the_attention(tmp_path):
                           stderr=subprocess.DEVNULL)
     assert open(out).read().count("v_mfma") > 500
     assert not isa_check.check(out)
+
+
+@pytest.mark.skipif(not os.path.exists(hip_build.HIPCC), reason="hipcc not installed")
+def test_host_side_of_the_operators_under_asan_and_ubsan(tmp_path):
+    """api_ops.hip with sanitized host code, linked with stand-ins for the kernel launchers: refusals, calls that end at a missing device, and the
+    launch plans of random shapes, held against the room there is for them."""
+    import test_sanitizers_cpu as san
+    host = [x for f in ("-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=all") for x in ("-Xarch_host", f)]
+    common = [hip_build.HIPCC, "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-fPIC", *host, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+    objs = []
+    for src in (os.path.join(hip_build.CSRC, "api_ops.hip"), os.path.join(ROOT, "tests", "sanitize_ops_driver.hip")):
+        objs.append(str(tmp_path / (os.path.basename(src) + ".o")))
+        subprocess.check_call([*common, "-c", src, "-o", objs[-1]], stderr=subprocess.DEVNULL)
+    exe = str(tmp_path / "ops_san")
+    subprocess.check_call([hip_build.HIPCC, "--offload-arch=gfx950", "-fno-gpu-sanitize", "-fsanitize=address", "-fsanitize=undefined", *objs, "-o", exe],
+                          stderr=subprocess.DEVNULL)
+    env = dict(san.ENV, ASAN_OPTIONS=san.ENV["ASAN_OPTIONS"] + ":protect_shadow_gap=0",
+               LSAN_OPTIONS="suppressions=" + os.path.join(ROOT, "tests", "sanitize_lsan.supp") + ":print_suppressions=0",
+               HIP_VISIBLE_DEVICES="", ROCR_VISIBLE_DEVICES="")
+    r = subprocess.run([exe], env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, f"sanitizer run failed ({r.returncode}):\n{r.stdout[-2000:]}\n{r.stderr[-4000:]}"
+    assert "runtime error" not in r.stderr and "ERROR: AddressSanitizer" not in r.stderr, r.stderr[-4000:]
+    assert "ops driver: all checks passed" in r.stdout
