@@ -5,7 +5,7 @@
 //                       last workgroup of a key stream to finish puts the splits together
 //   attend_later_kernel with `mass`: the splits put together there, and the weights of the keys added up; also for many splits of many heads
 //
-// Bound by the read of K and V: 16 384 bytes per 32 keys and KV head against 2 x 32 MFMA (d = 128, 16 bit), a tenth of the time the read takes.
+// Bound by the read of K and V: 16 384 bytes per 32 keys and KV head against 24 (fp16) or 32 (bf16) MFMA (d = 128), a tenth of the time the read takes.
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
@@ -54,8 +54,9 @@ __device__ __forceinline__ float max_over_rows(float v) {      // largest of lan
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Weights of 16-bit caches are the operand of an MFMA and go in as two parts, the rounding to the type and what it left: 16 (bf16) or 22
-// (fp16) bits of each weight, errors of at most 2^-18 of it.  (One part alone: 2^-9, a hundred times what the sums' roundings make.)
+// Weights of 16-bit caches are the operand of an MFMA and go in as parts, each the rounding to the type of what the ones before it left: two of
+// fp16 (22 bits of each weight) and three of bf16 (all 24).  (One part alone: errors of 2^-9 of a weight; two of bf16: 2^-18, three times the error
+// that the sums' roundings make; the third costs nothing that shows: the MFMA of a step take a tenth of the time its rows do.)
 // fp16 has no numbers below 2^-24, so there the weights are relative to the maximum less 13 powers of two.
 template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
 
@@ -328,11 +329,16 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
             }
         } else {
             using v8 = typename Mfma<DT>::v8;
-            v8 hi, lo;
+            constexpr int PARTS = DT == DT_F16 ? 2 : 3;
+            v8 part[PARTS];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                hi[e] = (decltype(+hi[0]))p[e];
-                lo[e] = (decltype(+lo[0]))(p[e] - (float)hi[e]);
+                float rest = p[e];
+#pragma unroll
+                for (int x = 0; x < PARTS; ++x) {
+                    part[x][e] = (decltype(+part[x][0]))rest;
+                    rest -= (float)part[x][e];
+                }
             }
 #pragma unroll
             for (int c = 0; c < T; ++c) {
@@ -342,8 +348,8 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
                 u32x4 col;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) col[x] = __builtin_amdgcn_perm(t.v[2 * x + 1][w], t.v[2 * x][w], half);
-                acc[c] = Mfma<DT>::mac(__builtin_bit_cast(v8, col), hi, acc[c]);
-                acc[c] = Mfma<DT>::mac(__builtin_bit_cast(v8, col), lo, acc[c]);
+#pragma unroll
+                for (int x = 0; x < PARTS; ++x) acc[c] = Mfma<DT>::mac(__builtin_bit_cast(v8, col), part[x], acc[c]);
             }
         }
     };
