@@ -19,13 +19,15 @@ constexpr uint32_t kZeroMass = 0x80000000u;      // of zero: tokens no query has
 // The weight of the last survivor is found from the top of the keys' bits: 11 of them by a histogram in LDS, then 11 and 10 more among the keys
 // that share the ones before (or, where at most 512 keys do after the first, those compared with each other); then the survivors are written
 // in order, a stretch of the cache per wave.  One workgroup has up to 16384 tokens of a key stream in its registers and does it all
-// (8065 tokens 16 us).  Longer streams are cut into up to eight chunks and take a launch per step, each workgroup adding up the chunks'
+// (8065 tokens 12 us).  Longer streams are cut into up to eight chunks and take a launch per step, each workgroup adding up the chunks'
 // histograms of the step before for itself (32 streams of 5k to 100k tokens: 84 us in one
-// workgroup each, 45 in four launches); chunks of more than 16384 tokens are read again by each step.
+// workgroup each, 32 in four launches); chunks of more than 16384 tokens are read again by each step.
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave, kEvictList = 512, kEvictHeld = 16;
+constexpr int kEvictCopies = 4;       // of a histogram, for every fourth lane one (16384 tokens of 80 different bins 9.2 -> 6.5 us), 16 banks apart
 struct EvictShared {
     uint32_t tot[2][16];
-    uint32_t hist[kEvictBins];
+    uint32_t hist_[kEvictCopies][kEvictBins + 16];
+    __device__ __forceinline__ uint32_t count(int bin) const { return (hist_[0][bin] + hist_[1][bin]) + (hist_[2][bin] + hist_[3][bin]); }
     uint32_t list[kEvictList];
     uint32_t n_list, prefix, need;
     uint32_t above[kEvictWaves], equal[kEvictWaves];
@@ -38,15 +40,15 @@ __device__ __forceinline__ constexpr int digit_bits(int pass) { return pass == 2
 // The keys of tokens [c0, c1), c1 > c0: each wave has a stretch of `steps` times 64 neighbouring ones.
 template <bool HELD> struct KeyWalk {
     const float* mass;
-    int64_t c1, s0, steps;
+    uint32_t c1, s0, steps;                                    // (a cache has fewer than 2^31 tokens, by 256 at least: no sum here reaches 2^32)
     uint32_t held[HELD ? kEvictHeld : 1];
-    __device__ __forceinline__ KeyWalk(const float* m, int64_t c0, int64_t c1_) : mass(m), c1(c1_) {
-        steps = (c1 - c0 + kEvictThreads - 1) / kEvictThreads;
-        s0 = c0 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * steps * kWave + lane_id();
+    __device__ __forceinline__ KeyWalk(const float* m, int64_t c0, int64_t end) : mass(m), c1((uint32_t)end) {
+        steps = (uint32_t)((end - c0 + kEvictThreads - 1) / kEvictThreads);
+        s0 = (uint32_t)c0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * steps * kWave + (uint32_t)lane_id();
         if (HELD) {
             float v[HELD ? kEvictHeld : 1];
 #pragma unroll
-            for (int u = 0; u < (HELD ? kEvictHeld : 1); ++u) v[u] = u < steps ? mass[s0 + u * kWave < c1 ? s0 + u * kWave : c1 - 1] : 0.f;
+            for (uint32_t u = 0; u < (HELD ? kEvictHeld : 1); ++u) v[u] = u < steps ? mass[s0 + u * kWave < c1 ? s0 + u * kWave : c1 - 1] : 0.f;
 #pragma unroll
             for (int u = 0; u < (HELD ? kEvictHeld : 1); ++u) held[u] = mass_key(v[u]);
         }
@@ -55,36 +57,37 @@ template <bool HELD> struct KeyWalk {
     template <class F> __device__ __forceinline__ void each(F f) const {
         if (HELD) {
 #pragma unroll
-            for (int u = 0; u < (HELD ? kEvictHeld : 1); ++u)
+            for (uint32_t u = 0; u < (HELD ? kEvictHeld : 1); ++u)
                 if (u < steps) f(s0 + u * kWave, held[u], s0 + u * kWave < c1);
         } else {
-            constexpr int U = 16;
-            for (int64_t u0 = 0; u0 < steps; u0 += U) {
-                const int64_t i = s0 + u0 * kWave;
+            constexpr uint32_t U = 16;
+            for (uint32_t u0 = 0; u0 < steps; u0 += U) {
+                const uint32_t i = s0 + u0 * kWave;
                 float v[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = mass[i + u * kWave < c1 ? i + u * kWave : c1 - 1];
+                for (uint32_t u = 0; u < U; ++u) v[u] = mass[i + u * kWave < c1 ? i + u * kWave : c1 - 1];
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (uint32_t u = 0; u < U; ++u)
                     if (u0 + u < steps) f(i + u * kWave, mass_key(v[u]), i + u * kWave < c1);
             }
         }
     }
 };
-// Histogram of step `pass` of the keys whose higher bits are those of `prefix`, in sm.hist (the caller waits).
+// Histogram of step `pass` of the keys whose higher bits are those of `prefix`, in sm.count() (the caller waits).
 template <class Walk>
 __device__ __forceinline__ void digit_histogram(const Walk& keys, int pass, uint32_t prefix, EvictShared& sm) {
     const int shift = digit_shift(pass), bits = digit_bits(pass);
     const uint32_t mask = pass == 0 ? 0u : ~0u << (shift + bits);
-    for (int i = (int)threadIdx.x; i < kEvictBins; i += kEvictThreads) sm.hist[i] = 0;
+    for (int i = (int)threadIdx.x; i < kEvictCopies * (kEvictBins + 16); i += kEvictThreads) (&sm.hist_[0][0])[i] = 0;
     __syncthreads();
+    uint32_t* const hist = sm.hist_[threadIdx.x % kEvictCopies];
     uint32_t zeros = 0;                                        // (counted apart: thousands of additions to one counter otherwise)
-    keys.each([&](int64_t, uint32_t k, bool there) {
+    keys.each([&](uint32_t, uint32_t k, bool there) {
         if (!there) return;
         if (k == kZeroMass) ++zeros;
-        else if ((k & mask) == prefix) atomicAdd(&sm.hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+        else if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
     });
-    if (zeros && (kZeroMass & mask) == prefix) atomicAdd(&sm.hist[(kZeroMass >> shift) & ((1u << bits) - 1)], zeros);
+    if (zeros && (kZeroMass & mask) == prefix) atomicAdd(&hist[(kZeroMass >> shift) & ((1u << bits) - 1)], zeros);
 }
 // Thread t brings the counts of bins 2047 - 2 t and 2046 - 2 t.  `prefix` grows by the bin that the need-th key from above lies in, `need` becomes
 // its rank there.  (The caller waits before sm.prefix and sm.need are used again.)
@@ -107,10 +110,9 @@ __device__ __forceinline__ void write_survivors(const Walk& keys, uint32_t edge,
                                                 EvictShared& sm) {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     uint32_t above = 0, equal = 0;
-    keys.each([&](int64_t, uint32_t k, bool there) {
-        above += (uint32_t)__popcll(__ballot(there && k > edge));
-        equal += (uint32_t)__popcll(__ballot(there && k == edge));
-    });
+    keys.each([&](uint32_t, uint32_t k, bool there) { above += there && k > edge; equal += there && k == edge; });
+    above = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(above), kWave - 1);
+    equal = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(equal), kWave - 1);
     if (lane_id() == 0) { sm.above[wave] = above; sm.equal[wave] = equal; }
     __syncthreads();
     for (int w = 0; w < wave; ++w) {
@@ -118,12 +120,21 @@ __device__ __forceinline__ void write_survivors(const Walk& keys, uint32_t edge,
         at += sm.above[w] + (sm.equal[w] < left ? sm.equal[w] : left);
         equal_before += sm.equal[w];
     }
-    keys.each([&](int64_t i, uint32_t k, bool there) {
+    int32_t* to = kept + at;
+    if (equal == 0 || equal_before >= need) {                  // (of the wave's tokens none that is equal survives, as in most waves)
+        keys.each([&](uint32_t i, uint32_t k, bool there) {
+            const uint64_t m = __ballot(there && k > edge);
+            if (there && k > edge) to[mask_rank(m)] = (int32_t)i;
+            to += __popcll(m);
+        });
+        return;
+    }
+    keys.each([&](uint32_t i, uint32_t k, bool there) {
         const uint64_t eq = __ballot(there && k == edge);
         const bool keep = there && (k > edge || (k == edge && equal_before + (uint32_t)mask_rank(eq) < need));
         const uint64_t m = __ballot(keep);
-        if (keep) kept[at + (uint32_t)mask_rank(m)] = (int32_t)i;
-        at += (uint32_t)__popcll(m);
+        if (keep) to[mask_rank(m)] = (int32_t)i;
+        to += __popcll(m);
         equal_before += (uint32_t)__popcll(eq);
     });
 }
@@ -165,10 +176,10 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictCall a
         digit_histogram(keys, pass, prefix, sm);
         if (tid == 0) sm.n_list = 0;
         __syncthreads();
-        digit_pick(sm.hist[kEvictBins - 1 - 2 * tid], sm.hist[kEvictBins - 2 - 2 * tid], pass, prefix, need, sm);
-        const uint32_t have = sm.hist[prefix >> digit_shift(0)];
+        digit_pick(sm.count(kEvictBins - 1 - 2 * tid), sm.count(kEvictBins - 2 - 2 * tid), pass, prefix, need, sm);
+        const uint32_t have = sm.count((int)(prefix >> digit_shift(0)));
         if (pass == 0 && have <= kEvictList) {
-            keys.each([&](int64_t, uint32_t k, bool there) {
+            keys.each([&](uint32_t, uint32_t k, bool there) {
                 if (there && (k >> digit_shift(0)) == (prefix >> digit_shift(0))) sm.list[atomicAdd(&sm.n_list, 1u)] = k;
             });
             __syncthreads();
@@ -205,10 +216,12 @@ __global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) 
         if (PASS > 1) { prefix = pick[2 * (PASS - 2)]; need = pick[2 * (PASS - 2) + 1]; }
         const uint32_t* before = a.hist + (stream * 2 + ((PASS - 1) & 1)) * kEvictChunks * kEvictBins;
         uint32_t c1 = 0, c0_ = 0;
-        for (int x = 0; x < n_chunks; ++x) {
-            const uint2 v = *reinterpret_cast<const uint2*>(before + x * kEvictBins + kEvictBins - 2 - 2 * tid);
-            c0_ += v.x; c1 += v.y;
-        }
+        uint2 v[kEvictChunks];                                 // (all asked for at once)
+#pragma unroll
+        for (int x = 0; x < kEvictChunks; ++x)
+            v[x] = x < n_chunks ? *reinterpret_cast<const uint2*>(before + x * kEvictBins + kEvictBins - 2 - 2 * tid) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int x = 0; x < kEvictChunks; ++x) { c0_ += v[x].x; c1 += v[x].y; }
         digit_pick(c1, c0_, PASS - 1, prefix, need, sm);
         if (chunk == 0 && tid == 0) { pick[2 * (PASS - 1)] = prefix; pick[2 * (PASS - 1) + 1] = need; }
     }
@@ -216,12 +229,13 @@ __global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) 
         digit_histogram(keys, PASS, prefix, sm);
         if (PASS == 2) {
             uint32_t above = 0;
-            keys.each([&](int64_t, uint32_t k, bool there) { above += (uint32_t)__popcll(__ballot(there && (k >> digit_shift(1)) > (prefix >> digit_shift(1)))); });
+            keys.each([&](uint32_t, uint32_t k, bool there) { above += there && (k >> digit_shift(1)) > (prefix >> digit_shift(1)); });
+            above = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(above), kWave - 1);
             if (lane == 0) sm.above[tid >> 6] = above;
         }
         __syncthreads();
         uint32_t* mine = a.hist + ((stream * 2 + (PASS & 1)) * kEvictChunks + chunk) * kEvictBins;
-        for (int i = tid; i < kEvictBins; i += kEvictThreads) mine[i] = sm.hist[i];
+        for (int i = tid; i < kEvictBins; i += kEvictThreads) mine[i] = sm.count(i);
         if (PASS == 2 && tid == 0) {
             uint32_t above = 0;
             for (int w = 0; w < kEvictWaves; ++w) above += sm.above[w];
