@@ -182,7 +182,7 @@ typedef struct {
 } topk_attn_rotary;
 /* seq: one sequence of the layer, or -1: all B of them.  Enqueued on `hip_stream`; like the other appends not to be replayed from a
  * HIP graph.  Errors: EINVAL (null, range, odd or too large rotary_dim, misaligned, a negative stride, one of q / q_out alone),
- * ECAPACITY (nothing is enqueued then), EUNSUPPORTED (2^31 or more tokens in a call). */
+ * ECAPACITY (nothing is enqueued then), EUNSUPPORTED (2^24 or more tokens in a call). */
 int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_rotary* r, void* hip_stream);
 
 /* One decode step of `layer` for all B sequences: steps 1-3 above over all tokens
@@ -257,7 +257,8 @@ int topk_attn_decode_multi(topk_attn_t* h, int layer, const void* q, int n_queri
  *         its KV head, is added to mass[b][kv_head][position]; entries behind a sequence's length stay as they are.  No atomics: the
  *         same call gives the same bits.
  * A decode recorded into a HIP graph may be replayed as long as no sequence of the layer has grown or shrunk since.
- * Errors: EINVAL (null h/q/out, layer range, misaligned q, a sequence with no tokens), EUNSUPPORTED (2^31 workgroups or more). */
+ * Errors: EINVAL (null h/q/out, layer range, misaligned q, a sequence with no tokens), EUNSUPPORTED (2^22 or more
+ * sequences times KV heads, or a call of 2^24 or more workgroups).  An infinity among the values of attended tokens may come out as NaN. */
 int topk_attn_decode_dense(topk_attn_t* h, int layer, const void* q, float* out, float* lse, float* mass, void* hip_stream);
 
 /* Block-sparse attention of one new token per sequence: for every sequence and KV head the n_blocks best pages of 64 tokens, each
@@ -273,7 +274,7 @@ int topk_attn_decode_blocks(topk_attn_t* h, int layer, const void* q, int n_bloc
 /* The same accumulation from what a top-k decode of the layer returned: mass[b][h / G][idx] += exp(vals / sqrt(d) - lse) for the k entries of
  * every head (idx, vals [B, Hq, k], lse [B, Hq]; the positions of a head are distinct; entries with idx < 0 or >= max_tokens are passed over).
  * With a recent-token window lse covers the window too, whose tokens are not among idx.  No atomics: the same call gives the same bits.
- * Errors: EINVAL (null, layer range, k < 1). */
+ * Errors: EINVAL (null, layer range, k < 1), EUNSUPPORTED (2^22 or more sequences times KV heads). */
 int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const float* vals, const float* lse, int k, float* mass,
                        void* hip_stream);
 
@@ -286,7 +287,7 @@ int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const floa
  * Rows are numbered by their place in the cache from then on (idx, windows, causal chunks); a window or `recent` still means the newest
  * tokens.  Not to be replayed from a HIP graph (the lengths' host copy changes).
  * Errors: EINVAL (null h/mass, layer range, budget < 1, budget > max_tokens, recent outside 0 .. budget), ENOMEM (the workspace has no room for
- * a word per 64 KB of rows: budgets of tens of millions of tokens). */
+ * a word per 64 KB of rows: budgets of tens of millions of tokens), EUNSUPPORTED (2^22 or more sequences times KV heads). */
 int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int64_t recent, int32_t* kept, void* hip_stream);
 
 /* Host-only helper for the paper's layer-wise settings of k ("Layer-Wise Settings for k":

@@ -96,6 +96,7 @@ constexpr int64_t kJoinBytes = 192 << 10;
 int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* out, int32_t* blocks, float* lse, float* mass,
                void* hip_stream) {
     const topk_attn_config& c = h->cfg;
+    if ((int64_t)c.n_seqs * c.n_kv_heads > kMostStreams) return TOPK_ATTN_EUNSUPPORTED;
     const Layer l = layer_of(h, layer);
     int64_t longest = 0;
     for (int b = 0; b < c.n_seqs; ++b) {
@@ -111,24 +112,8 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     a.K = l.K; a.V = l.V; a.q = q; a.len = l.len;
     a.B = c.n_seqs; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = c.n_q_heads / c.n_kv_heads; a.D = c.head_dim; a.dtype = c.dtype;
     a.Ncap = c.max_tokens;
-    if (n_blocks) {
-        BlockCall p{};
-        p.boxes = l.index + l.stream0 * page_cap_of(&c) * 2 * l.row;
-        p.q = q; p.len = l.len;
-        p.score = scratch_at<double>(h, h->ws.block_score);
-        p.list = blocks ? blocks : scratch_at<int32_t>(h, h->ws.block_list);
-        // (a longer list than the cache has pages: only the caller's own array has room for it)
-        p.n_blocks = blocks ? n_blocks : (int)std::min<int64_t>(n_blocks, page_cap_of(&c));
-        p.list_stride = p.n_blocks;
-        p.Pcap = page_cap_of(&c); p.pages = pages;
-        p.B = a.B; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.G; p.D = a.D; p.dtype = a.dtype;
-        if (pages > n_blocks && launch_block_scores(p, st) != hipSuccess) return TOPK_ATTN_EDEVICE;
-        if ((blocks || pages > n_blocks) && launch_block_select(p, st) != hipSuccess) return TOPK_ATTN_EDEVICE;
-        if (pages > n_blocks) {
-            a.list = p.list; a.list_stride = p.list_stride; a.n_list = n_blocks;
-            pages = n_blocks;
-        }
-    }
+    const bool some = n_blocks && pages > n_blocks;              // (a sequence of at most n_blocks pages is attended whole)
+    if (some) pages = n_blocks;
     a.walk = pages * 64;
     a.score_stride = c.max_tokens;               // (of a list: whole pages, one less than the cache has at least)
     a.scores = scratch_at<float>(h, h->ws.scores);
@@ -153,8 +138,23 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     a.arrive = scratch_at<uint32_t>(h, h->ws.arrive);
     a.out = out; a.lse = lse; a.mass = mass;
     a.scale_log2e = 1.4426950408889634f / sqrtf((float)c.head_dim);
-    const hipError_t e = launch_attend(a, st);
-    return e == hipSuccess ? TOPK_ATTN_OK : e == hipErrorInvalidValue ? TOPK_ATTN_EUNSUPPORTED : TOPK_ATTN_EDEVICE;
+    if (attend_walk_wgs(a) > kMostWorkgroups || attend_join_wgs(a) + attend_mass_wgs(a) > kMostWorkgroups) return TOPK_ATTN_EUNSUPPORTED;
+    if (n_blocks) {
+        BlockCall p{};
+        p.boxes = l.index + l.stream0 * page_cap_of(&c) * 2 * l.row;
+        p.q = q; p.len = l.len;
+        p.score = scratch_at<double>(h, h->ws.block_score);
+        p.list = blocks ? blocks : scratch_at<int32_t>(h, h->ws.block_list);
+        // (a longer list than the cache has pages: only the caller's own array has room for it)
+        p.n_blocks = blocks ? n_blocks : (int)std::min<int64_t>(n_blocks, page_cap_of(&c));
+        p.list_stride = p.n_blocks;
+        p.Pcap = page_cap_of(&c); p.pages = (longest + 63) / 64;
+        p.B = a.B; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.G; p.D = a.D; p.dtype = a.dtype;
+        if (some) { a.list = p.list; a.list_stride = p.list_stride; a.n_list = n_blocks; }
+        if (some && launch_block_scores(p, st) != hipSuccess) return TOPK_ATTN_EDEVICE;
+        if ((blocks || some) && launch_block_select(p, st) != hipSuccess) return TOPK_ATTN_EDEVICE;
+    }
+    return launch_attend(a, st) == hipSuccess ? TOPK_ATTN_OK : TOPK_ATTN_EDEVICE;
 }
 
 }  // namespace
@@ -177,6 +177,7 @@ int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const floa
                        void* hip_stream) {
     if (!h || !idx || !vals || !lse || !mass || layer < 0 || layer >= h->cfg.n_layers || k < 1) return TOPK_ATTN_EINVAL;
     const topk_attn_config& c = h->cfg;
+    if ((int64_t)c.n_seqs * c.n_kv_heads > kMostStreams) return TOPK_ATTN_EUNSUPPORTED;
     const DeviceOf device(h);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     MassCall a{};
@@ -193,6 +194,7 @@ int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int6
     int64_t longest = 0;
     for (int b = 0; b < c.n_seqs; ++b) longest = std::max(longest, h->len[(size_t)layer * c.n_seqs + b]);
     if (longest <= budget && !kept) return TOPK_ATTN_OK;
+    if ((int64_t)c.n_seqs * c.n_kv_heads > kMostStreams) return TOPK_ATTN_EUNSUPPORTED;
     const Layer l = layer_of(h, layer);
     EvictCall a{};
     a.mass = mass; a.len = l.len; a.Ncap = c.max_tokens; a.budget = budget; a.recent = recent; a.B = c.n_seqs; a.Hkv = c.n_kv_heads;
@@ -269,7 +271,7 @@ int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_
     const size_t slot = (size_t)layer * c.n_seqs + b0;
     for (int b = 0; b < B; ++b)
         if (r->n_new > c.max_tokens - h->len[slot + b]) return TOPK_ATTN_ECAPACITY;
-    if ((int64_t)B * r->n_new > INT32_MAX) return TOPK_ATTN_EUNSUPPORTED;
+    if ((int64_t)B * r->n_new > kMostWorkgroups) return TOPK_ATTN_EUNSUPPORTED;
     const DeviceOf device(h);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     hipStream_t st = (hipStream_t)hip_stream;

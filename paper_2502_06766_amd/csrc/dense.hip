@@ -424,8 +424,6 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     join_splits<NT>(a, head0, heads, ns, WeightShift<DT>::value, lds, reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits));
 }
 
-constexpr int kMassPerBlock = 1024;      // keys whose weights one workgroup adds up
-
 // The first workgroups put a head's, or a block of heads', splits together; the others add each key's weights, the heads of the group in order, from the
 // scores that the walk left: 4 bytes per key and head written and read, where a second walk over the keys reads 2 d / G.
 __global__ void __launch_bounds__(256) attend_later_kernel(AttendCall a, float shift, int n_join) {
@@ -482,12 +480,10 @@ __global__ void __launch_bounds__(256) attend_later_kernel(AttendCall a, float s
 }
 
 hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
-    const int64_t units = (int64_t)a.B * a.Hkv * a.n_split;
-    const int64_t blocks = a.row_blocks > 1 ? (units + 7) / 8 * 8 * a.row_blocks : units;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t n_join = attend_join_wgs(a), n_mass = attend_mass_wgs(a);
 #define TKA_ATTEND(DT_, D_)                                                                                             \
     do {                                                                                                                \
-        const dim3 grid((unsigned)blocks), wg(256);                                                                     \
+        const dim3 grid((unsigned)attend_walk_wgs(a)), wg(256);                                                                     \
         if (a.list && a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, true>), grid, wg, 0, st, a);             \
         else if (a.list) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, false>), grid, wg, 0, st, a);                 \
         else if (a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, false, true>), grid, wg, 0, st, a);                 \
@@ -495,10 +491,7 @@ hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_ATTEND, a.dtype, a.D);
 #undef TKA_ATTEND
-    hipError_t e = hipGetLastError();
-    const int64_t n_join = a.join_later && a.n_split > 1 ? (int64_t)a.B * a.Hkv * (a.join_heads == 1 ? a.G : a.row_blocks) : 0;
-    const int64_t n_mass = !a.mass ? 0 : (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock);
-    if (n_join + n_mass > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || n_join + n_mass == 0) return e;
     hipLaunchKernelGGL(attend_later_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, (int)n_join);
     return hipGetLastError();

@@ -198,13 +198,13 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(EvictCall a
     write_survivors(keys, prefix, need, 0, 0, a.kept + stream * a.budget, sm);
 }
 
-// The same in steps, a launch each; grid (chunks, streams).  pick: per stream the prefix and rank after the steps so far, and per chunk the keys
+// The same in steps, a launch each; grid (streams, chunks).  pick: per stream the prefix and rank after the steps so far, and per chunk the keys
 // above the second step's prefix.  The histograms of a step lie in one of two places, those of the step before in the other.
 template <int PASS, bool HELD>
 __global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) {
     __shared__ EvictShared sm;
-    const int64_t stream = blockIdx.y;
-    const int tid = (int)threadIdx.x, chunk = (int)blockIdx.x, lane = lane_id();
+    const int64_t stream = blockIdx.x;
+    const int tid = (int)threadIdx.x, chunk = (int)blockIdx.y, lane = lane_id();
     int64_t n = 0;
     uint32_t need = evict_task(a, stream, PASS == 0 && chunk == 0, n), prefix = 0;
     const int64_t c0 = chunk * a.chunk;
@@ -365,12 +365,11 @@ __global__ void __launch_bounds__(kMassThreads) add_mass_kernel(MassCall a) {
 
 hipError_t launch_evict(const EvictCall& a, hipStream_t st) {
     const int64_t streams = (int64_t)a.B * a.Hkv;
-    if (streams * a.units > INT32_MAX) return hipErrorInvalidValue;
+    if (streams * a.units > kMostWorkgroups) return hipErrorInvalidValue;
     if (a.longest <= kEvictHeldTokens) {
         hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)streams), dim3(kEvictThreads), 0, st, a);
     } else {
-        if (streams > 65535) return hipErrorInvalidValue;
-        const dim3 grid((unsigned)((a.longest + a.chunk - 1) / a.chunk), (unsigned)streams);
+        const dim3 grid((unsigned)streams, (unsigned)((a.longest + a.chunk - 1) / a.chunk));
 #define TKA_STEP(PASS_)                                                                                                            \
     do {                                                                                                                          \
         if (a.chunk <= kEvictHeldTokens) hipLaunchKernelGGL((evict_step_kernel<PASS_, true>), grid, dim3(kEvictThreads), 0, st, a); \

@@ -4,6 +4,10 @@
 
 namespace tka {
 
+// A launch has fewer than 2^32 threads.
+constexpr int64_t kMostWorkgroups = (1 << 24) - 1;     // of 256
+constexpr int64_t kMostStreams = (1 << 22) - 1;        // one workgroup of 1024 each
+
 constexpr int kMaxSplits = 256;  // splits of a sequence (their factors sit in LDS when they are joined)
 
 // Attention of one query per sequence and head over all cached tokens, or over a list of pages of 64 tokens.
@@ -33,6 +37,18 @@ struct AttendCall {
     int row_blocks;             // blocks of 16 heads of a group
     float scale_log2e;          // log2(e) / sqrt(D)
 };
+constexpr int kMassPerBlock = 1024;      // keys whose weights one workgroup adds up
+// Workgroups of the walk, of the joins after it and of the sums of weights.
+inline int64_t attend_walk_wgs(const AttendCall& a) {
+    const int64_t units = (int64_t)a.B * a.Hkv * a.n_split;
+    return a.row_blocks > 1 ? (units + 7) / 8 * 8 * a.row_blocks : units;
+}
+inline int64_t attend_join_wgs(const AttendCall& a) {
+    return a.join_later && a.n_split > 1 ? (int64_t)a.B * a.Hkv * (a.join_heads == 1 ? a.G : a.row_blocks) : 0;
+}
+inline int64_t attend_mass_wgs(const AttendCall& a) {
+    return a.mass ? (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock) : 0;
+}
 hipError_t launch_attend(const AttendCall& a, hipStream_t st);
 
 // Pages of the block-sparse decode.

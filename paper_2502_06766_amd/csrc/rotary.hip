@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryCall a) {
 
 hipError_t launch_rotary(const RotaryCall& a, hipStream_t st) {
     const int64_t blocks = (int64_t)a.B * a.n;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (blocks > kMostWorkgroups) return hipErrorInvalidValue;
 #define TKA_ROTARY(DT_, D_) hipLaunchKernelGGL((rotary_kernel<DT_, D_>), dim3((unsigned)blocks), dim3(256), 0, st, a)
     TKA_BY_TYPE_AND_DIM(TKA_ROTARY, a.dtype, a.D);
 #undef TKA_ROTARY

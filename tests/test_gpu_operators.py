@@ -677,3 +677,80 @@ def test_refusals():
     finally:
         cache.close()
         boxes.close()
+
+
+def test_the_top_k_decode_is_unchanged_between_the_operators():
+    """The calls share the handle's scratch with the filtered top-k decode: its results before, between and after them are the same bits."""
+    cache, _, _ = make([70000, 50001], 8, 2, 128, 70000, wl.F16, seed=21, index=ta.INDEX_BOXES, max_k=500)
+    try:
+        q = H.to_torch(draw(np.random.default_rng(22), 2, 8, 128, dtype=wl.F16), wl.F16, DEV)
+        mass = torch.zeros((2, 2, 70000), device=DEV)
+        first = cache.decode(0, q, 500)
+        order = torch.sort(first[1], dim=2)
+        dense, _ = cache.decode_dense(0, q)
+        blocks = cache.decode_blocks(0, q, 40)
+        for step in (lambda: cache.decode_dense(0, q, mass=mass), lambda: cache.decode_blocks(0, q, 40, mass=mass),
+                     lambda: cache.add_mass(0, first[1], first[2], first[3], mass), lambda: cache.evict(0, mass, 70000, 5)):
+            step()
+            again = cache.decode(0, q, 500)
+            assert torch.equal(again[0], first[0]) and torch.equal(again[3], first[3])
+            assert torch.equal(torch.sort(again[1], dim=2).values, order.values)
+            assert torch.equal(cache.decode_dense(0, q)[0], dense)
+            got = cache.decode_blocks(0, q, 40)
+            assert torch.equal(got[0], blocks[0]) and torch.equal(got[1], blocks[1]) and torch.equal(got[2], blocks[2])
+    finally:
+        cache.close()
+
+
+def test_two_handles_on_two_streams():
+    caches, qs, want, got, streams = [], [], [], [], []
+    try:
+        for i in range(2):
+            cache, _, _ = make([30000 + i], 8, 2, 64, 30001, wl.BF16, seed=30 + i, index=ta.INDEX_BOXES)
+            caches.append(cache)
+            qs.append(H.to_torch(draw(np.random.default_rng(40 + i), 1, 8, 64, dtype=wl.BF16), wl.BF16, DEV))
+            want.append((cache.decode_dense(0, qs[i])[0], cache.decode_blocks(0, qs[i], 30)[0]))
+            streams.append(torch.cuda.Stream())
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for i in range(2):
+                with torch.cuda.stream(streams[i]):
+                    got.append((i, caches[i].decode_dense(0, qs[i])[0], caches[i].decode_blocks(0, qs[i], 30)[0]))
+        torch.cuda.synchronize()
+        for i, a, b in got:
+            assert torch.equal(a, want[i][0]) and torch.equal(b, want[i][1])
+    finally:
+        for cache in caches:
+            cache.close()
+
+
+def test_many_short_sequences_and_many_layers():
+    """Hundreds of sequences of one to a few tokens, on the last layer of several; the other layers stay as they are."""
+    B, Hq, Hkv, d, cap = 300, 4, 2, 64, 9
+    g = np.random.default_rng(50)
+    cache = ta.TopkAttnCache(3, B, Hq, Hkv, d, cap, 8, wl.F16, index_kind=ta.INDEX_BOXES)
+    try:
+        k, v = (H.to_torch(draw(g, B, 7, Hkv, d, dtype=wl.F16), wl.F16, DEV) for _ in range(2))
+        for b in range(B):
+            cache.append(2, b, k[b, :1 + b % 7].contiguous(), v[b, :1 + b % 7].contiguous())
+        q = draw(g, B, Hq, d, dtype=wl.F16)
+        qt = H.to_torch(q, wl.F16, DEV)
+        mass = torch.zeros((B, Hkv, cap), device=DEV)
+        out, lse = cache.decode_dense(2, qt, mass=mass)
+        out2, blocks, _ = cache.decode_blocks(2, qt, 1)
+        assert torch.equal(out, out2) and (blocks == 0).all()
+        for b in range(0, B, 37):
+            K, V = (x[b, :1 + b % 7].transpose(0, 1).double().cpu().numpy() for x in (k, v))
+            qb = wl.widen(q[b], wl.F16)
+            check(out[b].cpu().numpy().astype(np.float64), lse[b].cpu().numpy(), mass[b].cpu().numpy(), np.zeros((Hkv, cap), np.float32),
+                  ref.attend(qb, K, V), qb, K, V, d)
+        kept = cache.evict(2, mass, 3, 1)
+        assert [cache.length(2, b) for b in range(B)] == [min(3, 1 + b % 7) for b in range(B)]
+        for b in range(0, B, 41):
+            n = 1 + b % 7
+            assert (kept[b, :, min(n, 3):] == -1).all() and (kept[b, :, min(n, 3) - 1] == n - 1).all()
+        assert all(cache.length(layer, b) == 0 for layer in (0, 1) for b in range(0, B, 50))
+        with pytest.raises(ta.TopkAttnError):
+            cache.decode_dense(1, qt)
+    finally:
+        cache.close()
