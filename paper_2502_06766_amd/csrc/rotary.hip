@@ -1,5 +1,6 @@
 // New tokens' projections into the cache (topk_attn_append_rotary): keys and queries normalised per head and turned by their position,
-// values copied, in one pass: every element is read once and written once, which is what bounds it.
+// values copied, in one pass: every element is read once and written once, which is what bounds it.  8191 tokens of 32 + 2 x 8 heads, d = 128: 47 us for
+// 201 MB (4.3 TB/s; a large copy reaches 4.8); one token of 16 sequences 6.3 us, all latency.
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
