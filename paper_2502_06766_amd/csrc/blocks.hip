@@ -93,21 +93,22 @@ struct PickShared {
     uint64_t edge_key, prefix;
     uint32_t edge_page;
 };
-template <bool HELD>
+// HELD: pages a thread holds, or 0.
+template <int HELD>
 __device__ __forceinline__ void pick_pages(const double* score, int32_t* list, int64_t n, uint32_t want, PickShared& sm) {
     using Team = WorkgroupTeam<kPickThreads>;
     const int tid = (int)threadIdx.x;
     const int64_t per = (n + kPickThreads - 1) / kPickThreads;
     const int64_t i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
-    double held[HELD ? kPickHeld : 1];
+    double held[HELD ? HELD : 1];
     if (HELD) {
 #pragma unroll
-        for (int u = 0; u < kPickHeld; ++u) held[u] = i0 + u < i1 ? score[i0 + u] : 0.0;
+        for (int u = 0; u < HELD; ++u) held[u] = i0 + u < i1 ? score[i0 + u] : 0.0;
     }
     auto each = [&](auto f) {                                  // f(page, its score) for the thread's pages in order
         if (HELD) {
 #pragma unroll
-            for (int u = 0; u < kPickHeld; ++u)
+            for (int u = 0; u < HELD; ++u)
                 if (i0 + u < i1) f(i0 + u, held[u]);
         } else {
             for (int64_t i = i0; i < i1; ++i) f(i, score[i]);
@@ -216,8 +217,10 @@ __global__ void __launch_bounds__(kPickThreads) block_select_kernel(BlockCall a)
     const uint32_t want = (uint32_t)a.n_blocks - 1;            // 0 <= want < P - 1: the newest page is in without a search
     if (tid == 0) list[want] = (int32_t)(P - 1);
     if (want == 0) return;
-    if (P - 1 <= kPickHeld * kPickThreads) pick_pages<true>(score, list, P - 1, want, sm);
-    else pick_pages<false>(score, list, P - 1, want, sm);
+    if (P - 1 <= kPickThreads) pick_pages<1>(score, list, P - 1, want, sm);
+    else if (P - 1 <= 4 * kPickThreads) pick_pages<4>(score, list, P - 1, want, sm);
+    else if (P - 1 <= kPickHeld * kPickThreads) pick_pages<kPickHeld>(score, list, P - 1, want, sm);
+    else pick_pages<0>(score, list, P - 1, want, sm);
 }
 
 hipError_t launch_block_scores(const BlockCall& a, hipStream_t st) {
