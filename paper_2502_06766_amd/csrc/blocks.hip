@@ -80,7 +80,7 @@ __device__ __forceinline__ uint64_t ord_of(double v) {
 // One workgroup per key stream.  The page that ends the selection (its score, and among equal scores its number: lower ones first) is
 // found from a linear histogram between the smallest and the largest score, whose one bin in question is ranked by direct comparison,
 // or, where that bin is crowded or the scores are not finite, byte by byte of their ordered bits.  Then the pages up to it are written in
-// their order.  Each thread has `per` neighbouring pages: up to 16 of them stay in its registers (16384 pages, a million tokens: 19 us; 37 us
+// their order.  A wave has a stretch of the pages, 64 neighbouring ones at a time; up to 16 a thread stay in registers (16384 pages, a million tokens: 13 us; 37 us
 // when each of the five passes reads them again), and beyond they are read again.
 constexpr int kPickThreads = 1024, kPickBins = 1024, kPickList = 2048, kPickHeld = 16;
 struct PickShared {
@@ -90,34 +90,45 @@ struct PickShared {
     uint64_t key[kPickList];
     uint32_t page[kPickList];
     uint32_t n_list, bin, need;
+    uint32_t wave[kPickThreads / kWave];
     uint64_t edge_key, prefix;
     uint32_t edge_page;
 };
+// sum of the counts of the waves before this one (of at most 16)
+__device__ __forceinline__ uint32_t row_scan_add_below(const uint32_t* count, int wave) {
+    const uint32_t t = row_scan_add(count[lane_id() & 15]);
+    return wave ? (uint32_t)__builtin_amdgcn_readlane((int)t, wave - 1) : 0u;
+}
 // HELD: pages a thread holds, or 0.
 template <int HELD>
 __device__ __forceinline__ void pick_pages(const double* score, int32_t* list, int64_t n, uint32_t want, PickShared& sm) {
     using Team = WorkgroupTeam<kPickThreads>;
     const int tid = (int)threadIdx.x;
-    const int64_t per = (n + kPickThreads - 1) / kPickThreads;
-    const int64_t i0 = tid * per < n ? tid * per : n, i1 = i0 + per < n ? i0 + per : n;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t steps = (uint32_t)((n + kPickThreads - 1) / kPickThreads), end = (uint32_t)n;
+    const uint32_t s0 = (uint32_t)wave * steps * kWave + (uint32_t)lane;
     double held[HELD ? HELD : 1];
     if (HELD) {
 #pragma unroll
-        for (int u = 0; u < HELD; ++u) held[u] = i0 + u < i1 ? score[i0 + u] : 0.0;
+        for (uint32_t u = 0; u < HELD; ++u) held[u] = u < steps ? score[s0 + u * kWave < end ? s0 + u * kWave : end - 1] : 0.0;
     }
-    auto each = [&](auto f) {                                  // f(page, its score) for the thread's pages in order
+    // f(page, its score, there is such a page) for 64 neighbouring pages at a time, in order
+    auto all = [&](auto f) {
         if (HELD) {
 #pragma unroll
-            for (int u = 0; u < HELD; ++u)
-                if (i0 + u < i1) f(i0 + u, held[u]);
+            for (uint32_t u = 0; u < HELD; ++u)
+                if (u < steps) f(s0 + u * kWave, held[u], s0 + u * kWave < end);
         } else {
-            for (int64_t i = i0; i < i1; ++i) f(i, score[i]);
+            for (uint32_t u = 0; u < steps; ++u) f(s0 + u * kWave, score[s0 + u * kWave < end ? s0 + u * kWave : end - 1], s0 + u * kWave < end);
         }
+    };
+    auto each = [&](auto f) {                                  // f(page, its score) for the thread's pages
+        all([&](uint32_t i, double s, bool there) { if (there) f(i, s); });
     };
     // range of the scores, in 32 bits (a histogram edge needs no more)
     float lo = INFINITY, hi = -INFINITY;
     bool bad = false;
-    each([&](int64_t, double s) {
+    each([&](uint32_t, double s) {
         const float v = (float)s;
         bad |= !(fabsf(v) < INFINITY);
         lo = fminf(lo, v); hi = fmaxf(hi, v);
@@ -131,7 +142,7 @@ __device__ __forceinline__ void pick_pages(const double* score, int32_t* list, i
     // (monotone: a rounding, a difference and a product with a positive number)
     auto bin_of = [&](double s) { const int x = (int)(((float)s - lo) * inv); return x < kPickBins - 1 ? x : kPickBins - 1; };
     if (listed) {
-        each([&](int64_t, double s) { atomicAdd(&sm.hist[bin_of(s)], 1u); });
+        each([&](uint32_t, double s) { atomicAdd(&sm.hist[bin_of(s)], 1u); });
         __syncthreads();
         // thread t looks at bin 1023 - t: the bin in which the want-th score from above lies
         const uint32_t c = sm.hist[kPickBins - 1 - tid];
@@ -142,10 +153,10 @@ __device__ __forceinline__ void pick_pages(const double* score, int32_t* list, i
         const int bin = (int)sm.bin;
         listed = sm.hist[bin] <= kPickList;
         if (listed) {
-            each([&](int64_t i, double s) {
+            each([&](uint32_t i, double s) {
                 if (bin_of(s) == bin) {
                     const uint32_t at = atomicAdd(&sm.n_list, 1u);      // (in any order: they are ranked by score and number)
-                    sm.key[at] = ord_of(s); sm.page[at] = (uint32_t)i;
+                    sm.key[at] = ord_of(s); sm.page[at] = i;
                 }
             });
             __syncthreads();
@@ -168,7 +179,7 @@ __device__ __forceinline__ void pick_pages(const double* score, int32_t* list, i
             for (int i = tid; i < 256; i += kPickThreads) sm.hist[i] = 0;
             __syncthreads();
             const uint64_t mask = shift == 56 ? 0ull : ~0ull << (shift + 8);
-            each([&](int64_t, double s) {
+            each([&](uint32_t, double s) {
                 const uint64_t k = ord_of(s);
                 if ((k & mask) == prefix) atomicAdd(&sm.hist[(k >> shift) & 255], 1u);
             });
@@ -181,26 +192,38 @@ __device__ __forceinline__ void pick_pages(const double* score, int32_t* list, i
             prefix = sm.prefix; need = sm.need;
         }
         uint32_t same = 0;
-        each([&](int64_t, double s) { same += ord_of(s) == prefix; });
-        uint32_t total;
-        uint32_t before = team_prefix<Team>(same, total, sm, 1);
-        each([&](int64_t i, double s) {
-            if (ord_of(s) == prefix && ++before == need) { sm.edge_key = prefix; sm.edge_page = (uint32_t)i; }
+        each([&](uint32_t, double s) { same += ord_of(s) == prefix; });
+        same = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(same), kWave - 1);
+        if (lane == 0) sm.wave[wave] = same;
+        __syncthreads();
+        uint32_t before = row_scan_add_below(sm.wave, wave);
+        all([&](uint32_t i, double s, bool there) {
+            const bool eq = there && ord_of(s) == prefix;
+            const uint64_t m = __ballot(eq);
+            if (eq && before + (uint32_t)mask_rank(m) == need - 1) { sm.edge_key = prefix; sm.edge_page = i; }
+            before += (uint32_t)__popcll(m);
         });
     }
     __syncthreads();
     const uint64_t edge_key = sm.edge_key;                     // selected: key > edge_key, or equal and page <= edge_page
     const uint32_t edge_page = sm.edge_page;
-    auto picked = [&](int64_t i, double s) {
+    auto picked = [&](uint32_t i, double s) {
         const uint64_t k = ord_of(s);
-        return k > edge_key || (k == edge_key && (uint32_t)i <= edge_page);
+        return k > edge_key || (k == edge_key && i <= edge_page);
     };
     uint32_t mine = 0;
-    each([&](int64_t i, double s) { mine += picked(i, s); });
-    uint32_t total;
-    uint32_t at = team_prefix<Team>(mine, total, sm, 0);
-    each([&](int64_t i, double s) {
-        if (picked(i, s)) list[at++] = (int32_t)i;
+    each([&](uint32_t i, double s) { mine += picked(i, s); });
+    mine = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(mine), kWave - 1);
+    __syncthreads();                                           // (sm.wave has been read)
+    if (lane == 0) sm.wave[wave] = mine;
+    __syncthreads();
+    int32_t* to = list + (row_scan_add_below(sm.wave, wave));
+    if (mine == 0) return;
+    all([&](uint32_t i, double s, bool there) {
+        const bool in = there && picked(i, s);
+        const uint64_t m = __ballot(in);
+        if (in) to[mask_rank(m)] = (int32_t)i;
+        to += __popcll(m);
     });
 }
 __global__ void __launch_bounds__(kPickThreads) block_select_kernel(BlockCall a) {
