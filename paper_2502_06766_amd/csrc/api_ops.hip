@@ -223,7 +223,7 @@ int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int6
         a.hist = take(streams * 2 * kEvictChunks * kEvictBins);
         a.pick = take(streams * kEvictPick);
     }
-    a.state = take(1 + streams * a.units);
+    a.state = take(streams * (a.units + 1));
     a.old_len = reinterpret_cast<int32_t*>(take(c.n_seqs));
     if (words * 4 > (size_t)c.n_seqs * c.n_q_heads * h->ws.cand_cap * sizeof(uint64_t)) return TOPK_ATTN_ENOMEM;
     const DeviceOf device(h);

@@ -146,11 +146,8 @@ __device__ __forceinline__ uint32_t evict_task(const EvictCall& a, int64_t strea
     const int64_t N = a.len[b];
     int32_t* const kept = a.kept + stream * a.budget;
     if (first) {
-        for (int i = tid; i < a.units; i += kEvictThreads) a.state[1 + stream * a.units + i] = 0u;
-        if (tid == 0) {
-            if (stream == 0) a.state[0] = 0u;
-            if (stream == (int64_t)b * a.Hkv) a.old_len[b] = (int32_t)N;
-        }
+        for (int i = tid; i <= a.units; i += kEvictThreads) a.state[stream * (a.units + 1) + i] = 0u;
+        if (tid == 0 && stream == (int64_t)b * a.Hkv) a.old_len[b] = (int32_t)N;
     }
     if (N <= a.budget) {                                       // all stay
         if (first)
@@ -265,18 +262,21 @@ __global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) 
 
 // Row j of the cache becomes row kept[j] >= j, for all j of a stream, in place.  A workgroup holds a unit of neighbouring rows j in
 // registers; it may overwrite them once every unit whose sources lie among them has read its own.  Those are units before it (kept[j] >= j),
-// each of which raises a flag when its loads have come back and waits for nothing before that.  Units are handed out by a counter, so the
-// units before a unit are always in the hands of a workgroup that runs or has run: every wait ends.  Flags carry no data (the rows
+// each of which raises a flag when its loads have come back and waits for nothing before that.  The units of a stream are handed out by a
+// counter, so those before a unit are always in the hands of a workgroup that runs or has run: every wait ends.  (A counter a stream, and the
+// streams in turn, so that the units before one were handed out some time ago: one counter,
+// stream after stream, took 131 us where this takes 117.)  Flags carry no data (the rows
 // themselves were written by earlier launches), so they need no more than the loads' return in front of them.
-// One read and one write of the rows that move; through a buffer it would be two of each.  32 streams cut to 16384 tokens (537 MB): 131 us, 4.1 TB/s
+// One read and one write of the rows that move; through a buffer it would be two of each.  32 streams cut to 16384 tokens (537 MB): 117 us, 4.6 TB/s
 // (a large copy reaches 4.8).
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictCall a) {
     __shared__ uint32_t ticket;
-    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(&a.state[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int64_t stream = blockIdx.x % (uint32_t)(a.B * a.Hkv);
+    uint32_t* flags = a.state + stream * (a.units + 1);
+    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(flags, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    const int64_t stream = ticket / (uint32_t)a.units;
-    int unit = (int)(ticket - (uint32_t)stream * (uint32_t)a.units);
-    uint32_t* flags = a.state + 1 + stream * a.units;
+    int unit = (int)ticket;                                     // (as many workgroups as units have the stream)
+    ++flags;
     const int b = (int)(stream / a.Hkv);
     const int64_t N = a.old_len[b];
     if (N <= a.budget) return;                                  // (the whole stream: nobody waits for it)

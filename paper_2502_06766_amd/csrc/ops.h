@@ -108,7 +108,7 @@ struct EvictCall {
     float* mass;                // [B][Hkv][Ncap]
     int32_t* len;               // [B]
     int32_t* kept;              // [B][Hkv][budget], or scratch of the same shape
-    uint32_t* state;            // scratch: one word for the next unit, then a flag per unit and key stream
+    uint32_t* state;            // scratch [B * Hkv][1 + units]: the next unit, then a flag per unit
     int32_t* old_len;           // scratch [B]
     uint32_t* hist;             // scratch [B * Hkv][2][kEvictChunks][kEvictBins], for streams of more than kEvictHeldTokens
     uint32_t* pick;             // scratch [B * Hkv][kEvictPick]
