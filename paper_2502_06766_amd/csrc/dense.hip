@@ -271,16 +271,20 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
 #pragma unroll
         for (int g = 0; g < SUB; ++g) {
             s[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (DT == DT_F32) {
+                // four sums of a quarter of the channels each: shorter chains, whose roundings are what a score's error is
+                f32x4 part[4] = {};
 #pragma unroll
-            for (int c = 0; c < KCH; ++c) {
-                if constexpr (DT == DT_F32) {
+                for (int c = 0; c < KCH; ++c) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[g][c][x]), __uint_as_float(q[c][x]), s[g], 0, 0, 0);
-                } else {
-                    using v8 = typename Mfma<DT>::v8;
-                    s[g] = Mfma<DT>::mac(__builtin_bit_cast(v8, t.k[g][c]), __builtin_bit_cast(v8, q[c]), s[g]);
+                        part[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[g][c][x]), __uint_as_float(q[c][x]), part[x], 0, 0, 0);
                 }
+                s[g] = (part[0] + part[1]) + (part[2] + part[3]);
+            } else {
+                using v8 = typename Mfma<DT>::v8;
+#pragma unroll
+                for (int c = 0; c < KCH; ++c) s[g] = Mfma<DT>::mac(__builtin_bit_cast(v8, t.k[g][c]), __builtin_bit_cast(v8, q[c]), s[g]);
             }
         }
         if (MASS) {
