@@ -148,7 +148,7 @@ int topk_attn_append_kv(topk_attn_t* h, int layer, int seq, const void* k_new, c
                         int64_t n_new, int64_t token_stride, int64_t head_stride, void* hip_stream);
 
 /* The per-step concat of Algorithm 1 for a whole batch: append n_new tokens to EVERY
- * sequence of `layer` in one call (two launches whatever B is, three with an int8 index;
+ * sequence of `layer` in one call (two launches whatever B is, three with an index;
  * topk_attn_append_kv costs one per sequence).  k_new / v_new: device [B, n_new, Hkv, d], contiguous, 16-byte
  * aligned.  Errors: EINVAL, ECAPACITY if any sequence would exceed max_tokens (nothing is
  * enqueued then).  n_new == 0 is a no-op. */

@@ -264,9 +264,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) 
 // registers; it may overwrite them once every unit whose sources lie among them has read its own.  Those are units before it (kept[j] >= j),
 // each of which raises a flag when its loads have come back and waits for nothing before that.  The units of a stream are handed out by a
 // counter, so those before a unit are always in the hands of a workgroup that runs or has run: every wait ends.  (A counter a stream, and the
-// streams in turn, so that the units before one were handed out some time ago: one counter,
-// stream after stream, took 131 us where this takes 117.)  Flags carry no data (the rows
-// themselves were written by earlier launches), so they need no more than the loads' return in front of them.
+// streams in turn, so that the units before one were handed out some time ago: one counter, stream after stream, took 131 us where this takes
+// 117.)  Flags carry no data (the rows themselves were written by earlier launches), so they need no more than the loads' return in front of them.
 // One read and one write of the rows that move; through a buffer it would be two of each.  32 streams cut to 16384 tokens (537 MB): 117 us, 4.6 TB/s
 // (a large copy reaches 4.8).
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictCall a) {
