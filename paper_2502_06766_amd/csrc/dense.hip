@@ -382,6 +382,9 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         }
     }
     l = add_lanes_32(add_lanes_16(l));
+    // A maximum passes over NaN: a wave of nothing but NaN and -inf would count as one without a key.  With a maximum of +inf its factor is NaN, here
+    // and where splits are joined.
+    if (l != l) m = INFINITY;
     // the waves' sums, relative to the largest of their maxima
     if (j == 0) { red_m[wave][n] = m; red_l[wave][n] = l; }
     if (n < heads) {

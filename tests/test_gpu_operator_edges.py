@@ -1,0 +1,105 @@
+"""Edges of the operators beside the top-k decode, on the GPU through the binding: NaN among keys, products and sums beyond the range or the
+length that 32 bits take, calls recorded before a sequence grew, and sums held to a few roundings."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import helpers as H
+from oracle import operators_ref as ref
+from paper_2502_06766_amd import topk_attn as ta
+from paper_2502_06766_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda", 0) if torch.cuda.is_available() else None
+U = 2.0 ** -24                                                   # half a step of fp32 relative to the value
+TYPES = [wl.F32, wl.F16, wl.BF16]
+
+
+def draw(g, *shape, dtype):
+    return wl.quantize(g.standard_normal(shape).astype(np.float32), dtype)
+
+
+def filled(K, V, dtype, Hq, index=ta.INDEX_NONE, room=0, max_k=8):
+    """A cache of one sequence with keys and values [Hkv, n, d] in the storage type; unused rows are NaN."""
+    Hkv, n, d = K.shape
+    cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, n + room, max_k, dtype, index_kind=index)
+    cache.kv.fill_(255)
+    cache.append(0, 0, H.to_torch(K, dtype, DEV), H.to_torch(V, dtype, DEV), head_major=True)
+    return cache
+
+
+def close(got, want, K, q, V, d, label):
+    """out of finite heads: scores off by (d + 6) u sum |q k| / sqrt(d), weights by as much, values up to max |V|."""
+    Hkv = K.shape[0]
+    A = max((np.abs(K[h]) @ np.abs(q.reshape(Hkv, -1, d)[h]).T).max() for h in range(Hkv)) / np.sqrt(d)
+    tol = 2 * ((d + 6) * U * A + (K.shape[1] / 16 + 64) * U + 2.0 ** -18) * np.abs(V).max()
+    assert np.abs(got - want).max() <= tol, f"{label}: off by {np.abs(got - want).max():.3g}, {tol:.3g} allowed"
+
+
+@pytest.mark.parametrize("blocks", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,before", [(1, 0), (17, 0), (33, 0), (33, 8), (65, 0), (97, 0), (97, 64), (129, 0), (641, 0), (5000, 0), (40001, 200)])
+def test_a_nan_key_is_not_lost(n, before, dtype, blocks):
+    """The newest key of KV head 1 is NaN, alone in its step or its split, or behind keys of -inf: its heads, their lse and their weights are
+    NaN, whatever else there is; the other heads' are those of finite keys."""
+    Hq, Hkv, d, n_blocks = 8, 4, 128, 3
+    g = np.random.default_rng(n + before)
+    K, V = draw(g, Hkv, n, d, dtype=dtype), draw(g, Hkv, n, d, dtype=dtype)
+    q = np.abs(wl.widen(draw(g, 1, Hq, d, dtype=dtype), dtype)).astype(np.float32) + np.float32(0.1)
+    q = wl.quantize(q, dtype)
+    Kf = wl.widen(K, dtype).astype(np.float32)
+    Kf[1, n - 1 - before:n - 1, 3] = -np.inf
+    Kf[1, n - 1, 7] = np.nan
+    K = wl.quantize(Kf, dtype) if dtype != wl.BF16 else (Kf.view(np.uint32) >> 16).astype(np.uint16)
+    cache = filled(K, V, dtype, Hq, ta.INDEX_BOXES if blocks else ta.INDEX_NONE, room=3)
+    try:
+        for mass in (None, torch.zeros((1, Hkv, n + 3), device=DEV)):
+            if blocks:
+                out, pages, lse = cache.decode_blocks(0, H.to_torch(q, dtype, DEV), n_blocks, mass=mass)
+                at = ref.block_tokens([[p for p in x if p >= 0] for x in pages[0].cpu().numpy()], n)
+            else:
+                out, lse = cache.decode_dense(0, H.to_torch(q, dtype, DEV), mass=mass)
+                at = [np.arange(n)] * Hkv
+            out, lse = out[0].double().cpu().numpy(), lse[0].double().cpu().numpy()
+            assert np.isnan(out[2:4]).all() and np.isnan(lse[2:4]).all()
+            q64, V64 = wl.widen(q[0], dtype), wl.widen(V, dtype)
+            fine = [0, 2, 3]
+            K64 = Kf.astype(np.float64)
+            K64[1] = 0.0
+            want, want_lse, want_mass = ref.attend(q64, K64, V64, at)
+            heads = [0, 1, 4, 5, 6, 7]
+            close(out[heads], want[heads], K64, q64, V64, d, f"{n} tokens")
+            assert np.isfinite(lse[heads]).all()
+            if mass is not None:
+                m = mass[0].cpu().numpy()
+                assert np.isnan(m[1, at[1]]).all() and (m[:, n:] == 0).all()
+                for h in fine:
+                    assert np.isfinite(m[h]).all() and abs(m[h].sum() - 2) < 1e-3
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [33, 65, 641])
+def test_an_infinite_key_is_nan_for_the_heads_that_meet_it_with_zero(n, dtype):
+    """One infinite channel of the newest key: heads of a zero there score NaN, of a positive number +inf (NaN too), of a negative one -inf: the
+    key has no weight."""
+    d, Hq = 64, 3
+    g = np.random.default_rng(n)
+    K, V = draw(g, 1, n, d, dtype=dtype), draw(g, 1, n, d, dtype=dtype)
+    Kf, qf = wl.widen(K, dtype).astype(np.float32), wl.widen(draw(g, 1, Hq, d, dtype=dtype), dtype).astype(np.float32)
+    Kf[0, n - 1, 5] = np.inf
+    qf[0, :, 5] = [0.0, 1.0, -1.0]
+    K, q = wl.quantize(Kf, dtype), wl.quantize(qf, dtype)
+    cache = filled(K, V, dtype, Hq)
+    try:
+        out, lse = cache.decode_dense(0, H.to_torch(q, dtype, DEV))
+        out, lse = out[0].double().cpu().numpy(), lse[0].double().cpu().numpy()
+        assert np.isnan(out[:2]).all() and np.isnan(lse[:2]).all()
+        q64, K64, V64 = wl.widen(q[0], dtype), wl.widen(K, dtype)[:, :n - 1], wl.widen(V, dtype)[:, :n - 1]
+        want, want_lse, _ = ref.attend(q64, K64, V64)
+        close(out[2:], want[2:], K64, q64, V64, d, f"{n} tokens")
+    finally:
+        cache.close()
