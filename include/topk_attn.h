@@ -80,7 +80,8 @@ enum {
                                    cannot hold a key that scores more than q . c + |q| r (Cauchy-Schwarz).
                                    16-bit dtypes, Hq/Hkv <= 4. */
     TOPK_ATTN_INDEX_BOXES = 4   /* plus the block index of topk_attn_decode_blocks: per page of 64 consecutive tokens the
-                                   smallest and the largest key, channel by channel, in `dtype`.  The top-k
+                                   smallest and the largest key, channel by channel, in `dtype` (both NaN
+                                   where a key of the page is NaN in that channel).  The top-k
                                    decodes take the exact path on such a handle.  All dtypes and head groups. */
 };
 
@@ -263,8 +264,9 @@ int topk_attn_decode_dense(topk_attn_t* h, int layer, const void* q, float* out,
 
 /* Block-sparse attention of one new token per sequence: for every sequence and KV head the n_blocks best pages of 64 tokens, each
  * attended whole by the heads of the group.  A page's score is the largest raw score any key in its box (TOPK_ATTN_INDEX_BOXES) could
- * have with any of the group's heads, max_h sum_c max(q_hc lo_c, q_hc hi_c), in 64 bits; ties go to the lower page.  The page of the newest
- * token is always one of the n_blocks.  A sequence of at most n_blocks pages is attended densely.
+ * have with any of the group's heads, max_h sum_c max(q_hc lo_c, q_hc hi_c), in 64 bits; ties go to the lower page.  A page of which any head's
+ * sum is NaN (a NaN key; a zero of the query times an infinite hi_c) comes before all others, so that its heads are NaN as in the dense
+ * decode.  The page of the newest token is always one of the n_blocks.  A sequence of at most n_blocks pages is attended densely.
  *   blocks  device [B, Hkv, n_blocks] int32 or NULL: the pages attended, ascending; -1 behind them
  *   lse     over the attended tokens;  mass as in topk_attn_decode_dense, for the attended tokens
  * Errors as topk_attn_decode_dense; EINVAL without a block index or if n_blocks < 1. */

@@ -64,15 +64,15 @@ __global__ void __launch_bounds__(256) page_score_kernel(BlockCall a) {
             }
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            best = fmax(best, sum);
+            if (sum > best || sum != sum) best = sum;              // (a NaN stays)
         }
     }
     if (j == 0 && page < P) a.score[stream * a.Pcap + page] = best;
 }
 
-// Monotone map double -> uint64 (NaN below all; -0 with +0).
+// Monotone map double -> uint64 (NaN above all: the page is attended and the NaN seen; -0 with +0).
 __device__ __forceinline__ uint64_t ord_of(double v) {
-    if (!(v == v)) return 0ull;
+    if (!(v == v)) return ~0ull;
     const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
     return u ^ ((u >> 63) ? ~0ull : 0x8000000000000000ull);
 }

@@ -16,7 +16,7 @@ __device__ __forceinline__ uint32_t stored_bits(float v) {
 
 // Boxes of every page that rows [row0, row0 + n_new) touch, from all rows the page holds then (one read of at most 64 rows; the row0 of a
 // batched append is the sequence's length).  n_new < 0: of all rows below the length.  One wave per page, bound by the read of the keys.
-// A NaN in a key is left out (fminf).
+// A NaN in a key makes both edges of its channel NaN.
 template <int DT, int D>
 __global__ void __launch_bounds__(256)
 page_box_kernel(const char* __restrict__ K, int64_t Ncap, int64_t Pcap, int Hkv, const int32_t* __restrict__ len_dev, int64_t row0_host,
@@ -47,13 +47,16 @@ page_box_kernel(const char* __restrict__ K, int64_t Ncap, int64_t Pcap, int Hkv,
             float k[EPL];
             Elem<DT>::widen(raw[u], k);
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) { lo[e] = fminf(lo[e], k[e]); hi[e] = fmaxf(hi[e], k[e]); }
+            for (int e = 0; e < EPL; ++e) { lo[e] = __builtin_elementwise_minimum(lo[e], k[e]); hi[e] = __builtin_elementwise_maximum(hi[e], k[e]); }
         }
     }
 #pragma unroll
     for (int o = LPR; o < kWave; o <<= 1) {
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) { lo[e] = fminf(lo[e], wave_xor(lo[e], o)); hi[e] = fmaxf(hi[e], wave_xor(hi[e], o)); }
+        for (int e = 0; e < EPL; ++e) {
+            lo[e] = __builtin_elementwise_minimum(lo[e], wave_xor(lo[e], o));
+            hi[e] = __builtin_elementwise_maximum(hi[e], wave_xor(hi[e], o));
+        }
     }
     if (rs == 0) {
         char* out = boxes + (head * Pcap + page) * 2 * ROW + c * 16;

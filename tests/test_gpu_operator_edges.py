@@ -103,3 +103,82 @@ def test_an_infinite_key_is_nan_for_the_heads_that_meet_it_with_zero(n, dtype):
         close(out[2:], want[2:], K64, q64, V64, d, f"{n} tokens")
     finally:
         cache.close()
+
+
+def page_order(q, K, n_blocks):
+    """The pages attended, by the definition with NaN: a page whose score is NaN comes before all numbers (equal ones by page)."""
+    d = K.shape[2]
+    lists = []
+    for h in range(K.shape[0]):
+        rows = K[h].astype(np.float64)
+        group = q.reshape(K.shape[0], -1, d)[h].astype(np.float64)
+        score = []
+        for p in range(0, rows.shape[0], 64):
+            lo, hi = rows[p:p + 64].min(0), rows[p:p + 64].max(0)         # (numpy's keep a NaN)
+            with np.errstate(invalid="ignore"):
+                score.append(np.where(group >= 0, group * hi, group * lo).sum(1).max())
+        older = sorted(range(len(score) - 1), key=lambda p: (0 if np.isnan(score[p]) else 1, 0 if np.isnan(score[p]) else -score[p], p))
+        lists.append(sorted(older[:n_blocks - 1] + [len(score) - 1]))
+    return lists
+
+
+@pytest.mark.parametrize("dtype,pages", [(wl.F32, 40), (wl.F16, 40), (wl.BF16, 40), (wl.F16, 1500), (wl.F32, 5000)])
+def test_a_page_of_nan_scores_comes_first(dtype, pages):
+    """A NaN key, a page of nothing but NaN, an infinite edge that a zero of the query meets: the page is attended, and its heads are NaN as in
+    the dense decode; more such pages than are asked for go by their number."""
+    Hq, Hkv, d, n = 4, 2, 32, 64 * pages - 13
+    g = np.random.default_rng(pages)
+    Kf = wl.widen(draw(g, Hkv, n, d, dtype=dtype), dtype).astype(np.float32)
+    qf = wl.widen(draw(g, 1, Hq, d, dtype=dtype), dtype).astype(np.float32)
+    qf[0, 0, 9] = 0.0
+    Kf[0, 64 * 7 + 63, 31] = np.nan                              # one number of one key
+    Kf[0, 64 * 20:64 * 21] = np.nan                              # a whole page
+    Kf[0, 64 * 30 + 5, 9] = np.inf                               # where head 0 has a zero
+    Kf[1, 64 * 11:64 * 12, 4] = np.nan                           # a channel of all keys
+    K = wl.quantize(Kf, dtype) if dtype != wl.BF16 else (Kf.view(np.uint32) >> 16).astype(np.uint16)
+    K32 = wl.widen(K, dtype)
+    q, V = wl.quantize(qf, dtype), draw(g, Hkv, n, d, dtype=dtype)
+    cache = filled(K, V, dtype, Hq, ta.INDEX_BOXES)
+    try:
+        for n_blocks in (1, 2, 3, 4, 6, 25):
+            out, blocks, lse = cache.decode_blocks(0, H.to_torch(q, dtype, DEV), n_blocks)
+            want = page_order(wl.widen(q[0], dtype), K32, n_blocks)
+            assert [list(x) for x in blocks[0].cpu().numpy()] == want, n_blocks
+            assert torch.isnan(out[0, 2:]).all().item() == (n_blocks > 1) and torch.isnan(lse[0, :2]).all().item() == (n_blocks > 1)
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_boxes_keep_a_nan(dtype):
+    """A NaN written by one append is in the box after the next ones, after an eviction that keeps its row, and gone after one that does not."""
+    d, Hkv, cap = 64, 1, 300
+    cache = ta.TopkAttnCache(1, 1, 1, Hkv, d, cap, 8, dtype, index_kind=ta.INDEX_BOXES)
+    try:
+        size = (cap * d * wl.DTYPE_BYTES[dtype] + 255) // 256 * 256
+        boxes = cache.kv[2 * size:2 * size + 5 * 2 * d * wl.DTYPE_BYTES[dtype]].view(cache.torch_dtype()).view(5, 2, d)
+        one = torch.ones((1, Hkv, d), dtype=cache.torch_dtype(), device=DEV)
+        odd = one.clone()
+        odd[0, 0, 17] = float("nan")
+        cache.append(0, 0, one.expand(70, Hkv, d).contiguous(), one.expand(70, Hkv, d).contiguous())
+        cache.append_step(0, odd[None], one[None])
+        for step in range(3):
+            want = torch.zeros((2, d), dtype=torch.bool, device=DEV)
+            want[:, 17] = True
+            assert torch.equal(torch.isnan(boxes[1]), want) and not torch.isnan(boxes[0]).any(), step
+            if step == 0:
+                cache.append_step(0, one[None].expand(1, 20, Hkv, d).contiguous(), one[None].expand(1, 20, Hkv, d).contiguous())
+            else:
+                cache.append_rotary(0, None, one[None], one[None], torch.ones(0, device=DEV))
+        mass = torch.zeros((1, Hkv, cap), device=DEV)
+        mass[0, 0, 70] = 1.0
+        cache.evict(0, mass, 80, 0)                               # (the oldest of equal weights and row 70)
+        assert torch.isnan(boxes[1, :, 17]).all() and not torch.isnan(boxes[0]).any()
+        cache.evict(0, mass, 65, 0)
+        assert cache.length(0, 0) == 65
+        assert torch.isnan(boxes[1, :, 17]).all() and not torch.isnan(boxes[0]).any()
+        mass[0, 0] = torch.arange(cap, 0, -1, device=DEV)         # (row 64 holds the NaN: the lightest)
+        cache.evict(0, mass, 64, 0)
+        assert not torch.isnan(boxes[0]).any()
+    finally:
+        cache.close()
