@@ -4,8 +4,8 @@
 //                       page can have with any of the heads (page_boxes.h)
 //   block_select_kernel the n_blocks - 1 best pages of a key stream and its newest one, ascending
 //
-// Which pages are read is a definite answer: products of 16-bit numbers are exact in 32 bits, products of 32-bit ones in 64, and they are
-// added up in 64 bits, so that only pages equal to 15 digits could change places.
+// Which pages are read is a definite answer: products of two numbers of 32 bits or fewer are exact in 64, whatever their exponents (those of bf16
+// leave the range of 32 bits), and they are added up there, so that only pages equal to 15 digits could change places.
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
@@ -15,13 +15,13 @@
 namespace tka {
 
 // 16 pages per wave, four lanes a page (lane / 16), each with every fourth 16-byte piece of the boxes; the queries of up to 16 heads at a
-// time in LDS.  Bound by d additions in 64 bits (with a choice, a product and a conversion each) per page and head, and the read of the boxes (2 / 64
-// of the keys) close behind: 16384 pages, 8 KV heads, 4 heads each 20 us for 67 MB (3.4 TB/s), 751 pages 6.5.
+// time in LDS, in 64 bits.  Bound by d fused products and sums in 64 bits (with a choice and a conversion each; with products of 16-bit types in 32 bits,
+// which bf16's leave, it took as long) per page and head, and the read of the boxes (2 / 64 of the keys) close behind: 16384 pages, 8 KV heads, 4 heads each 20 us for 67 MB (3.4 TB/s), 751 pages 6.5.
 constexpr int kScoreHeads = 16;
 template <int DT, int D>
 __global__ void __launch_bounds__(256) page_score_kernel(BlockCall a) {
     constexpr int EPL = Elem<DT>::kPerLoad, S = D / (4 * EPL), ROW = D * Elem<DT>::kBytes;
-    __shared__ float qs[kScoreHeads][D];
+    __shared__ double qs[kScoreHeads][D];
     const int lane = lane_id(), j = lane >> 4, m = lane & 15, wave = threadIdx.x >> 6;
     const int kvh = blockIdx.y, b = blockIdx.z;
     const int64_t P = ((int64_t)a.len[b] + 63) / 64;
@@ -54,13 +54,9 @@ __global__ void __launch_bounds__(256) page_score_kernel(BlockCall a) {
                 float l[EPL], h[EPL];
                 Elem<DT>::widen(lo[s], l);
                 Elem<DT>::widen(hi[s], h);
-                const float* qc = &qs[g][(4 * s + j) * EPL];
+                const double* qc = &qs[g][(4 * s + j) * EPL];
 #pragma unroll
-                for (int e = 0; e < EPL; ++e) {
-                    const float w = qc[e], v = w >= 0.f ? h[e] : l[e];
-                    if (DT == DT_F32) sum = fma((double)w, (double)v, sum);
-                    else sum += (double)(w * v);
-                }
+                for (int e = 0; e < EPL; ++e) sum = fma(qc[e], (double)(qc[e] >= 0.0 ? h[e] : l[e]), sum);
             }
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);

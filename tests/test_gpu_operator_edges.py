@@ -182,3 +182,21 @@ def test_the_boxes_keep_a_nan(dtype):
         assert not torch.isnan(boxes[0]).any()
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("dtype", [wl.BF16, wl.F32])
+@pytest.mark.parametrize("q_size,low,high", [(1e30, -30, 30), (1.0, -30, 30), (1e-30, -36, -15)])
+def test_page_scores_beyond_the_range_of_32_bits(dtype, q_size, low, high):
+    """Products of a query and a box edge above 2^128 or below 2^-149: pages are ordered by them all the same."""
+    d, pages, n_blocks = 32, 700, 60
+    n = 64 * pages - 5
+    g = np.random.default_rng(17)
+    size = (10.0 ** g.uniform(low, high, (1, pages, 1))).astype(np.float32) * np.where(g.random((1, pages, 1)) < 0.5, -1, 1).astype(np.float32)
+    K = wl.quantize((size.repeat(64, 1)[:, :n] * g.uniform(0.5, 1.0, (1, 1, d))).astype(np.float32), dtype)
+    q = wl.quantize((q_size * g.uniform(0.5, 1.0, (1, 2, d))).astype(np.float32), dtype)
+    cache = filled(K, draw(g, 1, n, d, dtype=dtype), dtype, 2, ta.INDEX_BOXES)
+    try:
+        _, blocks, _ = cache.decode_blocks(0, H.to_torch(q, dtype, DEV), n_blocks)
+        assert list(blocks[0, 0].cpu().numpy()) == ref.pick_blocks(wl.widen(q[0], dtype), wl.widen(K, dtype), n_blocks)[0]
+    finally:
+        cache.close()
