@@ -61,6 +61,8 @@ __device__ __forceinline__ float max_over_rows(float v) {      // largest of lan
 // fp16 has no numbers below 2^-24, so there the weights are relative to the maximum less 13 powers of two.
 template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
 
+constexpr int kFold = 64;        // steps of a wave whose sums follow each other
+
 // Splits of a sequence of N tokens.
 __device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t N) {
     int64_t pages = (N + 63) / 64;
@@ -166,7 +168,9 @@ __device__ __forceinline__ void join_splits(const AttendCall& a, int64_t head0, 
     else sum_splits<NT, 1>(a, head0, quads, n_split, f, part);
 }
 
-template <int DT, int D, bool LIST, bool MASS>
+// FOLD: for splits of more than kFold steps a wave.  (Shorter ones without the code for it, which takes registers: 32 sequences of 800 to 16384
+// tokens of d = 64 with mass 167 us, 176 with it.)
+template <int DT, int D, bool LIST, bool MASS, bool FOLD>
 __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) attend_kernel(AttendCall a) {
     using Tile = AttendTile<DT, D>;
     constexpr int SUB = Tile::SUB, STEP = Tile::STEP, KEYS = Tile::KEYS, KCH = Tile::KCH, T = Tile::T, ROW = Tile::ROW, EV = Tile::EV;
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     constexpr int NW = 4, NT = NW * kWave, RED = NW * 16 * (D + 4), JOIN = 16 * kMaxSplits + 8 * NT;
     __shared__ __align__(16) float lds[RED > JOIN ? RED : JOIN];
     float (*const red)[16][D + 4] = reinterpret_cast<float (*)[16][D + 4]>(lds);
-    __shared__ float red_m[NW][16], red_l[NW][16];
+    __shared__ float red_m[NW][16], red_l[NW][16], kept_m[NW][kWave], kept_l[NW][kWave];
     __shared__ uint32_t arrived;
     const int lane = lane_id(), j = lane >> 4, n = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -315,12 +319,11 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         const float ref = (m_new == -INFINITY ? 0.f : m_new) - WeightShift<DT>::value;      // (nothing but -inf so far: weights of zero)
         const float alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.f : m_new));
         m = m_new;
-        l *= alpha;
 #pragma unroll
-        for (int e = 0; e < KEYS; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2e, -ref));
-            l += p[e];
-        }
+        for (int e = 0; e < KEYS; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2e, -ref));
+        float step = (p[0] + p[1]) + (p[2] + p[3]);
+        if constexpr (KEYS == 8) step += (p[4] + p[5]) + (p[6] + p[7]);
+        l = fmaf(l, alpha, step);
 #pragma unroll
         for (int c = 0; c < T; ++c) {
 #pragma unroll
@@ -358,6 +361,28 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
             }
         }
     };
+    // Every kFold steps the sums so far are put aside (the weighted one in LDS), and begin again: 32 bits that grow without end round every small
+    // weight the same way (131072 tokens in one split, equal weights below one: 3.1e-5 of their sum before).  A maximum of -inf is the
+    // beginning: the next step's alpha is zero.
+    auto fold = [&](bool first) {
+        int at = lane_id();
+        asm volatile("" : "+v"(at));                           // (addresses worked out here, not kept in registers along the walk)
+        const float m_before = first ? -INFINITY : kept_m[wave][at], l_before = first ? 0.f : kept_l[wave][at];
+        const float top = fmaxf(m_before, m), ref = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(m_before - ref), f_now = __builtin_amdgcn_exp2f(m - ref);
+        kept_m[wave][at] = top;
+        kept_l[wave][at] = fmaf(l_before, f, l * f_now);
+#pragma unroll
+        for (int c = 0; c < T; ++c) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float& x = red[wave][at & 15][Tile::channel(c, 4 * (at >> 4) + r)];
+                x = first ? acc[c][r] * f_now : fmaf(x, f, acc[c][r] * f_now);
+            }
+            __builtin_amdgcn_sched_barrier(0);                 // (four registers at a time)
+        }
+        m = -INFINITY;
+    };
     const int mine = n_steps > wave ? (n_steps - wave + NW - 1) / NW : 0;
     if constexpr (Tile::kPipelined) {
         Tile ta, tb;
@@ -371,6 +396,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
             load(ta, i + 2, ra);
             __builtin_amdgcn_sched_barrier(0);
             use(tb, i + 1, rb_);
+            if (FOLD && (i + 2) % kFold == 0) fold(i + 2 == kFold);
         }
     } else {
         Tile t;
@@ -379,6 +405,18 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
             load(t, i, r);
             __builtin_amdgcn_sched_barrier(0);
             use(t, i, r);
+            if (FOLD && (i + 1) % kFold == 0) fold(i + 1 == kFold);
+        }
+    }
+    if (FOLD && mine >= kFold) {
+        fold(false);
+        m = kept_m[wave][lane];
+        l = kept_l[wave][lane];
+    } else {
+#pragma unroll
+        for (int c = 0; c < T; ++c) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[wave][n][Tile::channel(c, 4 * j + r)] = acc[c][r];
         }
     }
     l = add_lanes_32(add_lanes_16(l));
@@ -387,13 +425,6 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     if (l != l) m = INFINITY;
     // the waves' sums, relative to the largest of their maxima
     if (j == 0) { red_m[wave][n] = m; red_l[wave][n] = l; }
-    if (n < heads) {
-#pragma unroll
-        for (int c = 0; c < T; ++c) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) red[wave][n][Tile::channel(c, 4 * j + r)] = acc[c][r];
-        }
-    }
     __syncthreads();
     const bool whole = a.join_later ? a.n_split == 1 : pages <= a.chunk;        // the sequence's only split (a later join does all or none)
     for (int i = (int)threadIdx.x; i < heads * D; i += NT) {
@@ -490,16 +521,23 @@ __global__ void __launch_bounds__(256) attend_later_kernel(AttendCall a, float s
 
 hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
     const int64_t n_join = attend_join_wgs(a), n_mass = attend_mass_wgs(a);
+    const bool fold = (int64_t)a.chunk * 64 > (int64_t)kFold * 4 * (a.dtype == DT_F32 ? AttendTile<DT_F32, 32>::STEP : AttendTile<DT_F16, 32>::STEP);
+    const dim3 grid((unsigned)attend_walk_wgs(a)), wg(256);
+#define TKA_ATTEND_(DT_, D_, LIST_, MASS_)                                                                              \
+    do {                                                                                                                \
+        if (fold) hipLaunchKernelGGL((attend_kernel<DT_, D_, LIST_, MASS_, true>), grid, wg, 0, st, a);                 \
+        else hipLaunchKernelGGL((attend_kernel<DT_, D_, LIST_, MASS_, false>), grid, wg, 0, st, a);                     \
+    } while (0)
 #define TKA_ATTEND(DT_, D_)                                                                                             \
     do {                                                                                                                \
-        const dim3 grid((unsigned)attend_walk_wgs(a)), wg(256);                                                                     \
-        if (a.list && a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, true>), grid, wg, 0, st, a);             \
-        else if (a.list) hipLaunchKernelGGL((attend_kernel<DT_, D_, true, false>), grid, wg, 0, st, a);                 \
-        else if (a.mass) hipLaunchKernelGGL((attend_kernel<DT_, D_, false, true>), grid, wg, 0, st, a);                 \
-        else hipLaunchKernelGGL((attend_kernel<DT_, D_, false, false>), grid, wg, 0, st, a);                            \
+        if (a.list && a.mass) TKA_ATTEND_(DT_, D_, true, true);                                                         \
+        else if (a.list) TKA_ATTEND_(DT_, D_, true, false);                                                             \
+        else if (a.mass) TKA_ATTEND_(DT_, D_, false, true);                                                             \
+        else TKA_ATTEND_(DT_, D_, false, false);                                                                        \
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_ATTEND, a.dtype, a.D);
 #undef TKA_ATTEND
+#undef TKA_ATTEND_
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || n_join + n_mass == 0) return e;
     hipLaunchKernelGGL(attend_later_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, (int)n_join);

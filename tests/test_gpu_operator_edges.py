@@ -200,3 +200,100 @@ def test_page_scores_beyond_the_range_of_32_bits(dtype, q_size, low, high):
         assert list(blocks[0, 0].cpu().numpy()) == ref.pick_blocks(wl.widen(q[0], dtype), wl.widen(K, dtype), n_blocks)[0]
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("dtype,n,with_mass", [(wl.F16, 131072, False), (wl.BF16, 131072, True), (wl.F32, 65536, False)])
+def test_sums_of_many_equal_weights(dtype, n, with_mass):
+    """As many key streams as there are compute units, so that a sequence is one split: one key above all the others, whose weights
+    are equal and not powers of two.  Added up one after the other in 32 bits such weights round the same way for as long as the sum
+    stays between two powers of two (8192 of them: off by up to 9e-5)."""
+    B, Hkv, G, d = 32, 8, 4, 32
+    cache = ta.TopkAttnCache(1, B, Hkv * G, Hkv, d, n, 8, dtype)
+    try:
+        dt = cache.torch_dtype()
+        K = torch.zeros((Hkv, n, d), dtype=dt, device=DEV)
+        V = torch.zeros((Hkv, n, d), dtype=dt, device=DEV)
+        K[:, 1:, 0] = -1.0
+        V[:, :, 0] = 1.0
+        V[:, :, 1] = ((torch.arange(n, device=DEV) // 64) % 2).to(dt)
+        V[:, 1:, 2] = 1.0
+        for b in range(B):
+            cache.append(0, b, K, V, head_major=True)
+        g = np.random.default_rng(3)
+        q = torch.zeros((B, Hkv * G, d), device=DEV)
+        gap = torch.from_numpy(g.integers(16, 256, (B, Hkv * G)).astype(np.float32) / 32).to(DEV)
+        q[:, :, 0] = gap
+        mass = torch.zeros((B, Hkv, n), device=DEV) if with_mass else None
+        out, lse = cache.decode_dense(0, q.to(dt), mass=mass)
+        w = torch.exp(-gap.double() / np.sqrt(d))
+        total = 1.0 + (n - 1) * w
+        odd = (torch.arange(n) // 64 % 2).sum().item()
+        # a weight: the exponent's rounding, up to 2^4 in fp16 (8 u), its factor's (2 u of at most 3), the exponential (2 u), the parts (4 u);
+        # a sum: 64 steps of a wave, the larger sums of those (n / 2048 of fp32 at most), steps, lanes, waves (16), an addition each
+        weight, sums = 16 * U, (64 + n / 2048 + 16) * U
+        assert ((lse.double() - total.log()).abs() <= weight + sums + 3 * U * total.log()).all(), (lse.double() - total.log()).abs().max()
+        # of the weighted sum, whose steps are up to 8 roundings of the sum each
+        for c, want in ((0, torch.ones_like(w)), (1, odd * w / total), (2, (n - 1) * w / total)):
+            off = ((out[:, :, c].double() - want).abs() / want).max().item()
+            assert off <= 2 * weight + 8 * sums, f"channel {c}: off by {off:.3g}, {2 * weight + 8 * sums:.3g} allowed"
+        assert (out[:, :, 3:] == 0).all()
+        if with_mass:
+            want = (w / total).view(B, Hkv, G).sum(2)
+            assert ((mass[:, :, -1].double() - want).abs() <= (weight + sums + 20 * U * total.log().max()) * want).all()
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n_blocks", [0, 290])
+def test_long_splits_of_changing_scores(dtype, n_blocks):
+    """Splits of thousands of keys, dense and over lists of pages, with weights: scores that rise, fall and begin with thousands of -inf, so that
+    what a wave has put aside is rescaled in every way; lengths that end within and right after its first steps."""
+    B, Hkv, G, d, cap = 32, 8, 2, 32, 20001
+    lens = [cap - 331 * b for b in range(B - 3)] + [8192, 8193, 4097]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    cache = ta.TopkAttnCache(1, B, Hkv * G, Hkv, d, cap, 8, dtype, index_kind=ta.INDEX_BOXES if n_blocks else ta.INDEX_NONE)
+    try:
+        dt = cache.torch_dtype()
+        q = torch.randn((B, Hkv * G, d), generator=g, device=DEV)
+        q[:, :, 0] = 1.0
+        q, q_in = q.to(dt).double(), q.to(dt)
+        K = torch.randn((Hkv, cap, d), generator=g, device=DEV)
+        ramp = torch.linspace(0, 60, cap, device=DEV)
+        K[0, :, 0], K[1, :, 0], K[2, :, 0] = ramp, -ramp, 30 * torch.sin(ramp)
+        K[3, :9000, 0] = -float("inf")
+        V = torch.randn((Hkv, cap, d), generator=g, device=DEV).to(dt)
+        K = K.to(dt)
+        for b, n in enumerate(lens):
+            cache.append(0, b, K[:, :n].contiguous(), V[:, :n].contiguous(), head_major=True)
+        mass = torch.zeros((B, Hkv, cap), device=DEV)
+        if n_blocks:
+            out, blocks, lse = cache.decode_blocks(0, q_in, n_blocks, mass=mass)
+        else:
+            out, lse = cache.decode_dense(0, q_in, mass=mass)
+        A = 0.0
+        for b in (0, 5, 17, B - 3, B - 2, B - 1):
+            n = lens[b]
+            finite = torch.nan_to_num(K[:, :n].double(), neginf=0.0)
+            A = torch.matmul(finite.abs(), q[b].abs().view(Hkv, G, d).transpose(1, 2).contiguous()).max().item() / np.sqrt(d)
+            s = torch.matmul(K[:, :n].double(), q[b].view(Hkv, G, d).transpose(1, 2).contiguous()) / np.sqrt(d)          # [Hkv, n, G]
+            if n_blocks:
+                held = torch.zeros((Hkv, (n + 63) // 64), dtype=torch.bool, device=DEV)
+                for h in range(Hkv):
+                    held[h, blocks[b, h][blocks[b, h] >= 0].long()] = True
+                s = torch.where(held.repeat_interleave(64, 1)[:, :n, None], s, -float("inf"))
+            w = torch.softmax(s, 1)
+            want = torch.matmul(w.transpose(1, 2).contiguous(), V[:, :n].double()).view(Hkv * G, d)
+            dw = (d + 6) * U * A + 4 * U + 2.0 ** -18 + (n / 16 + 64) * U
+            live = torch.isfinite(want).all(1)                   # (a head whose keys are all of -inf has no result)
+            assert live.sum() >= (Hkv - 1) * G
+            off = (out[b].double() - want)[live].abs().max().item()
+            assert off <= 2 * dw * V.abs().max().item(), f"sequence {b}: off by {off:.3g}"
+            want = torch.logsumexp(s, 1).view(Hkv * G)
+            assert ((lse[b].double() - want)[live].abs() <= dw + 4 * U * want[live].abs()).all()
+            m, live = w.sum(2), live.view(Hkv, G).all(1)
+            assert ((mass[b, :, :n].double() - m)[live].abs() <= (2 * dw + 200 * U) * m[live] + 1e-37).all()
+            assert (mass[b, :, n:] == 0).all()
+    finally:
+        cache.close()
