@@ -63,11 +63,16 @@ template <int DT> struct WeightShift { static constexpr float value = DT == DT_F
 
 constexpr int kFold = 64;        // steps of a wave whose sums follow each other
 
-// Splits of a sequence of N tokens.
-__device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t N) {
-    int64_t pages = (N + 63) / 64;
-    if (a.list && a.n_list < pages) pages = a.n_list;
-    return (int)((pages + a.chunk - 1) / a.chunk);
+// Pages of a sequence of N tokens that are attended, and their splits: no more than the launch has.  (A recorded call may be replayed after the
+// sequence has grown, though its contract says otherwise: the last split then takes what there is, and the splits that are waited for are
+// those that come.)
+__device__ __forceinline__ int64_t attend_pages(const AttendCall& a, int64_t N) {
+    const int64_t pages = (N + 63) / 64;
+    return a.list && a.n_list < pages ? a.n_list : pages;
+}
+__device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t pages) {
+    const int64_t splits = (pages + a.chunk - 1) / a.chunk;
+    return (int)(splits < a.n_split ? splits : a.n_split);
 }
 // What the splits leave is read by a workgroup of the same launch, maybe on another XCD: written and read past the caches that are not shared.
 __device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -199,11 +204,10 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     if (stream < 0) stream += streams;
     const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
     const int64_t N = a.len[b];
-    const int64_t pages_b = (N + 63) / 64;
-    const int64_t pages = LIST ? (a.n_list < pages_b ? a.n_list : pages_b) : pages_b;
-    const int64_t p0 = (int64_t)split * a.chunk;
-    if (p0 >= pages) return;                                  // (the join knows how many splits a sequence has)
-    const int64_t p1 = p0 + a.chunk < pages ? p0 + a.chunk : pages;
+    const int64_t pages = attend_pages(a, N);
+    const int ns = attend_splits(a, pages);
+    if (split >= ns) return;                                  // (the join knows how many splits a sequence has)
+    const int64_t p0 = (int64_t)split * a.chunk, p1 = split + 1 < ns ? p0 + a.chunk : pages;
     const int n_steps = (int)(p1 - p0) * SPP;
     const int heads = a.G - 16 * rb < 16 ? a.G - 16 * rb : 16;
     const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G + 16 * rb;
@@ -426,7 +430,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     // the waves' sums, relative to the largest of their maxima
     if (j == 0) { red_m[wave][n] = m; red_l[wave][n] = l; }
     __syncthreads();
-    const bool whole = a.join_later ? a.n_split == 1 : pages <= a.chunk;        // the sequence's only split (a later join does all or none)
+    const bool whole = a.join_later ? a.n_split == 1 : ns == 1;        // the sequence's only split (a later join does all or none)
     for (int i = (int)threadIdx.x; i < heads * D; i += NT) {
         const int h = i / D, c = i - h * D;
         float top = -INFINITY;
@@ -457,7 +461,6 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     uint32_t* const counter = a.arrive + (int64_t)stream * a.row_blocks + rb;
     if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    const int ns = (int)((pages + a.chunk - 1) / a.chunk);
     if (arrived + 1u != (uint32_t)ns) return;
     if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     join_splits<NT>(a, head0, heads, ns, WeightShift<DT>::value, lds, reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits));
@@ -474,7 +477,7 @@ __global__ void __launch_bounds__(256) attend_later_kernel(AttendCall a, float s
     if ((int)blockIdx.x < n_join) {
         const int blocks = a.join_heads == 1 ? a.G : a.row_blocks, group = (int)blockIdx.x / blocks, in = (int)blockIdx.x - group * blocks;
         const int left = a.G - in * a.join_heads, heads = left < a.join_heads ? left : a.join_heads;
-        join_splits<256>(a, (int64_t)group * a.G + in * a.join_heads, heads, attend_splits(a, a.len[group / a.Hkv]), shift, f, sums);
+        join_splits<256>(a, (int64_t)group * a.G + in * a.join_heads, heads, attend_splits(a, attend_pages(a, a.len[group / a.Hkv])), shift, f, sums);
         return;
     }
     const int per_stream = (int)((a.walk + kMassPerBlock - 1) / kMassPerBlock);
@@ -482,10 +485,10 @@ __global__ void __launch_bounds__(256) attend_later_kernel(AttendCall a, float s
     const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
     const int64_t N = a.len[b];
     const int64_t i0 = (int64_t)part * kMassPerBlock;
-    const int64_t pages_b = (N + 63) / 64, pages = a.list && a.n_list < pages_b ? a.n_list : pages_b;
+    const int64_t pages = attend_pages(a, N);
     if (i0 >= pages * 64) return;
     const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G;
-    const int ns = attend_splits(a, N);
+    const int ns = attend_splits(a, pages);
     for (int g = wave; g < a.G; g += 4) {
         const float v = head_log2_sum(a, head0 + g, ns, shift, nullptr);
         if (lane_id() == 0) lg[g] = v;

@@ -297,3 +297,44 @@ def test_long_splits_of_changing_scores(dtype, n_blocks):
             assert (mass[b, :, n:] == 0).all()
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("with_mass", [False, True])
+@pytest.mark.parametrize("n,Hq", [(100, 4), (700, 4), (700, 64), (3000, 4)])
+def test_a_replay_after_the_cache_has_grown_leaves_the_handle_sound(n, Hq, with_mass):
+    """A decode recorded at n tokens and replayed at 40000, which its contract rules out: nothing waits for splits that the recorded launch does
+    not have, and later calls give what they gave before."""
+    Hkv, d, cap = 2, 64, 40000
+    g = np.random.default_rng(n)
+    K, V = draw(g, Hkv, cap, d, dtype=wl.F16), draw(g, Hkv, cap, d, dtype=wl.F16)
+    q = draw(g, 1, Hq, d, dtype=wl.F16)
+    cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, cap, 8, wl.F16)
+    try:
+        up = lambda x: H.to_torch(np.ascontiguousarray(x), wl.F16, DEV)
+        cache.append(0, 0, up(K[:, :n]), up(V[:, :n]), head_major=True)
+        qt = up(q)
+        mass = torch.zeros((1, Hkv, cap), device=DEV) if with_mass else None
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            first = cache.decode_dense(0, qt, mass=mass)[0]
+        torch.cuda.current_stream().wait_stream(s)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got, got_lse = cache.decode_dense(0, qt, mass=mass)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, first)
+        cache.append(0, 0, up(K[:, n:]), up(V[:, n:]), head_major=True)
+        want, want_lse = cache.decode_dense(0, qt)
+        for _ in range(3):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert (got - want).abs().max() < 1e-4 and (got_lse - want_lse).abs().max() < 1e-4
+            again, again_lse = cache.decode_dense(0, qt)
+            assert torch.equal(again, want) and torch.equal(again_lse, want_lse)
+        counted = torch.zeros((1, Hkv, cap), device=DEV)
+        cache.decode_dense(0, qt, mass=counted)
+        assert abs(counted.sum().item() - Hq) < 1e-2
+    finally:
+        cache.close()
