@@ -212,10 +212,11 @@ int topk_attn_decode(topk_attn_t* h, int layer, const void* q, int k, float* out
  * library: a device array of TOPK_ATTN_STATIC_SCRATCH_BYTES that every GPU the library runs on
  * holds until the process ends.  Only the cache lengths are still read from the handle's
  * workspace.  The call allocates and frees nothing and enqueues kernels only.
- * Limit: ESCRATCH (nothing enqueued) if topk_attn_workspace_bytes(cfg) minus the share of the
- * lengths (n_layers * n_seqs * 4, rounded up to 256) and of the dense decode's counters (4 bytes per sequence and 16 heads
- * of a KV head, rounded up) exceeds TOPK_ATTN_STATIC_SCRATCH_BYTES -- one
- * Llama-8B-shaped layer of 128k tokens at k = 2048 fits, a million-token layer does not.
+ * Limit: ESCRATCH (nothing enqueued) if topk_attn_workspace_bytes(cfg) minus what a top-k decode has no
+ * use for there exceeds TOPK_ATTN_STATIC_SCRATCH_BYTES: the lengths (n_layers * n_seqs * 4 bytes, rounded
+ * up to 256), the dense decode's counters (4 bytes per sequence and 16 heads of a KV head, rounded up) and,
+ * with a block index, its page scores and lists (8 and 4 bytes per sequence, KV head and page, each
+ * rounded up).  One Llama-8B-shaped layer of 128k tokens at k = 2048 fits, a million-token layer does not.
  * All calls on one GPU, from whatever handle, share the one array: the call clears the words
  * that must start at zero itself, and two such calls that overlap in time on one GPU race. */
 #define TOPK_ATTN_STATIC_SCRATCH_BYTES ((size_t)96 << 20)

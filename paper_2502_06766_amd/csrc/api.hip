@@ -752,7 +752,8 @@ struct Call {
 static int plan_call(topk_attn_t* h, int layer, const void* q, int n_queries, int causal, int k, int window,
                      float* out, int32_t* idx, float* vals, float* lse, bool use_static, Call* call) {
     if (!h || !q || !out) return TOPK_ATTN_EINVAL;
-    if (use_static && h->ws_one.total - h->ws_one.thr > kStaticScratchBytes) return TOPK_ATTN_ESCRATCH;
+    // (behind the per-call arrays: what only the block-sparse decode uses)
+    if (use_static && h->ws_one.block_score - h->ws_one.thr > kStaticScratchBytes) return TOPK_ATTN_ESCRATCH;
     if (layer < 0 || layer >= h->cfg.n_layers) return TOPK_ATTN_EINVAL;
     if (k < 1 || k > h->cfg.max_k) return TOPK_ATTN_EINVAL;
     if (window < 0 || window > h->cfg.max_window) return TOPK_ATTN_EINVAL;

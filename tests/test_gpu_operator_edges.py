@@ -338,3 +338,29 @@ def test_a_replay_after_the_cache_has_grown_leaves_the_handle_sound(n, Hq, with_
         assert abs(counted.sum().item() - Hq) < 1e-2
     finally:
         cache.close()
+
+
+def test_static_scratch_does_not_count_what_only_the_block_decode_uses():
+    """The top-k decode through the built-in scratch, on a handle whose workspace exceeds it by the block index's page scores and lists alone."""
+    Hq, Hkv, d, k = 1, 1, 32, 64
+    limit = 96 << 20
+    cfg = lambda cap, index: ta.make_config(1, 1, Hq, Hkv, d, cap, k, ta.F16, index_kind=index)
+    lo, hi = 1 << 10, 1 << 26
+    while hi - lo > 1:                                            # the longest cache that fits without a block index
+        mid = (lo + hi) // 2
+        lo, hi = (mid, hi) if ta.topk_attn_workspace_bytes(cfg(mid, ta.INDEX_NONE)) - 512 <= limit else (lo, mid)
+    assert ta.topk_attn_workspace_bytes(cfg(lo, ta.INDEX_BOXES)) - 512 > limit
+    cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, lo, k, wl.F16, index_kind=ta.INDEX_BOXES)
+    try:
+        g = np.random.default_rng(1)
+        kv = H.to_torch(draw(g, Hkv, 5000, d, dtype=wl.F16), wl.F16, DEV)
+        cache.append(0, 0, kv, kv, head_major=True)
+        q = H.to_torch(draw(g, 1, Hq, d, dtype=wl.F16), wl.F16, DEV)
+        want = cache.decode(0, q, k)[0]
+        out = torch.empty_like(want)
+        st = torch.cuda.current_stream().cuda_stream
+        assert ta.lib().topk_attn_decode_static(cache.h, 0, q.data_ptr(), k, out.data_ptr(), None, None, None, st) == ta.OK
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    finally:
+        cache.close()
