@@ -277,7 +277,7 @@ int topk_attn_decode_blocks(topk_attn_t* h, int layer, const void* q, int n_bloc
 /* The same accumulation from what a top-k decode of the layer returned: mass[b][h / G][idx] += exp(vals / sqrt(d) - lse) for the k entries of
  * every head (idx, vals [B, Hq, k], lse [B, Hq]; the positions of a head are distinct; entries with idx < 0 or >= max_tokens are passed over).
  * With a recent-token window lse covers the window too, whose tokens are not among idx.  No atomics: the same call gives the same bits.
- * Errors: EINVAL (null, layer range, k < 1), EUNSUPPORTED (2^22 or more sequences times KV heads). */
+ * Errors: EINVAL (null, layer range, k < 1 or > 2^28), EUNSUPPORTED (2^22 or more sequences times KV heads). */
 int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const float* vals, const float* lse, int k, float* mass,
                        void* hip_stream);
 

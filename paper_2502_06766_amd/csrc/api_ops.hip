@@ -176,6 +176,7 @@ int topk_attn_decode_blocks(topk_attn_t* h, int layer, const void* q, int n_bloc
 int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const float* vals, const float* lse, int k, float* mass,
                        void* hip_stream) {
     if (!h || !idx || !vals || !lse || !mass || layer < 0 || layer >= h->cfg.n_layers || k < 1) return TOPK_ATTN_EINVAL;
+    if (k > kMostSelected) return TOPK_ATTN_EINVAL;                  // (no decode has more; the kernel counts up to k + 4096 in 32 bits)
     const topk_attn_config& c = h->cfg;
     if ((int64_t)c.n_seqs * c.n_kv_heads > kMostStreams) return TOPK_ATTN_EUNSUPPORTED;
     const DeviceOf device(h);

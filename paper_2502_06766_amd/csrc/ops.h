@@ -8,6 +8,8 @@ namespace tka {
 constexpr int64_t kMostWorkgroups = (1 << 24) - 1;     // of 256
 constexpr int64_t kMostStreams = (1 << 22) - 1;        // one workgroup of 1024 each
 
+constexpr int kMostSelected = 1 << 28;                 // the largest max_k of a handle
+
 constexpr int kMaxSplits = 256;  // splits of a sequence (their factors sit in LDS when they are joined)
 
 // Attention of one query per sequence and head over all cached tokens, or over a list of pages of 64 tokens.
