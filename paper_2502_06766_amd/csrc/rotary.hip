@@ -26,6 +26,9 @@ __device__ __forceinline__ u32x4 pack_row(const float* f) {
     return r;
 }
 
+// Sums of squares that a row is scaled for: above the one infinity is near, below the other squares of its numbers lose bits.
+constexpr float kLargeSquares = 0x1p+120f, kSmallSquares = 0x1p-80f;
+
 // A workgroup per token.  D e / 16 lanes hold a row (a head of the token); a channel's partner, which lies in another lane when halves
 // are paired, comes through LDS.  The angle is pos * inv_freq in 64 bits, reduced to a fraction of a turn there: in 32 bits a position of
 // 10^6 leaves 0.06 radian of error.
@@ -82,7 +85,17 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryCall a) {
 #pragma unroll
                     for (int e = 0; e < EPL; ++e) ss = fmaf(x[e], x[e], ss);
                     ss = group_reduce<AddOp, LPR>(ss);
-                    const float inv = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+                    float eps = a.eps;
+                    if (DT != DT_F16 && (ss > kLargeSquares || (ss < kSmallSquares && eps < kSmallSquares))) {
+                        // squares beyond 32 bits: of the row times a power of two
+                        const float s = ss > kLargeSquares ? 0x1p-80f : 0x1p+90f;
+                        ss = 0.f;
+#pragma unroll
+                        for (int e = 0; e < EPL; ++e) { x[e] *= s; ss = fmaf(x[e], x[e], ss); }
+                        ss = group_reduce<AddOp, LPR>(ss);
+                        eps = eps * s * s;
+                    }
+                    const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
 #pragma unroll
                     for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * (is_q ? qw[e] : kw[e]);
                 }

@@ -364,3 +364,29 @@ def test_static_scratch_does_not_count_what_only_the_block_decode_uses():
         assert torch.equal(out, want)
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("size", [1e25, 3e38, 1e-22, 1e-30, 1e-37])
+@pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
+def test_norms_of_rows_whose_squares_leave_32_bits(dtype, size):
+    """Rows of very large and very small numbers, without and with an eps of their own size: normalised as the formula says."""
+    Hq, Hkv, d, n = 4, 2, 64, 5
+    g = np.random.default_rng(11)
+    x = wl.quantize((size * g.uniform(-1, 1, (1, n, Hq + 2 * Hkv, d))).astype(np.float32), dtype)
+    w = wl.quantize(g.uniform(0.5, 2.0, d).astype(np.float32), dtype)
+    freq = (10000.0 ** (-np.arange(d // 2) / (d // 2))).astype(np.float32)
+    t, wt = H.to_torch(x, dtype, DEV), H.to_torch(w, dtype, DEV)
+    half_step = {wl.F32: 2.0 ** -24, wl.BF16: 2.0 ** -8}[dtype]
+    for eps in (0.0, 1e-40, 1e-6):
+        cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, n, 8, dtype)
+        try:
+            out = cache.append_rotary(0, t[:, :, :Hq], t[:, :, Hq:Hq + Hkv], t[:, :, Hq + Hkv:], torch.from_numpy(freq).to(DEV), q_norm=wt,
+                                      k_norm=wt, eps=eps)
+            want = ref.rms_rotate(wl.widen(x[0, :, :Hq], dtype), wl.widen(w, dtype), np.float32(eps), np.arange(n), freq, False)
+            got = out[0].double().cpu().numpy()
+            # as for ordinary rows (the norm's sum, root, quotient and products, the turn), and half a step of the smallest numbers of 32 bits
+            r = np.sqrt(want ** 2 + np.abs(want).max(-1, keepdims=True) ** 2)
+            tol = (d / 2 + 24) * U * r + half_step * np.abs(want) * 1.01 + 2.0 ** -126
+            assert (np.abs(got - want) <= tol).all(), f"eps {eps}: off by {np.abs(got - want).max():.3g} of {np.abs(want).max():.3g}"
+        finally:
+            cache.close()
