@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import helpers as H
+import operator_bounds as ob
 from oracle import operators_ref as ref
 from paper_2502_06766_amd import topk_attn as ta
 from paper_2502_06766_amd import workloads as wl
@@ -390,3 +391,57 @@ def test_norms_of_rows_whose_squares_leave_32_bits(dtype, size):
             assert (np.abs(got - want) <= tol).all(), f"eps {eps}: off by {np.abs(got - want).max():.3g} of {np.abs(want).max():.3g}"
         finally:
             cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_every_weight_to_its_last_bits(dtype):
+    """64 keys of exact scores, the value of key c one in channel c: the outputs are the weights themselves."""
+    d, n, Hq = 64, 64, 4
+    q1, k1 = ob.grid_scores(np.random.default_rng(0), Hq, n)
+    q, K = np.zeros((1, Hq, d), np.float32), np.zeros((1, n, d), np.float32)
+    q[0, :, 0], K[0, :, 0] = q1, k1
+    cache = filled(wl.quantize(K, dtype), wl.quantize(np.eye(n, d, dtype=np.float32)[None], dtype), dtype, Hq)
+    try:
+        out, _ = cache.decode_dense(0, H.to_torch(wl.quantize(q, dtype), dtype, DEV))
+        w = np.exp(q1[:, None].astype(np.float64) * k1 / np.sqrt(d))
+        want = w / w.sum(1, keepdims=True)
+        # additions of a sum: three in a step, one to the steps before, two of lanes, four of waves
+        off = (np.abs(out[0].double().cpu().numpy() - want) / want).max()
+        assert off <= ob.quotient_bound(dtype, 10), f"off by {off:.3g}, {ob.quotient_bound(dtype, 10):.3g} allowed"
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype,n,blocks", [(wl.F16, 70001, 0), (wl.BF16, 40007, 0), (wl.F32, 30001, 0), (wl.F16, 700, 0), (wl.BF16, 700, 11),
+                                            (wl.F32, 130, 0), (wl.F16, 30001, 200), (wl.F32, 20003, 150)])
+def test_every_stretch_of_the_cache_shows(dtype, n, blocks):
+    """The values of each 64th of the cache are one in a channel of its own: a stretch that is lost, counted twice or joined with another one's
+    factor shows in that channel."""
+    d, Hq, Hkv = 64, 8, 2
+    g = np.random.default_rng(n)
+    q, K, V = np.zeros((1, Hq, d), np.float32), np.zeros((Hkv, n, d), np.float32), np.zeros((Hkv, n, d), np.float32)
+    part = np.arange(n) * d // n
+    V[:, np.arange(n), part] = 1.0
+    k1 = []
+    for h in range(Hkv):
+        q[0, 4 * h:4 * h + 4, 0], k = ob.grid_scores(g, 4, n)
+        K[h, :, 0] = k
+        k1.append(k.astype(np.float64))
+    cache = filled(wl.quantize(K, dtype), wl.quantize(V, dtype), dtype, Hq, ta.INDEX_BOXES if blocks else ta.INDEX_NONE)
+    try:
+        qt = H.to_torch(wl.quantize(q, dtype), dtype, DEV)
+        at = [np.arange(n)] * Hkv
+        if blocks:
+            out, pages, _ = cache.decode_blocks(0, qt, blocks)
+            at = ref.block_tokens([[p for p in x if p >= 0] for x in pages[0].cpu().numpy()], n)
+        else:
+            out, _ = cache.decode_dense(0, qt)
+        out = out[0].double().cpu().numpy()
+        # (16 steps of a wave at most here, each up to 8 roundings of each of three parts' sums; 64 splits in each of four sums, and the join)
+        bound = ob.quotient_bound(dtype, 16 * 24 + 64 + 10)
+        for h in range(Hq):
+            w = np.exp(q[0, h, 0] * k1[h // 4][at[h // 4]] / np.sqrt(d))
+            want = np.bincount(part[at[h // 4]], w, minlength=d) / w.sum()
+            assert (np.abs(out[h] - want) <= bound * want).all(), f"head {h}: off by {(np.abs(out[h] - want) / want.clip(1e-9)).max():.3g}"
+    finally:
+        cache.close()

@@ -2,8 +2,10 @@
 import os
 import subprocess
 
+import numpy as np
 import pytest
 
+import operator_bounds as ob
 import test_sanitizers_cpu as san
 from paper_2502_06766_amd import build as hip_build
 
@@ -28,3 +30,17 @@ def test_selections_longer_than_any_decode_has_are_refused(tmp_path):
     r = subprocess.run([exe], env=env, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, f"{r.stdout[-2000:]}\n{r.stderr[-4000:]}"
     assert "mass driver: all checks passed" in r.stdout
+
+
+@pytest.mark.parametrize("dtype,enough", [(ob.F16, 2), (ob.BF16, 3)])
+def test_the_bound_of_the_weights_tells_their_parts(dtype, enough):
+    """Weights in one part fewer than the kernel takes (and, in bf16, in two fewer) exceed the bound that the GPU test holds; those it takes do not."""
+    g = np.random.default_rng(0)
+    q, k = ob.grid_scores(g, 4, 64)
+    w = np.exp2(q[:, None].astype(np.float64) * k * (np.log2(np.e) / 8))
+    exact = w / w.sum(1, keepdims=True)
+    w32 = w.astype(np.float32)
+    for parts in range(1, enough + 1):
+        got = ob.in_parts(w32, dtype, parts) / w32.astype(np.float64).sum(1, keepdims=True)
+        off = (np.abs(got - exact) / exact).max()
+        assert (off <= ob.quotient_bound(dtype, 10)) == (parts == enough), (parts, off, ob.quotient_bound(dtype, 10))
