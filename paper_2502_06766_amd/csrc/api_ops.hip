@@ -60,6 +60,9 @@ T* scratch_at(const topk_attn* h, size_t offset) { return reinterpret_cast<T*>(s
 // One sequence of 500 / 1000 / 2000 / 16384 / 131072 tokens takes 8.3 / 8.8 / 9.6 / 17.8 / 93 us with 8 (one split), 2, 2, 8 and 64 pages a
 // workgroup; with 2, 16 (one split), 16, 4 and 32 pages 8.7 / 12.5 / 15.5 / 21.8 / 99.  24 sequences of 400 to 8192 tokens, 64 heads: 103 / 92 / 92
 // / 84 / 113 with 4 / 8 / 16 / 32 / 64 pages; 5 of 1600 to 32768: 80 / 75 / 73 / 76 / 107.
+// Rows of 512 and 1024 bytes (d = 256, single-buffered) against the best of 2, 8, 16, 32 and 64 pages: 16 bits, 500 / 4000 / 16000 / 128000 tokens 10.5 /
+// 14.7 / 28.4 / 181 and 10.5 / 14.7 / 28.4 / 178, 12 sequences of 400 to 8192 91 and 85; fp32, 500 / 4000 / 16000 / 64000 17.1 / 22.6 / 72.7 / 182
+// and the same, 6 sequences 141 and 120.
 int64_t pages_per_split(const int64_t* pages, int n, double weight, int64_t longest, int64_t max_splits, int n_cu, double row_bytes) {
     double best = 1e30, all = 0.0;
     int64_t chunk = longest;                                 // (max_splits >= 1)
@@ -89,9 +92,13 @@ int64_t pages_per_split(const int64_t* pages, int n, double weight, int64_t long
     return chunk;
 }
 // Beyond this many bytes of a head block's partial sums the one workgroup that would put them together takes longer than a launch that has a
-// workgroup per head: 8 heads, 32 splits (128 KB) of 128k tokens 95 us joined in the walk's launch, 98 after it; 16 heads, 252 splits (2 MB) of
-// 64k tokens 45 and 18.
-constexpr int64_t kJoinBytes = 192 << 10;
+// workgroup per head.  One sequence of 4k / 16k / 64k tokens, d = 128, joined in the walk's launch and after it, in us:
+//   64 KB (32 splits of the 4 heads of 8 KV heads)  11.3 / 17.9 / 58.0 and 10.3 / 18.1 / 60.3
+//   80 KB (5 heads)                                 12.7 / 19.2 / 66.7 and 10.4 / 18.5 / 67.2
+//   128 KB (8 heads)                                13.5 / 19.8 / 66.3 and 10.9 / 18.9 / 62.8
+//   256 to 728 KB (16 heads, one KV head)           16.3 / 19.4 / 30.1 and 11.7 / 14.8 / 18.5
+// (32 KB, four sequences, 8 heads to each of 8 KV heads, 8 splits: 18.1 and 18.8 of 4k tokens, 52.6 and 53.7 of 16k.)
+constexpr int64_t kJoinBytes = 64 << 10;
 
 int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* out, int32_t* blocks, float* lse, float* mass,
                void* hip_stream) {
