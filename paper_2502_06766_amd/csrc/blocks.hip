@@ -9,7 +9,6 @@
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
-#include "page_boxes.h"
 #include "team.h"
 
 namespace tka {

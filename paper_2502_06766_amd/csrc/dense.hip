@@ -10,7 +10,6 @@
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
-#include "page_boxes.h"
 #include "scan_tiles.h"
 
 namespace tka {

@@ -4,6 +4,17 @@
 
 namespace tka {
 
+// CALL(DT, D) for the handle's type and head dimension.
+#define TKA_BY_TYPE_AND_DIM(CALL, dtype, D)                                                                                \
+    do {                                                                                                                   \
+        if ((dtype) == DT_F16) { if ((D) == 32) CALL(DT_F16, 32); else if ((D) == 64) CALL(DT_F16, 64);                     \
+                                 else if ((D) == 128) CALL(DT_F16, 128); else CALL(DT_F16, 256); }                         \
+        else if ((dtype) == DT_BF16) { if ((D) == 32) CALL(DT_BF16, 32); else if ((D) == 64) CALL(DT_BF16, 64);             \
+                                       else if ((D) == 128) CALL(DT_BF16, 128); else CALL(DT_BF16, 256); }                 \
+        else { if ((D) == 32) CALL(DT_F32, 32); else if ((D) == 64) CALL(DT_F32, 64);                                       \
+               else if ((D) == 128) CALL(DT_F32, 128); else CALL(DT_F32, 256); }                                           \
+    } while (0)
+
 // A launch has fewer than 2^32 threads.
 constexpr int64_t kMostWorkgroups = (1 << 24) - 1;     // of 256
 constexpr int64_t kMostStreams = (1 << 22) - 1;        // one workgroup of 1024 each

@@ -4,6 +4,7 @@
 #pragma once
 #include "device_utils.h"
 #include "internal.h"
+#include "ops.h"
 
 namespace tka {
 
@@ -74,17 +75,6 @@ page_box_kernel(const char* __restrict__ K, int64_t Ncap, int64_t Pcap, int Hkv,
         *reinterpret_cast<u32x4*>(out + ROW) = u32x4{z[0], z[1], z[2], z[3]};
     }
 }
-
-// Calls KERNEL<DT, D> for the handle's type and head dimension.
-#define TKA_BY_TYPE_AND_DIM(CALL, dtype, D)                                                                                \
-    do {                                                                                                                   \
-        if ((dtype) == DT_F16) { if ((D) == 32) CALL(DT_F16, 32); else if ((D) == 64) CALL(DT_F16, 64);                     \
-                                 else if ((D) == 128) CALL(DT_F16, 128); else CALL(DT_F16, 256); }                         \
-        else if ((dtype) == DT_BF16) { if ((D) == 32) CALL(DT_BF16, 32); else if ((D) == 64) CALL(DT_BF16, 64);             \
-                                       else if ((D) == 128) CALL(DT_BF16, 128); else CALL(DT_BF16, 256); }                 \
-        else { if ((D) == 32) CALL(DT_F32, 32); else if ((D) == 64) CALL(DT_F32, 64);                                       \
-               else if ((D) == 128) CALL(DT_F32, 128); else CALL(DT_F32, 256); }                                           \
-    } while (0)
 
 // n_new < 0: the boxes of `max_rows` = -n_new rows at most, as many as the device lengths say.
 inline hipError_t launch_page_boxes(int dtype, int D, const void* K, int64_t Ncap, int64_t Pcap, int Hkv, int B, const int32_t* len_dev,

@@ -4,7 +4,6 @@
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
-#include "page_boxes.h"
 
 namespace tka {
 
