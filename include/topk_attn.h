@@ -1,7 +1,7 @@
 /*
  * topk_attn.h -- C ABI of the MI355X (gfx950) top-k attention decode library.
  *
- * The library implements one operator: the per-step "top-k attention" decode of
+ * The library's main operator is the per-step "top-k attention" decode of
  * arXiv 2502.06766 (Methodology, "Top-k Attention: Accelerating Decoding", and
  * Algorithm 1 "Top-k KV Cache Decoding") in its exact-search form, with the whole
  * KV cache resident in GPU memory.  For every query head it
@@ -13,6 +13,8 @@
  *      step over the retrieved rows).
  * With grouped-query attention, query head h reads KV head h / (n_q_heads /
  * n_kv_heads); every query head selects its own k positions.
+ * Around it stand appends that normalise and rotate what they store, dense and block-sparse
+ * decodes, the accumulated attention weight of the cached tokens, and eviction by it.
  *
  * All pointers named "device" are GPU addresses on the configured device; the
  * library never allocates or frees device memory, never synchronises the device
@@ -290,7 +292,8 @@ int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const floa
  * Rows are numbered by their place in the cache from then on (idx, windows, causal chunks); a window or `recent` still means the newest
  * tokens.  Not to be replayed from a HIP graph (the lengths' host copy changes).
  * Errors: EINVAL (null h/mass, layer range, budget < 1, budget > max_tokens, recent outside 0 .. budget), ENOMEM (the workspace has no room for
- * a word per 64 KB of rows: budgets of tens of millions of tokens), EUNSUPPORTED (2^22 or more sequences times KV heads). */
+ * a word per 64 KB of rows: where no two query heads share a KV head, budgets from about a million tokens with rows of 1 KB or four million with
+ * rows of 256 bytes; with G of them G times as many), EUNSUPPORTED (2^22 or more sequences times KV heads). */
 int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int64_t recent, int32_t* kept, void* hip_stream);
 
 /* Host-only helper for the paper's layer-wise settings of k ("Layer-Wise Settings for k":

@@ -57,8 +57,8 @@ T* scratch_at(const topk_attn* h, size_t offset) { return reinterpret_cast<T*>(s
 //   - a page takes a workgroup 0.5 on an empty chip and 1.42 with one on every compute unit (5.9 TB/s), between them as the root of their number;
 //   - more workgroups than compute units take whole rounds if all are alike, else their share of the work and a part of one at the end;
 //   - a workgroup costs 1 in itself, 1.7 where others follow it, putting splits together 3.2, and 0.05 a split.
-// One sequence of 500 / 1000 / 2000 / 16384 / 131072 tokens takes 8.3 / 8.8 / 9.6 / 17.8 / 93 us with 8 (one split), 2, 2, 8 and 64 pages a
-// workgroup; with 2, 16 (one split), 16, 4 and 32 pages 8.7 / 12.5 / 15.5 / 21.8 / 99.  24 sequences of 400 to 8192 tokens, 64 heads: 103 / 92 / 92
+// One sequence of 500 / 1000 / 2000 / 16384 / 131072 tokens takes 8.5 / 9.0 / 9.8 / 18.0 / 93.6 us with 8 (one split), 2, 2, 8 and 64 pages a
+// workgroup; with 2, 16 (one split), 16, 2 and 32 pages 8.8 / 12.7 / 16.0 / 21.8 / 97.3.  24 sequences of 400 to 8192 tokens, 64 heads: 105 / 92 / 92
 // / 84 / 113 with 4 / 8 / 16 / 32 / 64 pages; 5 of 1600 to 32768: 80 / 75 / 73 / 76 / 107.
 // Rows of 512 and 1024 bytes (d = 256, single-buffered) against the best of 2, 8, 16, 32 and 64 pages: 16 bits, 500 / 4000 / 16000 / 128000 tokens 10.5 /
 // 14.7 / 28.4 / 181 and 10.5 / 14.7 / 28.4 / 178, 12 sequences of 400 to 8192 91 and 85; fp32, 500 / 4000 / 16000 / 64000 17.1 / 22.6 / 72.7 / 182

@@ -15,7 +15,8 @@ namespace tka {
 
 // 16 pages per wave, four lanes a page (lane / 16), each with every fourth 16-byte piece of the boxes; the queries of up to 16 heads at a
 // time in LDS, in 64 bits.  Bound by d fused products and sums in 64 bits (with a choice and a conversion each; with products of 16-bit types in 32 bits,
-// which bf16's leave, it took as long) per page and head, and the read of the boxes (2 / 64 of the keys) close behind: 16384 pages, 8 KV heads, 4 heads each 20 us for 67 MB (3.4 TB/s), 751 pages 6.5.
+// which bf16's leave, it took as long) per page and head, and the read of the boxes (2 / 64 of the keys) close behind: 16384 pages, 8 KV heads, 4 heads
+// each 20 us for 67 MB (3.4 TB/s), 751 pages 6.3.
 constexpr int kScoreHeads = 16;
 template <int DT, int D>
 __global__ void __launch_bounds__(256) page_score_kernel(BlockCall a) {
@@ -75,7 +76,7 @@ __device__ __forceinline__ uint64_t ord_of(double v) {
 // One workgroup per key stream.  The page that ends the selection (its score, and among equal scores its number: lower ones first) is
 // found from a linear histogram between the smallest and the largest score, whose one bin in question is ranked by direct comparison,
 // or, where that bin is crowded or the scores are not finite, byte by byte of their ordered bits.  Then the pages up to it are written in
-// their order.  A wave has a stretch of the pages, 64 neighbouring ones at a time; up to 16 a thread stay in registers (16384 pages, a million tokens: 13 us; 37 us
+// their order.  A wave has a stretch of the pages, 64 neighbouring ones at a time; up to 16 a thread stay in registers (16384 pages, a million tokens: 14 us; 37 us
 // when each of the five passes reads them again), and beyond they are read again.
 constexpr int kPickThreads = 1024, kPickBins = 1024, kPickList = 2048, kPickHeld = 16;
 struct PickShared {

@@ -6,7 +6,7 @@
 //   attend_later_kernel with `mass`: the splits put together there, and the weights of the keys added up; also for many splits of many heads
 //
 // Bound by the read of K and V: 16 384 bytes per 32 keys and KV head against 24 (fp16) or 32 (bf16) MFMA (d = 128), a tenth of the time the read takes.
-// A million tokens, 8 KV heads: 708 us (6.06 TB/s, what plain reads reach); 128k tokens 93 us a call; 500 tokens 8.5 us, all latency.
+// A million tokens, 8 KV heads: 716 us (6.0 TB/s; plain reads reach 6.0 to 6.1); 128k tokens 94 us a call; 500 tokens 8.8 us, all latency.
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
@@ -55,9 +55,10 @@ __device__ __forceinline__ float max_over_rows(float v) {      // largest of lan
 }
 
 // Weights of 16-bit caches are the operand of an MFMA and go in as parts, each the rounding to the type of what the ones before it left: two of
-// fp16 (22 bits of each weight) and three of bf16 (all 24).  (One part alone: errors of 2^-9 of a weight; two of bf16: 2^-18, three times the error
-// that the sums' roundings make; the third costs nothing that shows: the MFMA of a step take a tenth of the time its rows do.)
-// fp16 has no numbers below 2^-24, so there the weights are relative to the maximum less 13 powers of two.
+// fp16 (to 2^-22 of a weight, half of what the rounding of its exponent leaves) and three of bf16 (to 2^-24).  (One part of fp16 alone: 2^-11 of a
+// weight; two of bf16: 2^-16; bf16's third costs nothing that shows: the MFMA of a step take a tenth of the time its rows do.)
+// fp16 has no numbers below 2^-24, so there the weights are relative to the maximum less 13 powers of two: one below 2^-16 of the maximum is off by
+// 2^-38 of that at most.
 template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
 
 constexpr int kFold = 64;        // steps of a wave whose sums follow each other

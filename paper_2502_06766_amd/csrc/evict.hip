@@ -19,8 +19,8 @@ constexpr uint32_t kZeroMass = 0x80000000u;      // of zero: tokens no query has
 // The weight of the last survivor is found from the top of the keys' bits: 11 of them by a histogram in LDS, then 11 and 10 more among the keys
 // that share the ones before (or, where at most 512 keys do after the first, those compared with each other); then the survivors are written
 // in order, a stretch of the cache per wave.  One workgroup has up to 16384 tokens of a key stream in its registers and does it all
-// (8065 tokens 12 us).  Longer streams are cut into up to eight chunks and take a launch per step, each workgroup adding up the chunks'
-// histograms of the step before for itself (32 streams of 5k to 100k tokens: 84 us in one
+// (8065 tokens 13 us).  Longer streams are cut into up to eight chunks and take a launch per step, each workgroup adding up the chunks'
+// histograms of the step before for itself (32 streams of 19k to 100k tokens: 84 us in one
 // workgroup each, 32 in four launches); chunks of more than 16384 tokens are read again by each step.
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave, kEvictList = 512, kEvictHeld = 16;
 constexpr int kEvictCopies = 4;       // of a histogram, for every fourth lane one (16384 tokens of 80 different bins 9.2 -> 6.5 us), 16 banks apart
@@ -266,8 +266,8 @@ __global__ void __launch_bounds__(kEvictThreads) evict_step_kernel(EvictCall a) 
 // counter, so those before a unit are always in the hands of a workgroup that runs or has run: every wait ends.  (A counter a stream, and the
 // streams in turn, so that the units before one were handed out some time ago: one counter, stream after stream, took 131 us where this takes
 // 117.)  Flags carry no data (the rows themselves were written by earlier launches), so they need no more than the loads' return in front of them.
-// One read and one write of the rows that move; through a buffer it would be two of each.  32 streams cut to 16384 tokens (537 MB): 117 us, 4.6 TB/s
-// (a large copy reaches 4.8).
+// One read and one write of the rows that move; through a buffer it would be two of each.  32 streams cut to 16384 tokens (537 MB): 117 to 121
+// us, 4.4 to 4.6 TB/s (a large copy reaches 4.8).
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictCall a) {
     __shared__ uint32_t ticket;
     const int64_t stream = blockIdx.x % (uint32_t)(a.B * a.Hkv);
@@ -332,7 +332,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictCall a) {
 }
 
 // One workgroup per key stream takes its heads one after the other (the positions of a head are distinct), so the sums come out the
-// same in every run: a chain of trips to memory, two a head.  256 positions of 32 heads 5.9 us, 16 sequences of 1024 positions 11.
+// same in every run: a chain of trips to memory, two a head.  256 positions of 32 heads 5.9 us, 16 sequences of 1024 positions 11; 16384
+// positions of 32 heads over 8, of a million tokens, 145 a call: 8 workgroups, 4 heads one after the other.
 constexpr int kMassThreads = 1024;
 __global__ void __launch_bounds__(kMassThreads) add_mass_kernel(MassCall a) {
     const int64_t stream = blockIdx.x;
