@@ -13,8 +13,9 @@
  *      step over the retrieved rows).
  * With grouped-query attention, query head h reads KV head h / (n_q_heads /
  * n_kv_heads); every query head selects its own k positions.
- * Around it stand appends that normalise and rotate what they store, dense and block-sparse
- * decodes, the accumulated attention weight of the cached tokens, and eviction by it.
+ * Around it stand appends that normalise and rotate what they store, dense, windowed and block-sparse
+ * decodes, attention of the tokens of a prompt, the accumulated attention weight of the cached tokens, eviction by it, and a
+ * cache of its own whose rows are held in 8 bits (topk_attn_coded_*).
  *
  * All pointers named "device" are GPU addresses on the configured device; the
  * library never allocates or frees device memory, never synchronises the device
@@ -265,6 +266,23 @@ int topk_attn_decode_multi(topk_attn_t* h, int layer, const void* q, int n_queri
  * sequences times KV heads, or a call of 2^24 or more workgroups).  An infinity among the values of attended tokens may come out as NaN. */
 int topk_attn_decode_dense(topk_attn_t* h, int layer, const void* q, float* out, float* lse, float* mass, void* hip_stream);
 
+/* The same over the first `sinks` tokens and the newest `window` ones (at least 1: the new token's own), for layers with a sliding window: a token t
+ * of N is attended if t < sinks or t >= N - window.  Nothing else is read.  Sequences of at most sinks + window tokens are attended whole, and
+ * where all are, the result is topk_attn_decode_dense's bit for bit.  Replays as there.  Errors as there; EINVAL if sinks < 0 or window < 1. */
+int topk_attn_decode_sinks(topk_attn_t* h, int layer, const void* q, int64_t sinks, int64_t window, float* out, float* lse, void* hip_stream);
+
+/* Attention of the last n_queries cached tokens of a sequence, each over what it sees: query m is the token at p = N - n_queries + m and attends the
+ * tokens t <= p with t < sinks or t > p - window (window >= N: all up to its own).  A whole prompt after its append, a chunk of one, or drafted tokens.
+ *   q    device [S, n_queries, Hq, d] in the cache dtype, 16-byte aligned (S: sequences of the call)
+ *   out  device [S, n_queries, Hq, d] in the cache dtype, 16-byte aligned;  lse  device [S, n_queries, Hq] fp32 or NULL
+ * seq: one sequence of the layer, or -1: all B of them (their lengths may differ).  Softmax statistics and sums are held in 32 bits; the weights of
+ * 16-bit caches are rounded to the cache dtype once, as the output is.  What a token does not see (NaN and infinities too) has no effect on its output.
+ * n_queries == 0 is a no-op.  Replays as topk_attn_decode_dense.
+ * Errors: EINVAL (null h/q/out, range, misaligned, n_queries < 0 or beyond a sequence's length, sinks < 0, window < 1), EUNSUPPORTED (2^24 or more
+ * workgroups: 128 rows of queries times heads of a group each; 2^31 or more rows of a KV head). */
+int topk_attn_prompt(topk_attn_t* h, int layer, int seq, const void* q, int64_t n_queries, int64_t sinks, int64_t window, void* out, float* lse,
+                     void* hip_stream);
+
 /* Block-sparse attention of one new token per sequence: for every sequence and KV head the n_blocks best pages of 64 tokens, each
  * attended whole by the heads of the group.  A page's score is the largest raw score any key in its box (TOPK_ATTN_INDEX_BOXES) could
  * have with any of the group's heads, max_h sum_c max(q_hc lo_c, q_hc hi_c), in 64 bits; ties go to the lower page.  A page of which any head's
@@ -324,6 +342,66 @@ int topk_attn_k_schedule(int64_t total_k, int n_layers, double last_over_first, 
 int topk_attn_decode_layers(topk_attn_t* h, int layer0, int n_layers, const void* q, const int32_t* k,
                             int window, float* out, int32_t* idx, float* vals, float* lse,
                             void* hip_stream);
+
+/* ---- A cache whose rows are held in 8 bits -------------------------------------------------------------------------------
+ * Half the room and half the reading of a 16-bit cache.  64 consecutive tokens of a KV head are a block.  A block that is full is held as one byte per
+ * element and two scales, one for its keys and one for its values; the rows behind the last full block are held as they came.  A block is coded once, when
+ * its last row arrives, so what the cache holds does not depend on how the rows were handed over.  With amax the largest magnitude of a block's keys (or values):
+ *   INT8  scale = amax / 127 rounded to 32 bits and then to 16 significant ones (down, where 127 scale would overflow); code = the integer nearest to x / scale, ties to even: within scale / 2
+ *   E4M3  scale = the smallest power of two with amax <= 448 scale; code = x / scale rounded to e4m3 (4 exponent bits, 3 of fraction): within 2^-4 of x, and
+ *         within 2^-10 scale where x is below 2^-6 scale.  For rows with a few channels far above the others.
+ * A row reads as code * scale, in 32 bits or more; amax below 2^-100 reads as zeros; a block with a NaN or an infinity reads as NaN, all of it.
+ * The handle is one of its own beside topk_attn_t, with the same rules: caller-owned memory, nothing allocated or synchronised after create, calls on a handle must not
+ * overlap, argument errors leave it unchanged, appends and resets are not to be replayed from a HIP graph. */
+typedef struct topk_attn_coded topk_attn_coded_t;
+enum { TOPK_ATTN_CODED_INT8 = 0, TOPK_ATTN_CODED_E4M3 = 1 };
+typedef struct {
+    uint32_t struct_size;   /* sizeof(topk_attn_coded_config) */
+    int32_t n_layers, n_seqs, n_q_heads, n_kv_heads;    /* as in topk_attn_config; Hq/Hkv <= 128 */
+    int32_t head_dim;       /* 32, 64, 128 or 256 */
+    int64_t max_tokens;     /* capacity per (layer, sequence) */
+    int32_t dtype;          /* TOPK_ATTN_F32 / F16 / BF16: queries, rows handed over and read back */
+    int32_t format;         /* TOPK_ATTN_CODED_* */
+    int32_t device;
+    int32_t reserved;       /* 0 */
+    void* kv_storage;       /* device, >= topk_attn_coded_kv_bytes(), 256-byte aligned, caller-owned */
+    size_t kv_bytes;
+    void* workspace;        /* device, >= topk_attn_coded_workspace_bytes(), 256-byte aligned, caller-owned */
+    size_t workspace_bytes;
+} topk_attn_coded_config;
+
+/* Storage (codes, scales, 64 rows per key stream in `dtype`) and scratch of the configuration; 0 on an invalid one. */
+size_t topk_attn_coded_kv_bytes(const topk_attn_coded_config* cfg);
+size_t topk_attn_coded_workspace_bytes(const topk_attn_coded_config* cfg);
+/* Errors of create: EINVAL, EUNSUPPORTED (head_dim, dtype, format, head grouping, 2^22 or more sequences times KV heads), ENOMEM, EDEVICE. */
+int topk_attn_coded_create(const topk_attn_coded_config* cfg, topk_attn_coded_t** out);
+int topk_attn_coded_destroy(topk_attn_coded_t* h);
+
+/* Append n_new tokens to sequence `seq` of `layer`, or to each of its sequences (seq = -1): element (s, t, h, c) of the call's s-th sequence at
+ * base[s * seq_stride + t * token_stride + h * head_stride + c] in `dtype` (strides in elements, rows 16-byte aligned, in any order: parts of a fused projection or another
+ * cache's heads).  Errors: EINVAL (null, range, misaligned, a negative stride), ECAPACITY (nothing is enqueued then), EUNSUPPORTED (2^24 or more workgroups: two per 64 tokens
+ * and KV head).  n_new == 0 is a no-op. */
+int topk_attn_coded_append(topk_attn_coded_t* h, int layer, int seq, const void* k_new, const void* v_new, int64_t n_new,
+                           int64_t seq_stride, int64_t token_stride, int64_t head_stride, void* hip_stream);
+
+/* Read rows [first, first + n) of sequence `seq` (or of every sequence, -1) back in `dtype`: the values they stand for, rounded once, laid out by strides as in
+ * topk_attn_coded_append.  Errors: EINVAL (also a range beyond a sequence's length), EUNSUPPORTED as there.  n == 0 is a no-op. */
+int topk_attn_coded_read(topk_attn_coded_t* h, int layer, int seq, int64_t first, int64_t n, void* k_out, void* v_out,
+                         int64_t seq_stride, int64_t token_stride, int64_t head_stride, void* hip_stream);
+
+/* topk_attn_decode_sinks over the rows as they read (products and sums of code * scale in 32 bits, not rounded to `dtype`): one new token per sequence, window >= N for all tokens.
+ *   q device [B, Hq, d] in `dtype`, 16-byte aligned; out device [B, Hq, d] fp32; lse device [B, Hq] fp32 or NULL
+ * Errors: EINVAL (null, range, misaligned, sinks < 0, window < 1, a sequence with no tokens), EUNSUPPORTED (2^24 or more workgroups). */
+int topk_attn_coded_decode(topk_attn_coded_t* h, int layer, const void* q, int64_t sinks, int64_t window, float* out, float* lse,
+                           void* hip_stream);
+
+/* topk_attn_prompt over the rows as they read: the same arguments, masks, output types and errors. */
+int topk_attn_coded_prompt(topk_attn_coded_t* h, int layer, int seq, const void* q, int64_t n_queries, int64_t sinks, int64_t window, void* out,
+                           float* lse, void* hip_stream);
+
+/* Tokens of (layer, seq), -1 on bad arguments; forget those of a sequence or (seq = -1) of all of the layer's. */
+int64_t topk_attn_coded_length(const topk_attn_coded_t* h, int layer, int seq);
+int topk_attn_coded_reset(topk_attn_coded_t* h, int layer, int seq, void* hip_stream);
 
 /* Scale beta in (0, 1] of the page radius in the bound q . c + beta |q| r that decides which pages the
  * key scan of TOPK_ATTN_PATH_PAGES reads.  1 (the default) is exact.  Below 1 fewer pages are read and a

@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtopk_attn.so")
 SOURCES = ["api.hip", "scan.hip", "select.hip", "gather.hip", "attend.hip", "index8.hip", "tail.hip", "pages.hip",
-           "api_ops.hip", "dense.hip", "blocks.hip", "rotary.hip", "evict.hip"]
+           "api_ops.hip", "dense.hip", "blocks.hip", "rotary.hip", "evict.hip",
+           "api_prompt.hip", "api_coded.hip", "coded_store.hip", "coded_decode.hip", "prompt.hip", "coded_prompt.hip"]
 # measurement program of its own (streaming-read ceiling over launch shapes), built beside the library
 PROBE_SRC = "read_probe_sweep.hip"
 PROBE = os.path.join(OBJ_DIR, "read_probe_sweep")

@@ -8,100 +8,17 @@
 #include "../../include/topk_attn.h"
 #include "handle.h"
 #include "internal.h"
+#include "layer.h"
 #include "ops.h"
 #include "page_boxes.h"
+#include "split_plan.h"
 
 using namespace tka;
 
 namespace {
 
-// The handle's device, current while the call enqueues.
-class DeviceOf {
-  public:
-    explicit DeviceOf(const topk_attn* h) {
-        ok_ = hipGetDevice(&before_) == hipSuccess && (before_ == h->cfg.device || hipSetDevice(h->cfg.device) == hipSuccess);
-        changed_ = ok_ && before_ != h->cfg.device;
-    }
-    ~DeviceOf() { if (changed_) (void)hipSetDevice(before_); }
-    bool ok() const { return ok_; }
-  private:
-    int before_ = 0;
-    bool ok_ = false, changed_ = false;
-};
-
-// Where a layer's arrays lie.
-struct Layer {
-    int64_t row, head;              // bytes of a row, and of a key stream's rows
-    char *K, *V;
-    int32_t* len;
-    char* index;                    // behind K and V, all layers
-    int64_t stream0;                // key streams of the layers before
-};
-Layer layer_of(const topk_attn* h, int layer) {
-    const topk_attn_config& c = h->cfg;
-    Layer l;
-    l.row = (int64_t)c.head_dim * elem_bytes(c.dtype);
-    l.head = c.max_tokens * l.row;
-    l.stream0 = (int64_t)layer * c.n_seqs * c.n_kv_heads;
-    l.K = static_cast<char*>(c.kv_storage) + l.stream0 * l.head;
-    l.V = l.K + h->kv_half;
-    l.len = reinterpret_cast<int32_t*>(static_cast<char*>(c.workspace) + h->ws.len) + (size_t)layer * c.n_seqs;
-    l.index = static_cast<char*>(c.kv_storage) + 2 * h->kv_half;
-    return l;
-}
-template <class T>
-T* scratch_at(const topk_attn* h, size_t offset) { return reinterpret_cast<T*>(static_cast<char*>(h->cfg.workspace) + offset); }
-
-// Pages that one workgroup of the walk takes: the split with the least estimated time.  The estimate, in microseconds, for key streams of
-// pages[i] pages (each standing for `weight` streams), from measurements with 8 KV heads of d = 128 in 16 bits (32 KB a page):
-//   - a page takes a workgroup 0.5 on an empty chip and 1.42 with one on every compute unit (5.9 TB/s), between them as the root of their number;
-//   - more workgroups than compute units take whole rounds if all are alike, else their share of the work and a part of one at the end;
-//   - a workgroup costs 1 in itself, 1.7 where others follow it, putting splits together 3.2, and 0.05 a split.
-// One sequence of 500 / 1000 / 2000 / 16384 / 131072 tokens takes 8.5 / 9.0 / 9.8 / 18.0 / 93.6 us with 8 (one split), 2, 2, 8 and 64 pages a
-// workgroup; with 2, 16 (one split), 16, 2 and 32 pages 8.8 / 12.7 / 16.0 / 21.8 / 97.3.  24 sequences of 400 to 8192 tokens, 64 heads: 105 / 92 / 92
-// / 84 / 113 with 4 / 8 / 16 / 32 / 64 pages; 5 of 1600 to 32768: 80 / 75 / 73 / 76 / 107.
-// Rows of 512 and 1024 bytes (d = 256, single-buffered) against the best of 2, 8, 16, 32 and 64 pages: 16 bits, 500 / 4000 / 16000 / 128000 tokens 10.5 /
-// 14.7 / 28.4 / 181 and 10.5 / 14.7 / 28.4 / 178, 12 sequences of 400 to 8192 91 and 85; fp32, 500 / 4000 / 16000 / 64000 17.1 / 22.6 / 72.7 / 182
-// and the same, 6 sequences 141 and 120.
-int64_t pages_per_split(const int64_t* pages, int n, double weight, int64_t longest, int64_t max_splits, int n_cu, double row_bytes) {
-    double best = 1e30, all = 0.0;
-    int64_t chunk = longest;                                 // (max_splits >= 1)
-    const double scale = row_bytes / 256.0;
-    for (int i = 0; i < n; ++i) all += (double)pages[i];
-    all *= weight / n_cu;
-    const auto consider = [&](int64_t splits) {              // of the longest sequence
-        const int64_t c = std::max<int64_t>(2, (longest + splits - 1) / splits);
-        double wgs = 0.0;
-        const float inv = 1.0f / (float)c;
-        for (int i = 0; i < n; ++i) wgs += (double)(int64_t)((float)(pages[i] + c - 1) * inv);
-        wgs *= weight / n_cu;                                // to a compute unit
-        double cost = splits > 1 ? 3.2 + 0.05 * (double)splits : 0.0;
-        if (wgs <= 1.0) cost += 1.0 + scale * (double)c * std::max(0.5, 1.42 * sqrt(wgs));
-        else cost += 1.7 * wgs + scale * 1.42 * std::min(ceil(wgs) * (double)c, all + 0.25 * (double)c);
-        if (cost < best) { best = cost; chunk = c; }
-    };
-    // powers of two, one number between each two of them, and what fills whole rounds if all sequences are as long
-    for (int64_t k = 1; k <= max_splits && k <= longest; k *= 2) {
-        consider(k);
-        if (k >= 2 && k + k / 2 <= max_splits) consider(k + k / 2);
-    }
-    for (int r = 1; r <= 4; ++r) {
-        const int64_t k = (int64_t)(r * n_cu / (n * weight));
-        if (k >= 1 && k <= max_splits) consider(k);
-    }
-    return chunk;
-}
-// Beyond this many bytes of a head block's partial sums the one workgroup that would put them together takes longer than a launch that has a
-// workgroup per head.  One sequence of 4k / 16k / 64k tokens, d = 128, joined in the walk's launch and after it, in us:
-//   64 KB (32 splits of the 4 heads of 8 KV heads)  11.3 / 17.9 / 58.0 and 10.3 / 18.1 / 60.3
-//   80 KB (5 heads)                                 12.7 / 19.2 / 66.7 and 10.4 / 18.5 / 67.2
-//   128 KB (8 heads)                                13.5 / 19.8 / 66.3 and 10.9 / 18.9 / 62.8
-//   256 to 728 KB (16 heads, one KV head)           16.3 / 19.4 / 30.1 and 11.7 / 14.8 / 18.5
-// (32 KB, four sequences, 8 heads to each of 8 KV heads, 8 splits: 18.1 and 18.8 of 4k tokens, 52.6 and 53.7 of 16k.)
-constexpr int64_t kJoinBytes = 64 << 10;
-
 int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* out, int32_t* blocks, float* lse, float* mass,
-               void* hip_stream) {
+               void* hip_stream, int64_t sinks = 0, int64_t window = 0) {
     const topk_attn_config& c = h->cfg;
     if ((int64_t)c.n_seqs * c.n_kv_heads > kMostStreams) return TOPK_ATTN_EUNSUPPORTED;
     const Layer l = layer_of(h, layer);
@@ -111,7 +28,7 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
         if (n < 1) return TOPK_ATTN_EINVAL;
         longest = std::max(longest, n);
     }
-    const DeviceOf device(h);
+    const DeviceOf device(h->cfg.device);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     hipStream_t st = (hipStream_t)hip_stream;
     int64_t pages = (longest + 63) / 64;
@@ -121,6 +38,13 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     a.Ncap = c.max_tokens;
     const bool some = n_blocks && pages > n_blocks;              // (a sequence of at most n_blocks pages is attended whole)
     if (some) pages = n_blocks;
+    // (sequences that are seen whole: as the dense decode)
+    if (window && WindowWalk(longest, sinks, window).first > 0) {
+        a.sinks = sinks; a.window = window;
+        pages = WindowWalk(longest, sinks, window).pages();
+        for (int b = 0; b < c.n_seqs; ++b)               // (a shorter sequence may have more pages: its sinks and its window meet)
+            pages = std::max(pages, WindowWalk(h->len[(size_t)layer * c.n_seqs + b], sinks, window).pages());
+    }
     a.walk = pages * 64;
     a.score_stride = c.max_tokens;               // (of a list: whole pages, one less than the cache has at least)
     a.scores = scratch_at<float>(h, h->ws.scores);
@@ -132,7 +56,7 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     const int n_sample = std::min(c.n_seqs, 16);
     for (int i = 0; i < n_sample; ++i) {
         const int64_t n = h->len[(size_t)layer * c.n_seqs + (size_t)((int64_t)i * c.n_seqs / n_sample)];
-        sample[i] = std::min((n + 63) / 64, pages);
+        sample[i] = std::min(a.window ? WindowWalk(n, sinks, window).pages() : (n + 63) / 64, pages);
     }
     a.chunk = (int)pages_per_split(sample, n_sample, (double)c.n_seqs / n_sample * a.Hkv * a.row_blocks, pages, max_splits, h->n_cu,
                                    (double)l.row);
@@ -173,6 +97,12 @@ int topk_attn_decode_dense(topk_attn_t* h, int layer, const void* q, float* out,
     return decode_all(h, layer, q, 0, out, nullptr, lse, mass, hip_stream);
 }
 
+int topk_attn_decode_sinks(topk_attn_t* h, int layer, const void* q, int64_t sinks, int64_t window, float* out, float* lse, void* hip_stream) {
+    if (!h || !q || !out || layer < 0 || layer >= h->cfg.n_layers || ((uintptr_t)q & 15)) return TOPK_ATTN_EINVAL;
+    if (sinks < 0 || window < 1) return TOPK_ATTN_EINVAL;
+    return decode_all(h, layer, q, 0, out, nullptr, lse, nullptr, hip_stream, sinks, window);
+}
+
 int topk_attn_decode_blocks(topk_attn_t* h, int layer, const void* q, int n_blocks, float* out, int32_t* blocks, float* lse, float* mass,
                             void* hip_stream) {
     if (!h || !q || !out || layer < 0 || layer >= h->cfg.n_layers || ((uintptr_t)q & 15)) return TOPK_ATTN_EINVAL;
@@ -186,7 +116,7 @@ int topk_attn_add_mass(topk_attn_t* h, int layer, const int32_t* idx, const floa
     if (k > kMostSelected) return TOPK_ATTN_EINVAL;                  // (no decode has more; the kernel counts up to k + 4096 in 32 bits)
     const topk_attn_config& c = h->cfg;
     if ((int64_t)c.n_seqs * c.n_kv_heads > kMostStreams) return TOPK_ATTN_EUNSUPPORTED;
-    const DeviceOf device(h);
+    const DeviceOf device(h->cfg.device);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     MassCall a{};
     a.idx = idx; a.vals = vals; a.lse = lse; a.mass = mass; a.Ncap = c.max_tokens;
@@ -234,7 +164,7 @@ int topk_attn_evict(topk_attn_t* h, int layer, float* mass, int64_t budget, int6
     a.state = take(streams * (a.units + 1));
     a.old_len = reinterpret_cast<int32_t*>(take(c.n_seqs));
     if (words * 4 > (size_t)c.n_seqs * c.n_q_heads * h->ws.cand_cap * sizeof(uint64_t)) return TOPK_ATTN_ENOMEM;
-    const DeviceOf device(h);
+    const DeviceOf device(h->cfg.device);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     hipStream_t st = (hipStream_t)hip_stream;
     const hipError_t e = launch_evict(a, st);
@@ -280,7 +210,7 @@ int topk_attn_append_rotary(topk_attn_t* h, int layer, int seq, const topk_attn_
     for (int b = 0; b < B; ++b)
         if (r->n_new > c.max_tokens - h->len[slot + b]) return TOPK_ATTN_ECAPACITY;
     if ((int64_t)B * r->n_new > kMostWorkgroups) return TOPK_ATTN_EUNSUPPORTED;
-    const DeviceOf device(h);
+    const DeviceOf device(h->cfg.device);
     if (!device.ok()) return TOPK_ATTN_EDEVICE;
     hipStream_t st = (hipStream_t)hip_stream;
     const Layer l = layer_of(h, layer);

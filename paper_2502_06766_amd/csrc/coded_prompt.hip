@@ -1,0 +1,27 @@
+// Attention of the tokens of a prompt over the 8-bit cache (prompt.h has the kernel).
+#include "prompt.h"
+
+namespace tka {
+
+hipError_t launch_prompt_coded(const PromptCall& a, hipStream_t st) {
+    const dim3 grid((unsigned)((int64_t)a.S * a.Hkv * a.n_split * a.row_blocks));
+#define TKA_PROMPT_(DT_, FMT_, D_)                                                                                        \
+    do {                                                                                                                  \
+        if (a.block_rows == 32) hipLaunchKernelGGL((prompt_kernel<DT_, FMT_, D_, 1, 1>), grid, dim3(64), 0, st, a);       \
+        else if (a.block_rows == 128) hipLaunchKernelGGL((prompt_kernel<DT_, FMT_, D_, 4, 1>), grid, dim3(256), 0, st, a); \
+        else if constexpr (DT_ != DT_F32 && D_ <= 128) hipLaunchKernelGGL((prompt_kernel<DT_, FMT_, D_, 4, 2>), grid, dim3(256), 0, st, a); \
+        else return hipErrorInvalidValue;                                                                                 \
+    } while (0)
+#define TKA_PROMPT(DT_, D_)                                                                                               \
+    do {                                                                                                                  \
+        if (a.format == CODED_INT8) TKA_PROMPT_(DT_, CODED_INT8, D_);                                                     \
+        else TKA_PROMPT_(DT_, CODED_E4M3, D_);                                                                            \
+    } while (0)
+    TKA_BY_TYPE_AND_DIM(TKA_PROMPT, a.dtype, a.D);
+#undef TKA_PROMPT
+#undef TKA_PROMPT_
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.n_split == 1 ? e : launch_prompt_join(a, st);
+}
+
+}  // namespace tka

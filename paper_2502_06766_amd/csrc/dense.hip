@@ -11,6 +11,7 @@
 #include "internal.h"
 #include "ops.h"
 #include "scan_tiles.h"
+#include "split_join.h"
 
 namespace tka {
 
@@ -61,12 +62,15 @@ __device__ __forceinline__ float max_over_rows(float v) {      // largest of lan
 // 2^-38 of that at most.
 template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
 
+constexpr int kWalkAll = 0, kWalkList = 1, kWalkWindow = 2;        // what is attended: all tokens, a list of pages, the first and the newest ones
+
 constexpr int kFold = 64;        // steps of a wave whose sums follow each other
 
 // Pages of a sequence of N tokens that are attended, and their splits: no more than the launch has.  (A recorded call may be replayed after the
 // sequence has grown, though its contract says otherwise: the last split then takes what there is, and the splits that are waited for are
 // those that come.)
 __device__ __forceinline__ int64_t attend_pages(const AttendCall& a, int64_t N) {
+    if (a.window) return WindowWalk(N, a.sinks, a.window).pages();
     const int64_t pages = (N + 63) / 64;
     return a.list && a.n_list < pages ? a.n_list : pages;
 }
@@ -74,110 +78,12 @@ __device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t pages)
     const int64_t splits = (pages + a.chunk - 1) / a.chunk;
     return (int)(splits < a.n_split ? splits : a.n_split);
 }
-// What the splits leave is read by a workgroup of the same launch, maybe on another XCD: written and read past the caches that are not shared.
-__device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float2 get2(const float* p) {
-    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-// log2 of the sum of a head's weights (not shifted), over its splits; one wave.  `f` (or null) gets the factor of each split's weighted sum.
-__device__ __forceinline__ float head_log2_sum(const AttendCall& a, int64_t bh, int n_split, float shift, float* f) {
-    const float* lm = a.part_lm + bh * a.n_split * 2;
-    constexpr int U = kMaxSplits / kWave;
-    float2 v[U];
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int i = u * kWave + lane_id();
-        v[u] = make_float2(0.f, -INFINITY);
-        if (u * kWave < n_split && i < n_split) v[u] = get2(lm + 2 * i);
-        top = fmaxf(top, v[u].y);
-    }
-    top = wave_max(top);
-    float sum = 0.f;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        v[u].y = v[u].y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(v[u].y - top);     // (nothing but -inf: no part in the sum)
-        if (v[u].y != 0.f) sum = fmaf(v[u].y, v[u].x, sum);
-    }
-    sum = group_reduce<AddOp, 64>(sum);
-    const float inv = 1.0f / sum;
-    if (f) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u * kWave + lane_id() < n_split) f[u * kWave + lane_id()] = v[u].y * inv;
-    }
-    return (top - shift) + log2f(sum);
-}
-// Weighted sum of the splits of `quads` groups of four channels.  Four sums, by split modulo four, whichever thread takes them: the result does
-// not depend on how many heads are joined at a time.
-template <int NT, int SHARES>
-__device__ __forceinline__ void sum_splits(const AttendCall& a, int64_t head0, int quads, int n_split, const float* f, f32x4* part) {
-    constexpr int U = 16, SUMS = 4 / SHARES;                       // splits in flight (a trip to memory each otherwise); sums of a thread
-    const __amdgpu_buffer_rsrc_t rsrc =
-        __builtin_amdgcn_make_buffer_rsrc(a.part_acc + head0 * a.n_split * a.D, 0, 16 * a.n_split * a.D * 4, 0x00020000);
-    const int quarter = a.D / 4, first = SHARES > 1 ? (int)threadIdx.x / quads : 0;
-    for (int i = SHARES > 1 ? (int)threadIdx.x % quads : (int)threadIdx.x; i < quads && first < SHARES; i += NT) {
-        const int h = i / quarter, c = 4 * (i - h * quarter);
-        const float* const fh = f + h * n_split;
-        const uint32_t off = (uint32_t)(h * a.n_split * a.D + c) * 4;
-        f32x4 sum[SUMS] = {};
-        for (int x0 = first; x0 < n_split; x0 += U * SHARES) {
-            f32x4 v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {                          // (sc1: past the L2 of this XCD)
-                const int x = x0 + u * SHARES < n_split ? x0 + u * SHARES : x0;
-                v[u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(off + (uint32_t)(x * a.D) * 4), 0, 16));
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float w = x0 + u * SHARES < n_split ? fh[x0 + u * SHARES] : 0.f;
-                if (w != 0.f) {                                     // (a split of nothing but -inf may hold anything)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) sum[u % SUMS][y] = fmaf(w, v[u][y], sum[u % SUMS][y]);
-                }
-            }
-        }
-        if (SHARES > 1) {
-#pragma unroll
-            for (int y = 0; y < SUMS; ++y) part[(first + y * SHARES) * quads + i] = sum[y];
-        } else {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) a.out[(head0 + h) * a.D + c + y] = (sum[0][y] + sum[1 % SUMS][y]) + (sum[2 % SUMS][y] + sum[3 % SUMS][y]);
-        }
-    }
-    if (SHARES > 1) {
-        __syncthreads();
-        if ((int)threadIdx.x < quads) {
-            const f32x4* q = part + threadIdx.x;
-            const f32x4 sum = (q[0] + q[quads]) + (q[2 * quads] + q[3 * quads]);
-            float* out = a.out + (head0 + (int)threadIdx.x / quarter) * a.D + 4 * ((int)threadIdx.x % quarter);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) out[y] = sum[y];
-        }
-    }
-}
-// out and lse of `heads` neighbouring heads (at most 16) from their splits; a workgroup of NT threads, f: [heads][n_split] in LDS.
-template <int NT>
-__device__ __forceinline__ void join_splits(const AttendCall& a, int64_t head0, int heads, int n_split, float shift, float* f, f32x4* part) {
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    for (int h = wave; h < heads; h += NT / kWave) {
-        const float lg2 = head_log2_sum(a, head0 + h, n_split, shift, f + h * n_split);
-        if (lane_id() == 0 && a.lse) a.lse[head0 + h] = lg2 * 0.69314718055994531f;
-    }
-    __syncthreads();
-    // Four channels a thread; with few of them two or four threads share a group's splits.
-    const int quads = heads * (a.D / 4);
-    if (quads <= NT / 4) sum_splits<NT, 4>(a, head0, quads, n_split, f, part);
-    else if (quads <= NT / 2) sum_splits<NT, 2>(a, head0, quads, n_split, f, part);
-    else sum_splits<NT, 1>(a, head0, quads, n_split, f, part);
-}
-
 // FOLD: for splits of more than kFold steps a wave.  (Shorter ones without the code for it, which takes registers: 32 sequences of 800 to 16384
 // tokens of d = 64 with mass 167 us, 176 with it.)
-template <int DT, int D, bool LIST, bool MASS, bool FOLD>
+template <int DT, int D, int WALK, bool MASS, bool FOLD>
 __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) attend_kernel(AttendCall a) {
     using Tile = AttendTile<DT, D>;
+    constexpr bool LIST = WALK == kWalkList;
     constexpr int SUB = Tile::SUB, STEP = Tile::STEP, KEYS = Tile::KEYS, KCH = Tile::KCH, T = Tile::T, ROW = Tile::ROW, EV = Tile::EV;
     constexpr int SPP = 64 / STEP;
     constexpr int NW = 4, NT = NW * kWave, RED = NW * 16 * (D + 4), JOIN = 16 * kMaxSplits + 8 * NT;
@@ -204,6 +110,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     if (stream < 0) stream += streams;
     const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
     const int64_t N = a.len[b];
+    const WindowWalk seen(N, a.sinks, WALK == kWalkWindow ? a.window : N);
     const int64_t pages = attend_pages(a, N);
     const int ns = attend_splits(a, pages);
     if (split >= ns) return;                                  // (the join knows how many splits a sequence has)
@@ -236,6 +143,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     // First row of the wave's step i (steps wave, wave + NW, ... of the split), asked for in order.
     auto row_of = [&](int i) -> int64_t {
         const int s = wave + NW * i;
+        if (WALK == kWalkWindow) return seen.row(p0 + s / SPP) + (s % SPP) * STEP;
         if (!LIST) return p0 * 64 + (int64_t)s * STEP;
         if ((i & 63) == 0) {
             const int at = wave + NW * (i + lane);
@@ -244,8 +152,8 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages_ahead, i & 63);
         return (int64_t)page * 64 + (s % SPP) * STEP;
     };
-    auto rows_from = [&](int64_t row0, bool live) -> int {      // rows of the step that the cache holds
-        const int64_t left = live ? N - row0 : 0;
+    auto rows_from = [&](int64_t row0, int s) -> int {          // rows of step s that are seen
+        const int64_t left = s < n_steps ? (WALK == kWalkWindow ? seen.end(p0 + s / SPP) : N) - row0 : 0;
         int r = (int)(left < 0 ? 0 : left > STEP ? STEP : left);
         r = __builtin_amdgcn_readfirstlane(r);
         asm("" : "+s"(r));
@@ -253,7 +161,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     };
     auto load = [&](Tile& t, int i, int& rows) {
         const int64_t row0 = row_of(i);
-        rows = rows_from(row0, wave + NW * i < n_steps);
+        rows = rows_from(row0, wave + NW * i);
         // what lies behind the rows there are reads as zero and is not fetched: no weight of zero meets a value of infinity
         const int64_t at = rows > 0 ? row0 * ROW : 0;
         const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(Kh + at), 0, rows * ROW, 0x00020000);
@@ -526,17 +434,18 @@ hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
     const int64_t n_join = attend_join_wgs(a), n_mass = attend_mass_wgs(a);
     const bool fold = (int64_t)a.chunk * 64 > (int64_t)kFold * 4 * (a.dtype == DT_F32 ? AttendTile<DT_F32, 32>::STEP : AttendTile<DT_F16, 32>::STEP);
     const dim3 grid((unsigned)attend_walk_wgs(a)), wg(256);
-#define TKA_ATTEND_(DT_, D_, LIST_, MASS_)                                                                              \
+#define TKA_ATTEND_(DT_, D_, WALK_, MASS_)                                                                              \
     do {                                                                                                                \
-        if (fold) hipLaunchKernelGGL((attend_kernel<DT_, D_, LIST_, MASS_, true>), grid, wg, 0, st, a);                 \
-        else hipLaunchKernelGGL((attend_kernel<DT_, D_, LIST_, MASS_, false>), grid, wg, 0, st, a);                     \
+        if (fold) hipLaunchKernelGGL((attend_kernel<DT_, D_, WALK_, MASS_, true>), grid, wg, 0, st, a);                 \
+        else hipLaunchKernelGGL((attend_kernel<DT_, D_, WALK_, MASS_, false>), grid, wg, 0, st, a);                     \
     } while (0)
 #define TKA_ATTEND(DT_, D_)                                                                                             \
     do {                                                                                                                \
-        if (a.list && a.mass) TKA_ATTEND_(DT_, D_, true, true);                                                         \
-        else if (a.list) TKA_ATTEND_(DT_, D_, true, false);                                                             \
-        else if (a.mass) TKA_ATTEND_(DT_, D_, false, true);                                                             \
-        else TKA_ATTEND_(DT_, D_, false, false);                                                                        \
+        if (a.list && a.mass) TKA_ATTEND_(DT_, D_, kWalkList, true);                                                    \
+        else if (a.list) TKA_ATTEND_(DT_, D_, kWalkList, false);                                                        \
+        else if (a.mass) TKA_ATTEND_(DT_, D_, kWalkAll, true);                                                          \
+        else if (a.window) TKA_ATTEND_(DT_, D_, kWalkWindow, false);                                                    \
+        else TKA_ATTEND_(DT_, D_, kWalkAll, false);                                                                     \
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_ATTEND, a.dtype, a.D);
 #undef TKA_ATTEND

@@ -23,8 +23,33 @@ constexpr int kMostSelected = 1 << 28;                 // the largest max_k of a
 
 constexpr int kMaxSplits = 256;  // splits of a sequence (their factors sit in LDS when they are joined)
 
-// Attention of one query per sequence and head over all cached tokens, or over a list of pages of 64 tokens.
-struct AttendCall {
+// The first `sinks` and the newest `window` (>= 1) of N tokens, in pages of 64 rows: those of the first ones from the front, those of the
+// newest ones from the first token of the window on, so that a page has rows to leave out at its end only.
+struct WindowWalk {
+    int64_t N, first, sinks, sink_pages;     // (first token of the window; sinks in front of it)
+    __host__ __device__ WindowWalk(int64_t n, int64_t sinks_, int64_t window) : N(n) {
+        first = window < n ? n - window : 0;
+        if (sinks_ >= first) { first = 0; sinks_ = 0; }
+        sinks = sinks_;
+        sink_pages = (sinks + 63) / 64;
+    }
+    __host__ __device__ int64_t pages() const { return sink_pages + (N - first + 63) / 64; }
+    __host__ __device__ int64_t row(int64_t page) const { return page < sink_pages ? page * 64 : first + (page - sink_pages) * 64; }
+    __host__ __device__ int64_t end(int64_t page) const { return page < sink_pages ? sinks : N; }     // row that the page's stretch ends before
+};
+
+// Splits of the keys of [heads] and what they leave.
+struct SplitParts {
+    float* part_acc;            // [heads][n_split][D] weighted sums of the splits
+    float* part_lm;             // [heads][n_split][2] their sums of weights, and the score the weights are relative to (times log2(e) / sqrt(D))
+    float* out;                 // [heads][D]
+    float* lse;                 // [heads] or null
+    int n_split;                // splits of the longest sequence
+    int D;
+};
+
+// Attention of one query per sequence and head over all cached tokens, the newest and the first ones, or a list of pages of 64 tokens.
+struct AttendCall : SplitParts {
     const char* K;              // this layer's keys and values [B][Hkv][Ncap][D]
     const char* V;
     const void* q;              // [B][Hq][D]
@@ -32,21 +57,17 @@ struct AttendCall {
     const int32_t* list;        // [B][Hkv][list_stride] pages to attend, ascending, or null: all
     int64_t list_stride;
     int n_list;                 // pages of a list (a sequence of fewer pages: all of its own)
-    float* part_acc;            // [B*Hq][n_split][D] weighted sums of the splits
-    float* part_lm;             // [B*Hq][n_split][2] their sums of weights, and the score the weights are relative to (times log2(e) / sqrt(D))
     uint32_t* arrive;           // [B][Hkv][row_blocks] splits that are done; zero between calls
     float* scores;              // [B*Hq][score_stride] raw scores in the order of the walk, kept for `mass`
     int64_t score_stride;
-    float* out;                 // [B*Hq][D]
-    float* lse;                 // [B*Hq] or null
     float* mass;                // [B][Hkv][Ncap] or null
     int64_t Ncap;
     int64_t walk;               // most keys a sequence's walk covers, whole pages
-    int B, Hq, Hkv, G, D, dtype;
+    int64_t sinks, window;      // window > 0: the first `sinks` and the newest `window` tokens alone
+    int B, Hq, Hkv, G, dtype;
     int chunk;                  // pages per split
     int join_later;             // the splits are put together in a launch of its own,
     int join_heads;             // by a workgroup per head (1) or per block of heads (16)
-    int n_split;                // splits of the longest sequence
     int row_blocks;             // blocks of 16 heads of a group
     float scale_log2e;          // log2(e) / sqrt(D)
 };

@@ -1,0 +1,617 @@
+// Attention of the last M tokens of a sequence over what each sees (topk_attn_prompt, topk_attn_coded_prompt): the kernel, shared by prompt.hip (caches in
+// their own type) and coded_prompt.hip (the 8-bit cache).
+//
+//   out_m = sum_t w_t V_t / sum_t w_t,  w_t = exp(q_m . K_t / sqrt(d)),  t <= p_m and (t < sinks or t > p_m - window)
+//
+// A row is a query and a head of the group, m G + g: the heads of a group read the same keys, and a block of rows covers few queries, so little of what
+// it computes is masked.  A wave has 32 rows (or twice that), the workgroup walks the keys in tiles of 64 through LDS.  Products are taken transposed (keys x channels
+// times channels x rows, then channels x keys times keys x rows): a lane holds scores and weighted sums of one row, lane % 32, the running maximum is
+// a number per lane, and the scores come out of the first product in the order in which the second one takes the weights:
+//   score register i of a 32-key tile is key 8 (i / 4) + 4 (lane / 32) + i % 4; step x of 16 keys takes registers 8 x .. 8 x + 7.
+// Weights are rounded once to the type of the values (16 bits); their sum is of the unrounded ones.
+#pragma once
+#include <type_traits>
+
+#include "coded.h"
+#include "device_utils.h"
+#include "internal.h"
+
+namespace tka {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct PromptCall {
+    const char* K;              // rows [S][Hkv][Ncap][D] of the call's first sequence
+    const char* V;
+    CodedArrays c;              // or the coded cache
+    const void* q;              // [S][M][Hq][D]
+    void* out;                  // [S][M][Hq][D] in the type of q
+    float* lse;                 // [S][M][Hq] or null
+    const int32_t* len;         // [S]
+    int64_t Ncap, M;
+    int64_t sinks, window;
+    float* part_acc;            // [S Hkv][row_blocks][n_split][rows of a block][D], where keys are split
+    float* part_lm;             // [...][rows of a block][2]
+    int S, Hq, Hkv, G, D, dtype, format;
+    int n_split, row_blocks, block_rows;
+};
+// Tiles of 64 keys that the rows of the last block, which see most, see of a sequence of N tokens.
+inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int64_t window) {
+    const int64_t oldest = N - last_queries - window, from = oldest < 0 ? 0 : oldest / 64, front = ((sinks < N ? sinks : N) + 63) / 64;
+    return (N + 63) / 64 - from + (front < from ? front : from);
+}
+// Rows of a block, and the splits of its keys.  (room: bytes there are for partial sums)
+inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu) {
+    const int64_t rows = a->M * a->G, streams = (int64_t)a->S * a->Hkv;
+    const bool wide = a->dtype != DT_F32 && a->D <= 128;
+    a->block_rows = rows <= 32 ? 32 : wide && streams * ((rows + 255) / 256) >= n_cu ? 256 : 128;
+    a->row_blocks = (int)((rows + a->block_rows - 1) / a->block_rows);
+    int64_t tiles = 1;
+    for (int b = 0; b < a->S; ++b) {
+        const int64_t n = prompt_tiles(len[b], (a->block_rows + a->G - 1) / a->G, a->sinks, a->window);
+        if (n > tiles) tiles = n;
+    }
+    const int64_t wgs = streams * a->row_blocks, want = 2 * n_cu;
+    int64_t split = wgs >= n_cu ? 1 : (want + wgs - 1) / wgs;
+    const int64_t most = (int64_t)(room / ((size_t)wgs * a->block_rows * (a->D + 2) * sizeof(float)));
+    if (split > tiles / 4) split = tiles / 4;
+    if (split > most) split = most;
+    if (split > 64) split = 64;
+    a->n_split = split < 1 ? 1 : (int)split;
+}
+inline void place_prompt_parts(PromptCall* a, void* room) {
+    a->part_acc = static_cast<float*>(room);
+    a->part_lm = a->part_acc + (size_t)a->S * a->Hkv * a->row_blocks * a->n_split * a->block_rows * a->D;
+}
+constexpr int64_t kMostPromptRows = 1 << 30;      // of a stream: counted in 32 bits
+hipError_t launch_prompt(const PromptCall& a, hipStream_t st);
+hipError_t launch_prompt_coded(const PromptCall& a, hipStream_t st);
+hipError_t launch_prompt_join(const PromptCall& a, hipStream_t st);
+
+// ---- tiles in LDS ----
+// Rows of 64 keys lie one after the other; the 16-byte pieces of a row change places among each other by its number, so that the lanes that read at a time meet
+// all banks: 32 rows at one piece (keys), 8 rows at four neighbouring pieces (values, 16 bits), two rows four apart (values, 32 bits).
+template <int ROWB> __device__ __forceinline__ constexpr int key_piece(int row, int piece) {
+    constexpr int P = ROWB / 16, L = P < 16 ? P : 16;
+    return piece ^ ((row / (16 / L)) % L);
+}
+template <int ROWB, int EB> __device__ __forceinline__ constexpr int value_piece(int row, int piece) {
+    constexpr int P = ROWB / 16;
+    if (EB == 4) return P >= 16 ? piece ^ (8 * ((row >> 2) & 1)) : piece;
+    return P >= 16 ? piece ^ ((4 * (row & 3)) ^ ((row >> 2) & 3)) : P == 8 ? piece ^ (4 * ((row >> 1) & 1)) : piece;
+}
+
+template <int CT> struct TileType;      // what a tile's products are taken in
+template <> struct TileType<DT_F16> { using v8 = f16x8; static constexpr int bytes = 2; };
+template <> struct TileType<DT_BF16> { using v8 = bf16x8; static constexpr int bytes = 2; };
+template <> struct TileType<DT_F32> { static constexpr int bytes = 4; };
+
+__device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// Queries of a wave's rows as the second operand: 16 bits, 16 channels of a row in eight-channel halves; 32 bits, 8 channels in four-channel halves.
+template <int CT, int D, int NR, int PQ> struct QueryFrag {
+    using type = typename std::conditional<CT == DT_F32, f32x4, typename std::conditional<CT == DT_BF16, bf16x8, f16x8>::type>::type;
+    static constexpr int N = CT == DT_F32 ? D / 8 : D / 16;
+    type v[PQ][NR][N];
+};
+
+template <int D, int NR> struct RowState {
+    f32x16 acc[NR][D / 32];
+    float m[NR], l[NR], e[NR];  // running maximum (whole), sum of weights relative to it, power of two of the weighted sum
+    int pos[NR], hidden[NR];    // token of the row; the newest one its window leaves out
+};
+
+__device__ __forceinline__ float other_half_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Values of a tile for channels 32 ct + lane % 32, the keys of step x: FRAG: laid out as the operand; else rows, read transposed.
+template <int D, bool FRAG>
+__device__ __forceinline__ u32x4 value_frag(const char* lds, int ct, int x) {
+    const int lane = lane_id();
+    if (FRAG) return *reinterpret_cast<const u32x4*>(lds + ((x * (D / 32) + ct) * 64 + lane) * 16);
+    constexpr int ROWB = 2 * D;
+    const int i = lane & 15, hh = lane >> 5, col = 32 * ct + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+    u32x4 r;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        const int row = 16 * x + 8 * y + 4 * hh + (i >> 2);
+        const char* p = lds + row * ROWB + value_piece<ROWB, 2>(row, col >> 3) * 16 + (col & 7) * 2;
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+        const uint2 w = __builtin_bit_cast(uint2, v);
+        r[2 * y] = w.x; r[2 * y + 1] = w.y;
+    }
+    return r;
+}
+
+// 16-bit halves that are an infinity or a NaN: as ones in their place, and the word without them
+template <int CT> __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+    constexpr uint32_t E = CT == DT_F16 ? 0x7C00u : 0x7F80u;
+    uint32_t keep = 0;
+    if ((w & E) != E) keep |= 0xFFFFu;
+    if (((w >> 16) & E) != E) keep |= 0xFFFF0000u;
+    return w & keep;
+}
+template <int CT> __device__ __forceinline__ bool has_no_number(uint32_t w) {
+    if (CT == DT_F32) return (w & 0x7F800000u) == 0x7F800000u;
+    return finite_halves<CT>(w) != w;
+}
+
+// One tile of 64 keys from token t0 on.  f (and f_lo, of 32-bit rows): score times this is the exponent of two.  VSCALE: the values are times `sv` (a block's scale),
+// the weighted sum has a power of two of its own (coded_decode.hip).  `masked`: not all rows of the wave see all keys.
+template <int CT, bool FRAG, bool VSCALE, bool EXACT, int D, int NR, int PQ, int PP>
+__device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, const QueryFrag<CT, D, NR, PQ>& q, RowState<D, NR>& st,
+                                            const float (&f)[NR], const float (&f_lo)[NR], float sv, bool masked, int t0, int sinks) {
+    constexpr int EB = TileType<CT>::bytes, ROWB = D * EB;
+    const int lane = lane_id(), hh = lane >> 5, row = lane & 31;
+    f32x16 s[2][NR];
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[sub][r] = f32x16{};
+        const char* const base = ldsK + (32 * sub + row) * ROWB;
+#pragma unroll
+        for (int c = 0; c < QueryFrag<CT, D, NR, PQ>::N; ++c) {
+            const u32x4 k = *reinterpret_cast<const u32x4*>(base + key_piece<ROWB>(32 * sub + row, 2 * c + hh) * 16);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                if constexpr (CT == DT_F32) {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) s[sub][r] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[y]), q.v[0][r][c][y], s[sub][r], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int z = 0; z < PQ; ++z) s[sub][r] = mfma32(__builtin_bit_cast(typename TileType<CT>::v8, k), q.v[z][r][c], s[sub][r]);
+                }
+            }
+        }
+    }
+    // ---- weights, in place of the scores ----
+    float g[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int t = t0 + 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hh + i % 4;
+                if (t > st.pos[r] || (t <= st.hidden[r] && t >= sinks)) s[i / 16][r][i % 16] = -INFINITY;
+            }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i / 16][r][i % 16]);
+        top = other_half_max(top);
+        const bool none = top == -INFINITY;
+        const float bm = ceilf(top * f[r]), m_new = fmaxf(st.m[r], none ? -INFINITY : bm), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float down = __builtin_amdgcn_exp2f(st.m[r] - ref);
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float x = s[i / 16][r][i % 16];
+            float w = __builtin_amdgcn_exp2f(EXACT ? fmaf(x, f[r], fmaf(x, f_lo[r], -ref)) : fmaf(x, f[r], -ref));
+            if ((VSCALE || EXACT) && masked && x == -INFINITY) w = 0.f;          // (a factor of zero, or of two parts)
+            s[i / 16][r][i % 16] = w;
+            sum[i & 1] += w;
+        }
+        st.l[r] = fmaf(st.l[r], down, sum[0] + sum[1]);
+        float turn = down;                                          // of the weighted sum
+        g[r] = 1.f;
+        if (VSCALE) {
+            const int ke = (int)(__float_as_uint(sv) >> 23) - 126;  // sv < 2^ke
+            const float e_new = sv > 0.f && !none ? fmaxf(st.e[r], bm + (float)ke) : st.e[r];
+            g[r] = sv;
+            if (sv > 0.f) g[r] = ldexpf(sv, (int)fmaxf(fminf(ref - e_new + kShift, (float)(127 - ke)), -300.f));
+            if (none) g[r] = 0.f;                                   // (a block of NaN that the row does not see)
+            turn = st.e[r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.e[r] - e_new);
+            st.e[r] = e_new;
+        }
+        st.m[r] = m_new;
+        if (__any(turn != 1.f)) {
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st.acc[r][ct][i] *= turn;
+            }
+        }
+        if (VSCALE) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[i / 16][r][i % 16] *= g[r];
+        }
+    }
+    // ---- values that are no numbers, in a tile that not all rows see ----
+    bool poison = false;
+    if (!FRAG && masked) {
+        uint64_t keys = 0;
+        for (int at = 0; at < 64 * ROWB; at += 1024) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(ldsV + at + lane * 16);
+            const uint64_t bad = __ballot(has_no_number<CT>(w.x) || has_no_number<CT>(w.y) || has_no_number<CT>(w.z) || has_no_number<CT>(w.w));
+            if (bad) {
+                if (ROWB >= 1024) keys |= 1ull << (at / ROWB);
+                else
+                    for (int y = 0; y < 1024 / ROWB; ++y)
+                        if ((bad >> (y * (ROWB / 16))) & (ROWB / 16 == 64 ? ~0ull : (1ull << (ROWB / 16 % 64)) - 1)) keys |= 1ull << (at / ROWB + y);
+            }
+        }
+        poison = keys != 0;
+        // such a value goes to the rows that see it, one key at a time; the products below take zero in its place
+        while (keys) {
+            const int key = __builtin_ctzll(keys);
+            keys &= keys - 1;
+            const int reg = (key >> 5) * 16 + ((key & 31) >> 3) * 4 + (key & 3), t = t0 + key;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                float p = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i == reg) p = s[i / 16][r][i % 16];
+                p = __shfl(p, row + 32 * ((key >> 2) & 1), 64);
+                const bool sees = !(t > st.pos[r] || (t <= st.hidden[r] && t >= sinks));
+#pragma unroll
+                for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int ch = 32 * ct + 8 * (i / 4) + 4 * hh + i % 4;
+                        const char* at = ldsV + key * ROWB + value_piece<ROWB, EB>(key, ch * EB / 16) * 16 + ch * EB % 16;
+                        float v;
+                        if (CT == DT_F32) v = *reinterpret_cast<const float*>(at);
+                        else if (CT == DT_F16) v = (float)*reinterpret_cast<const _Float16*>(at);
+                        else v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
+                        if (sees && !(fabsf(v) < INFINITY)) st.acc[r][ct][i] = fmaf(p, v, st.acc[r][ct][i]);
+                    }
+                }
+            }
+        }
+    }
+    // ---- weighted sum ----
+    if constexpr (CT == DT_F32) {
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int key = 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hh + i % 4, ch = 32 * ct + row;
+                float v = *reinterpret_cast<const float*>(ldsV + key * ROWB + value_piece<ROWB, 4>(key, ch >> 2) * 16 + (ch & 3) * 4);
+                if (poison && !(fabsf(v) < INFINITY)) v = 0.f;
+#pragma unroll
+                for (int r = 0; r < NR; ++r) st.acc[r][ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i / 16][r][i % 16], st.acc[r][ct], 0, 0, 0);
+            }
+        }
+    } else {
+        using v8 = typename TileType<CT>::v8;
+        using E = typename std::conditional<CT == DT_F16, _Float16, __bf16>::type;
+        v8 p[PP][NR][4];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                float rest = s[i / 16][r][i % 16];
+#pragma unroll
+                for (int z = 0; z < PP; ++z) {
+                    p[z][r][i / 8][i % 8] = (E)rest;
+                    rest -= (float)p[z][r][i / 8][i % 8];
+                }
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct) {
+                u32x4 v = value_frag<D, FRAG>(ldsV, ct, x);
+                if (!FRAG && poison) {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) v[y] = finite_halves<CT>(v[y]);
+                }
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+#pragma unroll
+                    for (int z = 0; z < PP; ++z) st.acc[r][ct] = mfma32(__builtin_bit_cast(v8, v), p[z][r][x], st.acc[r][ct]);
+                }
+            }
+        }
+    }
+}
+
+// 64 rows of a type into LDS, straight from memory; rows behind `rows` are zeros.  Not waited for.
+template <int ROWB, int NW, bool VALUES, int EB>
+__device__ __forceinline__ void fetch_rows(const char* from, int rows, char* lds) {
+    constexpr int PIECES = ROWB / 16, I = 64 * ROWB / 1024;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id();
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, rows * ROWB, 0x00020000);
+#pragma unroll
+    for (int u = 0; u < (I + NW - 1) / NW; ++u) {
+        const int in = wave + NW * u, at = in * 64 + lane, row = at / PIECES, piece = at % PIECES;
+        const int off = row * ROWB + (VALUES ? value_piece<ROWB, EB>(row, piece) : key_piece<ROWB>(row, piece)) * 16;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + in * 1024), 16, off, 0, 0, 0);
+    }
+}
+
+// DT: type of queries, output and open rows; FMT: the coded cache's format, or -1: rows of DT.  NW waves of 32 NR rows.
+template <int DT, int FMT, int D, int NW, int NR>
+__global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
+    constexpr bool CODED = FMT >= 0;
+    constexpr int CT = CODED ? DT_F16 : DT, PARTS = CODED && DT == DT_F32 ? 2 : 1;
+    constexpr int EB = TileType<CT>::bytes, ROWB = D * EB, TILE = 64 * ROWB, OPEN_ROWB = D * TileType<DT>::bytes;
+    constexpr int NBUF = 4 * TILE <= 131072 ? 2 : 1;
+    constexpr int LDS = 2 * NBUF * TILE > 128 * OPEN_ROWB || !CODED ? 2 * NBUF * TILE : 128 * OPEN_ROWB;
+    constexpr int NT = 64 * NW, ROWS = 32 * NW * NR, FM = CODED ? FMT : CODED_E4M3;
+    __shared__ __align__(16) char lds[LDS];
+    const int lane = lane_id(), hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // Streams next to each other (workgroups go to the XCDs in turn: a stream stays on one where their number is a multiple of eight), the last rows, which see most, first.
+    const int streams = a.S * a.Hkv, stream = (int)blockIdx.x % streams, rest = (int)blockIdx.x / streams;
+    const int split = rest % a.n_split, rb = a.row_blocks - 1 - rest / a.n_split;
+    const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
+    const int N = a.len[b], M = (int)a.M, n_rows = M * a.G, row0 = rb * ROWS;
+    const int sinks = (int)(a.sinks < N ? a.sinks : N);
+    const int before = N - M;                                       // tokens in front of the first query's
+    const auto query_of = [&](int row) { return (row < n_rows ? row : n_rows - 1) / a.G; };
+    const auto hidden_of = [&](int p) { return a.window <= p ? p - (int)a.window : -1; };
+
+    // tiles that some row of the workgroup sees
+    const int p_lo = before + query_of(row0), p_hi = before + query_of(row0 + ROWS - 1);
+    const int first = hidden_of(p_lo) + 1;
+    int front = ((sinks < p_hi + 1 ? sinks : p_hi + 1) + 63) / 64, from = first / 64;
+    if (front >= from) { front = 0; from = 0; }
+    const int full = CODED ? N / 64 : 0x7FFFFFFF;                   // (open rows after the loop)
+    if (front > full) front = full;
+    int to = p_hi / 64 + 1;
+    if (to > full) to = full;
+    if (from > to) from = to;
+    const int n_tiles = front + to - from;
+    const int i0 = (int)((int64_t)split * n_tiles / a.n_split), i1 = (int)((int64_t)(split + 1) * n_tiles / a.n_split);
+    const auto tile_of = [&](int i) { return i < front ? i : from + (i - front); };
+
+    RowState<D, NR> st;
+    int wave_lo = 0x7FFFFFFF, wave_hi = 0;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int at = row0 + 32 * (NR * wave + r);
+        st.m[r] = st.e[r] = -INFINITY;
+        st.l[r] = 0.f;
+        st.pos[r] = before + query_of(at + (lane & 31));
+        st.hidden[r] = hidden_of(st.pos[r]);
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) st.acc[r][ct] = f32x16{};
+        if (r == 0) wave_lo = before + query_of(at);
+        wave_hi = before + query_of(at + 31);
+    }
+    const bool idle = row0 + 32 * NR * wave >= n_rows;
+    const int wave_first = hidden_of(wave_lo) + 1, wave_last = hidden_of(wave_hi);     // oldest token a window of the wave has, newest one that some window leaves out
+    // Whether a row of the wave sees a key of the tile, and whether all see all.
+    const auto seen = [&](int t0) { return !idle && t0 <= wave_hi && (t0 + 63 >= wave_first || t0 < sinks); };
+    const auto whole = [&](int t0) { return t0 + 63 <= wave_lo && (t0 > wave_last || t0 + 63 < sinks); };
+
+    constexpr double kScale = 1.4426950408889634 / (D == 32 ? 5.656854249492381 : D == 64 ? 8.0 : D == 128 ? 11.313708498984761 : 16.0);
+    constexpr float kScaleHi = (float)kScale, kScaleLo = (float)(kScale - (double)kScaleHi);
+
+    const auto query_row = [&](int r) {
+        int row = row0 + 32 * (NR * wave + r) + (lane & 31);
+        row = row < n_rows ? row : n_rows - 1;
+        const int m = row / a.G;
+        return (((int64_t)b * M + m) * a.Hq + kvh * a.G + (row - m * a.G)) * D;
+    };
+    const auto load_rows = [&](auto& frag) {                        // queries in their own type
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const char* p = static_cast<const char*>(a.q) + query_row(r) * TileType<DT>::bytes;
+#pragma unroll
+            for (int c = 0; c < D * TileType<DT>::bytes / 32; ++c)
+                frag.v[0][r][c] = __builtin_bit_cast(typename std::remove_reference<decltype(frag.v[0][r][c])>::type, *reinterpret_cast<const u32x4*>(p + 32 * c + 16 * hh));
+        }
+    };
+
+    if constexpr (!CODED) {
+        QueryFrag<DT, D, NR, 1> q;
+        load_rows(q);
+        const char* const Kh = a.K + (int64_t)stream * a.Ncap * ROWB;
+        const char* const Vh = a.V + (int64_t)stream * a.Ncap * ROWB;
+        const auto fetch = [&](int i, int buf) {
+            const int t0 = 64 * tile_of(i), rows = N - t0 < 64 ? N - t0 : 64;
+            fetch_rows<ROWB, NW, false, EB>(Kh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE);
+            fetch_rows<ROWB, NW, true, EB>(Vh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE + TILE);
+        };
+        float f[NR], f_lo[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) { f[r] = kScaleHi; f_lo[r] = kScaleLo; }
+        if (NBUF == 2 && i0 < i1) fetch(i0, 0);
+        for (int i = i0; i < i1; ++i) {
+            const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
+            if (NBUF == 1) {
+                __syncthreads();
+                fetch(i, 0);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (NBUF == 2 && i + 1 < i1) fetch(i + 1, buf ^ 1);
+            const int t0 = 64 * tile_of(i);
+            if (seen(t0))
+                prompt_tile<DT, false, false, DT == DT_F32, D, NR, 1, 1>(lds + buf * 2 * TILE, lds + buf * 2 * TILE + TILE, q, st, f, f_lo, 1.f, !whole(t0), t0, sinks);
+        }
+    } else {
+        // ---- blocks: codes through registers, into LDS as fp16 ----
+        float unit_q[NR];
+        {
+            QueryFrag<DT_F16, D, NR, PARTS> q;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const char* p = static_cast<const char*>(a.q) + query_row(r) * TileType<DT>::bytes;
+                float amax = 0.f;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    float x[8];
+#pragma unroll
+                    for (int y = 0; y < 8; y += Elem<DT>::kPerLoad)
+                        Elem<DT>::widen(*reinterpret_cast<const u32x4*>(p + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) amax = fmaxf(amax, fabsf(x[y]));
+                }
+                amax = other_half_max(amax);
+                int up = 13 - ((int)(__float_as_uint(amax) >> 23) - 127);       // amax times 2^up lies in [2^13, 2^14)
+                up = amax == 0.f || up > 120 ? 120 : up < -114 ? -114 : up;
+                const float by = __uint_as_float((uint32_t)(up + 127) << 23);
+                unit_q[r] = __uint_as_float((uint32_t)(127 - up) << 23) * CodeUnit<FM>::value;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    float x[8];
+#pragma unroll
+                    for (int y = 0; y < 8; y += Elem<DT>::kPerLoad)
+                        Elem<DT>::widen(*reinterpret_cast<const u32x4*>(p + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) {
+                        float left = x[y] * by;
+#pragma unroll
+                        for (int z = 0; z < PARTS; ++z) {
+                            q.v[z][r][c][y] = (_Float16)left;
+                            left -= (float)q.v[z][r][c][y];
+                        }
+                    }
+                }
+            }
+            constexpr int CB = coded_block_bytes(D), PT = CB / 16 / NT;         // pieces of 16 bytes of a thread
+            static_assert(CB / 16 % NT == 0 || CB / 16 < NT, "whole passes");
+            constexpr int P = PT ? PT : 1;
+            u32x4 k[P], v[P];
+            float2 scale, next = make_float2(0.f, 0.f);
+            const char* const Kb = a.c.codes[0] + (int64_t)stream * a.c.blocks * CB;
+            const char* const Vb = a.c.codes[1] + (int64_t)stream * a.c.blocks * CB;
+            const float* const Sb = a.c.scales + (int64_t)stream * a.c.blocks * 2;
+            const bool mine = PT || (int)threadIdx.x < CB / 16;
+            const auto load = [&](int i) {
+                const int64_t block = tile_of(i);
+                if (mine) {
+#pragma unroll
+                    for (int u = 0; u < P; ++u) {
+                        const int at = (u * NT + (int)threadIdx.x) * 16;
+                        k[u] = *reinterpret_cast<const u32x4*>(Kb + block * CB + at);
+                        v[u] = *reinterpret_cast<const u32x4*>(Vb + block * CB + at);
+                    }
+                }
+                next = *reinterpret_cast<const float2*>(Sb + 2 * block);
+            };
+            const auto place = [&](int buf) {
+                char* const to = lds + buf * 2 * TILE;
+                if (!mine) return;
+#pragma unroll
+                for (int u = 0; u < P; ++u) {
+                    const int x = u * NT + (int)threadIdx.x, pair = x / 64, j = (x >> 4) & 3, n = x & 15;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int unit = 2 * pair + y, key = 16 * (unit / (D / 32)) + n, piece = 4 * (unit % (D / 32)) + j;
+                        *reinterpret_cast<f16x8*>(to + key * ROWB + key_piece<ROWB>(key, piece) * 16) = code_values<FM>(k[u][2 * y], k[u][2 * y + 1]);
+                    }
+                    const int ch = 16 * pair + n;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const u32x4 w = __builtin_bit_cast(u32x4, code_values<FM>(v[u][2 * y], v[u][2 * y + 1]));
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)                  // keys 16 (2 y + z) + 4 j .. + 3
+                            *reinterpret_cast<uint2*>(to + TILE + (((2 * y + z) * (D / 32) + ch / 32) * 64 + (j & 1) * 32 + ch % 32) * 16 + (j >> 1) * 8) =
+                                make_uint2(w[2 * z], w[2 * z + 1]);
+                    }
+                }
+            };
+            if (i0 < i1) {
+                load(i0);
+                place(0);
+            }
+            for (int i = i0; i < i1; ++i) {
+                const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
+                scale = next;
+                if (i + 1 < i1) load(i + 1);
+                __syncthreads();
+                const int t0 = 64 * tile_of(i);
+                if (seen(t0)) {
+                    float f[NR], f_lo[NR];
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+                        const float by = scale.x * unit_q[r];
+                        f[r] = by * kScaleHi;
+                        f_lo[r] = fmaf(by, kScaleHi, -f[r]) + by * kScaleLo;
+                    }
+                    prompt_tile<DT_F16, true, true, DT == DT_F32, D, NR, PARTS, PARTS>(lds + buf * 2 * TILE, lds + buf * 2 * TILE + TILE, q, st, f, f_lo, scale.y,
+                                                                                       !whole(t0), t0, sinks);
+                }
+                if (NBUF == 1) __syncthreads();
+                if (i + 1 < i1) place(NBUF == 2 ? buf ^ 1 : 0);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st.acc[r][ct][i] *= CodeUnit<FM>::value;
+            }
+        }
+        // ---- open rows, in their own type, with the last split ----
+        const int t0 = 64 * full;
+        if (split == a.n_split - 1 && p_hi >= t0) {
+            const char* const open = a.c.open + (int64_t)stream * 2 * 64 * OPEN_ROWB;
+            __syncthreads();
+            fetch_rows<OPEN_ROWB, NW, false, TileType<DT>::bytes>(open, N - t0, lds);
+            fetch_rows<OPEN_ROWB, NW, true, TileType<DT>::bytes>(open + 64 * OPEN_ROWB, N - t0, lds + 64 * OPEN_ROWB);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (seen(t0)) {
+                QueryFrag<DT, D, NR, 1> q;
+                load_rows(q);
+                float f[NR], f_lo[NR];
+#pragma unroll
+                for (int r = 0; r < NR; ++r) { f[r] = kScaleHi; f_lo[r] = kScaleLo; }
+                prompt_tile<DT, false, true, DT == DT_F32, D, NR, 1, 1>(lds, lds + 64 * OPEN_ROWB, q, st, f, f_lo, 1.f, true, t0, sinks);
+            }
+        }
+    }
+    // ---- what the rows leave ----
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        float l = st.l[r];
+        {
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+            l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+        }
+        float m = st.m[r];
+        const int at = 32 * (NR * wave + r) + (lane & 31), row = row0 + at;
+        float by = 1.f;                                             // brings the weighted sum to 2^m
+        if (CODED) by = st.e[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e[r] - kShift - (m == -INFINITY ? 0.f : m));
+        if (row >= n_rows) continue;
+        if (a.n_split == 1) {
+            const float inv = by / l;
+            char* const o = static_cast<char*>(a.out) + query_row(r) * TileType<DT>::bytes;
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int ch = 32 * ct + 8 * x + 4 * hh;
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = st.acc[r][ct][4 * x + e] * inv;
+                    if constexpr (DT == DT_F32) {
+                        *reinterpret_cast<f32x4*>(o + ch * 4) = f32x4{y[0], y[1], y[2], y[3]};
+                    } else {
+                        using E = typename std::conditional<DT == DT_F16, _Float16, __bf16>::type;
+                        typedef E e4 __attribute__((ext_vector_type(4)));
+                        *reinterpret_cast<e4*>(o + ch * 2) = e4{(E)y[0], (E)y[1], (E)y[2], (E)y[3]};
+                    }
+                }
+            }
+            if (hh == 0 && a.lse) a.lse[query_row(r) / D] = (m + log2f(l)) * 0.69314718055994531f;
+        } else {
+            // (a maximum passes over NaN: a split of nothing but NaN would count as one without a key)
+            if (l != l) m = INFINITY;
+            const int64_t slot = ((int64_t)(stream * a.row_blocks + rb) * a.n_split + split) * ROWS + at;
+            float* const o = a.part_acc + slot * D;
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    *reinterpret_cast<f32x4*>(o + 32 * ct + 8 * x + 4 * hh) =
+                        f32x4{st.acc[r][ct][4 * x] * by, st.acc[r][ct][4 * x + 1] * by, st.acc[r][ct][4 * x + 2] * by, st.acc[r][ct][4 * x + 3] * by};
+            }
+            if (hh == 0) { a.part_lm[2 * slot] = l; a.part_lm[2 * slot + 1] = m; }
+        }
+    }
+}
+
+}  // namespace tka

@@ -18,9 +18,12 @@ OK, EINVAL, ECAPACITY, EUNSUPPORTED, EDEVICE, ENOMEM, ESCRATCH = range(7)
 F32, F16, BF16 = 0, 1, 2
 PATH_AUTO, PATH_FULL, PATH_FILTER, PATH_INDEX, PATH_PAGES = 0, 1, 2, 3, 4
 INDEX_NONE, INDEX_INT8, INDEX_PAGES, INDEX_BOXES = 0, 1, 2, 4
+CODED_INT8, CODED_E4M3 = 0, 1
 
 EXPORTS = [
     "topk_attn_kv_bytes", "topk_attn_workspace_bytes", "topk_attn_layers_workspace_bytes", "topk_attn_create", "topk_attn_append_kv", "topk_attn_append_step", "topk_attn_append_rotary",
+    "topk_attn_coded_kv_bytes", "topk_attn_coded_workspace_bytes", "topk_attn_coded_create", "topk_attn_coded_destroy", "topk_attn_coded_append", "topk_attn_coded_read",
+    "topk_attn_coded_decode", "topk_attn_coded_prompt", "topk_attn_coded_length", "topk_attn_coded_reset", "topk_attn_decode_sinks", "topk_attn_prompt",
     "topk_attn_decode_dense", "topk_attn_decode_blocks", "topk_attn_add_mass", "topk_attn_evict",
     "topk_attn_decode", "topk_attn_decode_static", "topk_attn_decode_window", "topk_attn_decode_multi", "topk_attn_decode_layers", "topk_attn_k_schedule", "topk_attn_scores", "topk_attn_length", "topk_attn_reset", "topk_attn_set_path",
     "topk_attn_last_fallbacks", "topk_attn_set_page_bound_scale", "topk_attn_last_pages_read", "topk_attn_last_selection_records", "topk_attn_debug_read_workspace", "topk_attn_debug_read_workspace_dims", "topk_attn_debug_force_redo", "topk_attn_set_scan_timing", "topk_attn_scan_time", "topk_attn_read_probe", "topk_attn_build_id", "topk_attn_strerror", "topk_attn_destroy",
@@ -43,6 +46,27 @@ class Config(ctypes.Structure):
         ("max_window", ctypes.c_int32),
         ("max_queries", ctypes.c_int32),
         ("index_kind", ctypes.c_int32),
+        ("kv_storage", ctypes.c_void_p),
+        ("kv_bytes", ctypes.c_size_t),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class CodedConfig(ctypes.Structure):
+    """Mirror of topk_attn_coded_config."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("n_layers", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("max_tokens", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("device", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
         ("kv_storage", ctypes.c_void_p),
         ("kv_bytes", ctypes.c_size_t),
         ("workspace", ctypes.c_void_p),
@@ -110,6 +134,31 @@ def lib() -> ctypes.CDLL:
         L.topk_attn_decode_dense.restype = i32
         L.topk_attn_decode_blocks.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp]
         L.topk_attn_decode_blocks.restype = i32
+        L.topk_attn_decode_sinks.argtypes = [vp, i32, vp, i64, i64, vp, vp, vp]
+        L.topk_attn_decode_sinks.restype = i32
+        L.topk_attn_prompt.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, vp, vp]
+        L.topk_attn_prompt.restype = i32
+        codedp = ctypes.POINTER(CodedConfig)
+        L.topk_attn_coded_kv_bytes.argtypes = [codedp]
+        L.topk_attn_coded_kv_bytes.restype = sz
+        L.topk_attn_coded_workspace_bytes.argtypes = [codedp]
+        L.topk_attn_coded_workspace_bytes.restype = sz
+        L.topk_attn_coded_create.argtypes = [codedp, ctypes.POINTER(vp)]
+        L.topk_attn_coded_create.restype = i32
+        L.topk_attn_coded_destroy.argtypes = [vp]
+        L.topk_attn_coded_destroy.restype = i32
+        L.topk_attn_coded_append.argtypes = [vp, i32, i32, vp, vp, i64, i64, i64, i64, vp]
+        L.topk_attn_coded_append.restype = i32
+        L.topk_attn_coded_read.argtypes = [vp, i32, i32, i64, i64, vp, vp, i64, i64, i64, vp]
+        L.topk_attn_coded_read.restype = i32
+        L.topk_attn_coded_decode.argtypes = [vp, i32, vp, i64, i64, vp, vp, vp]
+        L.topk_attn_coded_decode.restype = i32
+        L.topk_attn_coded_prompt.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, vp, vp]
+        L.topk_attn_coded_prompt.restype = i32
+        L.topk_attn_coded_length.argtypes = [vp, i32, i32]
+        L.topk_attn_coded_length.restype = i64
+        L.topk_attn_coded_reset.argtypes = [vp, i32, i32, vp]
+        L.topk_attn_coded_reset.restype = i32
         L.topk_attn_add_mass.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp]
         L.topk_attn_add_mass.restype = i32
         L.topk_attn_evict.argtypes = [vp, i32, vp, i64, i64, vp, vp]
@@ -238,6 +287,67 @@ def topk_attn_decode_blocks(h, layer, q_ptr, n_blocks, out_ptr, blocks_ptr=0, ls
                                          mass_ptr or None, stream), "topk_attn_decode_blocks")
 
 
+def topk_attn_decode_sinks(h, layer, q_ptr, sinks, window, out_ptr, lse_ptr=0, stream=0):
+    _check(lib().topk_attn_decode_sinks(h, layer, q_ptr, sinks, window, out_ptr, lse_ptr or None, stream), "topk_attn_decode_sinks")
+
+
+def topk_attn_prompt(h, layer, seq, q_ptr, n_queries, sinks, window, out_ptr, lse_ptr=0, stream=0):
+    """seq: a sequence, or -1 for all of the layer's."""
+    _check(lib().topk_attn_prompt(h, layer, seq, q_ptr, n_queries, sinks, window, out_ptr, lse_ptr or None, stream), "topk_attn_prompt")
+
+
+def make_coded_config(n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, dtype, format=CODED_INT8, device=0, kv_storage=0,
+                      kv_bytes=0, workspace=0, workspace_bytes=0) -> CodedConfig:
+    return CodedConfig(ctypes.sizeof(CodedConfig), n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, dtype, format, device, 0,
+                       kv_storage, kv_bytes, workspace, workspace_bytes)
+
+
+def topk_attn_coded_kv_bytes(cfg: CodedConfig) -> int:
+    return int(lib().topk_attn_coded_kv_bytes(ctypes.byref(cfg)))
+
+
+def topk_attn_coded_workspace_bytes(cfg: CodedConfig) -> int:
+    return int(lib().topk_attn_coded_workspace_bytes(ctypes.byref(cfg)))
+
+
+def topk_attn_coded_create(cfg: CodedConfig) -> int:
+    """Returns the opaque handle (an integer address); raises TopkAttnError."""
+    h = ctypes.c_void_p()
+    _check(lib().topk_attn_coded_create(ctypes.byref(cfg), ctypes.byref(h)), "topk_attn_coded_create")
+    return h.value
+
+
+def topk_attn_coded_destroy(h: int) -> None:
+    _check(lib().topk_attn_coded_destroy(h), "topk_attn_coded_destroy")
+
+
+def topk_attn_coded_append(h, layer, seq, k_ptr, v_ptr, n_new, seq_stride, token_stride, head_stride, stream=0):
+    _check(lib().topk_attn_coded_append(h, layer, seq, k_ptr, v_ptr, n_new, seq_stride, token_stride, head_stride, stream),
+           "topk_attn_coded_append")
+
+
+def topk_attn_coded_read(h, layer, seq, first, n, k_ptr, v_ptr, seq_stride, token_stride, head_stride, stream=0):
+    _check(lib().topk_attn_coded_read(h, layer, seq, first, n, k_ptr, v_ptr, seq_stride, token_stride, head_stride, stream),
+           "topk_attn_coded_read")
+
+
+def topk_attn_coded_decode(h, layer, q_ptr, sinks, window, out_ptr, lse_ptr=0, stream=0):
+    _check(lib().topk_attn_coded_decode(h, layer, q_ptr, sinks, window, out_ptr, lse_ptr or None, stream), "topk_attn_coded_decode")
+
+
+def topk_attn_coded_prompt(h, layer, seq, q_ptr, n_queries, sinks, window, out_ptr, lse_ptr=0, stream=0):
+    _check(lib().topk_attn_coded_prompt(h, layer, seq, q_ptr, n_queries, sinks, window, out_ptr, lse_ptr or None, stream),
+           "topk_attn_coded_prompt")
+
+
+def topk_attn_coded_length(h, layer, seq) -> int:
+    return int(lib().topk_attn_coded_length(h, layer, seq))
+
+
+def topk_attn_coded_reset(h, layer, seq=-1, stream=0):
+    _check(lib().topk_attn_coded_reset(h, layer, seq, stream), "topk_attn_coded_reset")
+
+
 def topk_attn_add_mass(h, layer, idx_ptr, vals_ptr, lse_ptr, k, mass_ptr, stream=0):
     _check(lib().topk_attn_add_mass(h, layer, idx_ptr, vals_ptr, lse_ptr, k, mass_ptr, stream), "topk_attn_add_mass")
 
@@ -360,7 +470,43 @@ def topk_attn_read_probe(src_ptr, nbytes, sink_ptr, stream=0):
 # --------------------------------------------------------------------------
 # Convenience owner of the torch allocations a handle borrows (marshalling only).
 # --------------------------------------------------------------------------
-class TopkAttnCache:
+ALL_TOKENS = (1 << 62)      # a window that leaves nothing out
+
+
+class _WindowAttention:
+    """Marshalling shared by the caches: single tokens and prompts over the first `sinks` and the newest `window` tokens (None: all).
+    Needs torch, device, dtype, h, n_seqs, n_q_heads, head_dim."""
+
+    def torch_dtype(self):
+        t = self.torch
+        return {F32: t.float32, F16: t.float16, BF16: t.bfloat16}[self.dtype]
+
+    def _stream(self) -> int:
+        # (the current stream's handle, without a Stream object around it: 1.9 us less per call)
+        return self.torch._C._cuda_getCurrentRawStream(self.device.index)
+
+    def _token(self, entry, layer, q, sinks, window, want_lse):
+        t = self.torch
+        assert q.device == self.device and q.is_contiguous() and q.dtype == self.torch_dtype()
+        assert q.shape == (self.n_seqs, self.n_q_heads, self.head_dim)
+        out = t.empty(q.shape, dtype=t.float32, device=self.device)
+        lse = t.empty(q.shape[:2], dtype=t.float32, device=self.device) if want_lse else None
+        entry(self.h, layer, q.data_ptr(), sinks, ALL_TOKENS if window is None else window, out.data_ptr(), lse.data_ptr() if want_lse else 0,
+              self._stream())
+        return out, lse
+
+    def _rows(self, entry, layer, q, sinks, window, seq, want_lse):
+        t = self.torch
+        assert q.device == self.device and q.is_contiguous() and q.dtype == self.torch_dtype() and q.dim() == 4
+        assert q.shape[0] == (self.n_seqs if seq < 0 else 1) and q.shape[2:] == (self.n_q_heads, self.head_dim)
+        out = t.empty_like(q)
+        lse = t.empty(q.shape[:3], dtype=t.float32, device=self.device) if want_lse else None
+        entry(self.h, layer, seq, q.data_ptr(), q.shape[1], sinks, ALL_TOKENS if window is None else window, out.data_ptr(),
+              lse.data_ptr() if want_lse else 0, self._stream())
+        return out, lse
+
+
+class TopkAttnCache(_WindowAttention):
     """Allocates kv_storage/workspace as torch tensors and wraps the handle.
 
     joined_layers: layers that topk_attn_decode_layers may let share their launches; the workspace grows in proportion.
@@ -371,7 +517,7 @@ class TopkAttnCache:
         import torch
         self.torch = torch
         self.shape = (n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, max_k, dtype)
-        self.dtype = dtype
+        self.n_seqs, self.n_q_heads, self.head_dim, self.dtype = n_seqs, n_q_heads, head_dim, dtype
         self.device = torch.device("cuda", device)
         cfg = make_config(n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, max_k, dtype, device,
                           max_window=max_window, max_queries=max_queries, index_kind=index_kind)
@@ -386,14 +532,6 @@ class TopkAttnCache:
         torch.cuda.synchronize(self.device)
         self.h = topk_attn_create(cfg)
         self.cfg = cfg
-
-    def torch_dtype(self):
-        t = self.torch
-        return {F32: t.float32, F16: t.float16, BF16: t.bfloat16}[self.dtype]
-
-    def _stream(self) -> int:
-        # (the current stream's handle, without a Stream object around it: 1.9 us less per call)
-        return self.torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def append(self, layer, seq, k_new, v_new, head_major=False):
         """k_new/v_new: [n, Hkv, d] (token-major) or [Hkv, n, d] (head_major) device tensors."""
@@ -463,6 +601,15 @@ class TopkAttnCache:
         topk_attn_decode_dense(self.h, layer, q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, self._mass_ptr(mass),
                                self._stream())
         return out, lse
+
+    def decode_sinks(self, layer, q, window, sinks=0, want_lse=True):
+        """q [B, Hq, d] -> (out, lse) over the first `sinks` and the newest `window` tokens."""
+        return self._token(topk_attn_decode_sinks, layer, q, sinks, window, want_lse)
+
+    def prompt(self, layer, q, window=None, sinks=0, seq=-1, want_lse=True):
+        """q [S, M, Hq, d], the last M cached tokens' queries -> (out [S, M, Hq, d] in the cache dtype, lse [S, M, Hq]): each token over those up to
+        itself that are among its newest `window` (None: all) or the first `sinks`.  All sequences of the layer, or `seq` (S = 1)."""
+        return self._rows(topk_attn_prompt, layer, q, sinks, window, seq, want_lse)
 
     def decode_blocks(self, layer, q, n_blocks, want_blocks=True, want_lse=True, mass=None):
         """q [B, Hq, d] -> (out, blocks [B, Hkv, n_blocks], lse) over the n_blocks best pages of each KV head (index_kind INDEX_BOXES)."""
@@ -548,6 +695,74 @@ class TopkAttnCache:
         if self.h:
             self.torch.cuda.synchronize(self.device)
             topk_attn_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class TopkAttnCodedCache(_WindowAttention):
+    """A cache whose rows are held in 8 bits (format CODED_INT8 or CODED_E4M3): owner of the torch allocations its handle borrows."""
+
+    def __init__(self, n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, dtype, format=CODED_INT8, device=0):
+        import torch
+        self.torch = torch
+        self.n_seqs, self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype = n_seqs, n_q_heads, n_kv_heads, head_dim, dtype
+        self.device = torch.device("cuda", device)
+        cfg = make_coded_config(n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, dtype, format, device)
+        kvb, wsb = topk_attn_coded_kv_bytes(cfg), topk_attn_coded_workspace_bytes(cfg)
+        if kvb == 0 or wsb == 0:
+            h = ctypes.c_void_p()
+            _check(lib().topk_attn_coded_create(ctypes.byref(cfg), ctypes.byref(h)), "topk_attn_coded_create")
+        self.kv = torch.empty(kvb, dtype=torch.uint8, device=self.device)
+        self.ws = torch.empty(wsb, dtype=torch.uint8, device=self.device)
+        cfg.kv_storage, cfg.kv_bytes = self.kv.data_ptr(), kvb
+        cfg.workspace, cfg.workspace_bytes = self.ws.data_ptr(), wsb
+        torch.cuda.synchronize(self.device)
+        self.h = topk_attn_coded_create(cfg)
+        self.cfg = cfg
+
+    def append(self, layer, k_new, v_new, seq=-1):
+        """k_new/v_new: [S, n, Hkv, d] device tensors, strided alike in any order (rows of a head together): n tokens for all sequences of the layer, or
+        for `seq` (S = 1)."""
+        assert k_new.device == self.device and v_new.device == self.device and k_new.dtype == v_new.dtype == self.torch_dtype()
+        S, n, heads, d = k_new.shape
+        assert (heads, d) == (self.n_kv_heads, self.head_dim) and S == (self.n_seqs if seq < 0 else 1) and v_new.shape == k_new.shape
+        # (of one sequence, token or head: any stride)
+        (ks, kt, kh, kc), (vs, vt, vh, vc) = (tuple(st if m > 1 else 0 for st, m in zip(x.stride(), x.shape)) for x in (k_new, v_new))
+        assert kc == vc == 1 and (ks, kt, kh) == (vs, vt, vh)
+        topk_attn_coded_append(self.h, layer, seq, k_new.data_ptr(), v_new.data_ptr(), n, ks, kt, kh, self._stream())
+
+    def read(self, layer, first, n, seq=-1):
+        """-> k, v [S, n, Hkv, d]: rows [first, first + n) as they read, of all sequences of the layer or of `seq` (S = 1)."""
+        t = self.torch
+        k, v = (t.empty((self.n_seqs if seq < 0 else 1, max(n, 0), self.n_kv_heads, self.head_dim), dtype=self.torch_dtype(), device=self.device)
+                for _ in range(2))
+        row = self.n_kv_heads * self.head_dim
+        topk_attn_coded_read(self.h, layer, seq, first, n, k.data_ptr(), v.data_ptr(), max(n, 0) * row, row, self.head_dim, self._stream())
+        return k, v
+
+    def decode(self, layer, q, window=None, sinks=0, want_lse=True):
+        """q [B, Hq, d] -> (out fp32, lse) over all tokens, or the first `sinks` and the newest `window`."""
+        return self._token(topk_attn_coded_decode, layer, q, sinks, window, want_lse)
+
+    def prompt(self, layer, q, window=None, sinks=0, seq=-1, want_lse=True):
+        """As TopkAttnCache.prompt."""
+        return self._rows(topk_attn_coded_prompt, layer, q, sinks, window, seq, want_lse)
+
+    def length(self, layer, seq) -> int:
+        return topk_attn_coded_length(self.h, layer, seq)
+
+    def reset(self, layer, seq=-1):
+        topk_attn_coded_reset(self.h, layer, seq, self._stream())
+
+    def close(self):
+        if self.h:
+            self.torch.cuda.synchronize(self.device)
+            topk_attn_coded_destroy(self.h)
             self.h = None
 
     def __del__(self):

@@ -1,0 +1,546 @@
+"""The cache held in 8 bits on the GPU, through the binding, against oracle/coded_cache_ref.py in 64 bits: rows coded and read back, single tokens and
+chunks of a prompt attending them."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import helpers as H
+from oracle import coded_cache_ref as ref
+from paper_2502_06766_amd import topk_attn as ta
+from paper_2502_06766_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda", 0) if torch.cuda.is_available() else None
+U = 2.0 ** -24                                                   # half a step of fp32 relative to the value
+HALF = {wl.F32: 2.0 ** -24, wl.F16: 2.0 ** -11, wl.BF16: 2.0 ** -8}
+FORMATS = [ta.CODED_INT8, ta.CODED_E4M3]
+TYPES = [wl.F32, wl.F16, wl.BF16]
+
+
+def draw(g, *shape, dtype, size=1.0):
+    return wl.quantize((size * g.standard_normal(shape)).astype(np.float32), dtype)
+
+
+def up(x, dtype):
+    return H.to_torch(x, dtype, DEV)
+
+
+def filled(lens, Hq, Hkv, d, cap, dtype, fmt, seed=0, layers=1, layer=0, rows=None):
+    """A coded cache whose storage and scratch were NaN and -1, sequence b holding lens[b] tokens -> cache, K, V as given and as held, per sequence."""
+    g = np.random.default_rng(seed)
+    cache = ta.TopkAttnCodedCache(layers, len(lens), Hq, Hkv, d, cap, dtype, format=fmt)
+    cache.kv.fill_(255)
+    got = []
+    for b, n in enumerate(lens):
+        K, V = (draw(g, Hkv, n, d, dtype=dtype) for _ in range(2)) if rows is None else rows[b]
+        if n:
+            cache.append(layer, up(K, dtype).transpose(0, 1)[None], up(V, dtype).transpose(0, 1)[None], seq=b)
+        K, V = wl.widen(K, dtype).astype(np.float64), wl.widen(V, dtype).astype(np.float64)
+        got.append((K, V, np.stack([ref.held(K[h], fmt) for h in range(Hkv)]), np.stack([ref.held(V[h], fmt) for h in range(Hkv)])))
+    return cache, got
+
+
+def rounded(x, dtype):
+    """x in 64 bits, rounded once to the type."""
+    if dtype == wl.BF16:
+        # (a code times a scale of 16 bits has 24: the conversion to 32 bits is exact)
+        return wl.widen(wl.to_bf16_bits(x.astype(np.float32)), dtype)
+    return x.astype(np.float16 if dtype == wl.F16 else np.float32).astype(np.float32)
+
+
+# ---- rows in and out ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,Hkv,d,n", [(wl.F16, 2, 32, 1), (wl.BF16, 1, 64, 64), (wl.F32, 2, 32, 65), (wl.BF16, 3, 128, 63), (wl.F16, 1, 256, 200),
+                                           (wl.F32, 2, 256, 129), (wl.F16, 2, 128, 640), (wl.F32, 1, 64, 128), (wl.BF16, 5, 32, 321)])
+def test_rows_read_as_the_nearest_codes(dtype, Hkv, d, n, fmt):
+    cache, got = filled([n], Hkv, Hkv, d, n, dtype, fmt, seed=n)
+    try:
+        k, v = cache.read(0, 0, n)
+        for x, want in ((k, got[0][2]), (v, got[0][3])):
+            np.testing.assert_array_equal(x[0].transpose(0, 1).float().cpu().numpy(), rounded(want, dtype))
+        first = n // 3
+        k, v = cache.read(0, first, n - first - n // 5, seq=0)
+        np.testing.assert_array_equal(k[0].transpose(0, 1).float().cpu().numpy(), rounded(got[0][2], dtype)[:, first:n - n // 5])
+        np.testing.assert_array_equal(v[0].transpose(0, 1).float().cpu().numpy(), rounded(got[0][3], dtype)[:, first:n - n // 5])
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_at_the_borders_between_codes(dtype, fmt):
+    """Quotients x / scale at, just below and just above halves: the scale is exact (amax = 127 s, 448 s), the rows hold halves of the codes' steps
+    and their neighbours in the type."""
+    d, n = 32, 64
+    codes = np.arange(-127, 127) + 0.5 if fmt == ta.CODED_INT8 else np.array([s * (m + 0.5) * 2.0 ** (e - 3) for e in range(-6, 9) for m in range(8, 16) for s in (-1, 1)])
+    codes = codes[np.abs(codes) < (127 if fmt == ta.CODED_INT8 else 448)]
+    x = wl.widen(wl.quantize(codes.astype(np.float32), dtype), dtype)
+    eps = {wl.F32: 2.0 ** -23, wl.F16: 2.0 ** -10, wl.BF16: 2.0 ** -7}[dtype]
+    rows = np.concatenate([x, wl.widen(wl.quantize((x * (1 + eps)).astype(np.float32), dtype), dtype), wl.widen(wl.quantize((x * (1 - eps)).astype(np.float32), dtype), dtype)])
+    flat = np.zeros(n * d, np.float32)
+    flat[0] = 127.0 if fmt == ta.CODED_INT8 else 448.0
+    flat[1:1 + rows.size] = np.clip(rows[:n * d - 1], -flat[0], flat[0])
+    for scale in (1.0, 2.0 ** -20 if dtype != wl.F16 else 2.0 ** -5):
+        K = wl.quantize((flat * scale).reshape(1, n, d), dtype)
+        V = K[:, ::-1].copy()
+        cache, got = filled([n], 1, 1, d, n, dtype, fmt, rows=[(K, V)])
+        try:
+            k, v = cache.read(0, 0, n)
+            np.testing.assert_array_equal(k[0, :, 0].float().cpu().numpy(), rounded(got[0][2][0], dtype))
+            np.testing.assert_array_equal(v[0, :, 0].float().cpu().numpy(), rounded(got[0][3][0], dtype))
+        finally:
+            cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_unusual_blocks(fmt):
+    """Zeros, the smallest and the largest numbers, infinities and NaN: the scale's edges; a block with no number for one element reads as none for all,
+    its neighbours do not notice."""
+    d, dtype = 64, wl.F32
+    g = np.random.default_rng(3)
+    kinds = [0.0, 3.4028234e38, 1e-45, 2.0 ** -101, 2.0 ** -100, 1e-30, 1e30, 3.4e38, np.inf, np.nan, 1.0]
+    K = np.concatenate([g.uniform(-1, 1, (1, 64, d)) for _ in kinds], 1).astype(np.float32)
+    for i, x in enumerate(kinds):
+        if np.isfinite(x):
+            K[0, 64 * i:64 * i + 64] *= np.float32(x)
+            K[0, 64 * i + 5, 7] = x
+        else:
+            K[0, 64 * i + 63, d - 1] = x if i % 2 else -x
+    n = K.shape[1]
+    cache, got = filled([n], 1, 1, d, n, dtype, fmt, rows=[(K, K[:, ::-1].copy())])
+    try:
+        k, v = cache.read(0, 0, n)
+        np.testing.assert_array_equal(k[0, :, 0].cpu().numpy(), got[0][2][0].astype(np.float32))
+        np.testing.assert_array_equal(v[0, :, 0].cpu().numpy(), got[0][3][0].astype(np.float32))
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_is_held_does_not_depend_on_how_it_came(dtype, fmt):
+    """One call, one token at a time, odd chunks, a fused projection's views, another cache's heads, all sequences or each alone: the same bytes."""
+    B, Hkv, d, n = 3, 2, 64, 203
+    g = np.random.default_rng(9)
+    K, V = (up(draw(g, B, n, Hkv, d, dtype=dtype), dtype) for _ in range(2))
+    fused = torch.cat([torch.full_like(K, float("nan")), K, V], 2)
+    ways = {
+        "at once": lambda c: c.append(0, K, V),
+        "token by token": lambda c: [c.append(0, K[:, t:t + 1], V[:, t:t + 1]) for t in range(n)],
+        "chunks": lambda c: [c.append(0, K[:, a:b], V[:, a:b]) for a, b in ((0, 1), (1, 64), (64, 64), (64, 191), (191, 192), (192, n))],
+        "views": lambda c: [c.append(0, fused[:, a:b, Hkv:2 * Hkv], fused[:, a:b, 2 * Hkv:]) for a, b in ((0, 70), (70, n))],
+        "heads": lambda c: [c.append(0, *(x.transpose(1, 2).contiguous().transpose(1, 2)[:, a:b] for x in (K, V))) for a, b in ((0, 100), (100, n))],
+        "alone": lambda c: [c.append(0, K[b:b + 1], V[b:b + 1], seq=b) for b in (2, 0, 1)],
+    }
+    want = None
+    for name, way in ways.items():
+        cache = ta.TopkAttnCodedCache(2, B, Hkv, Hkv, d, 256, dtype, format=fmt)
+        try:
+            cache.kv.zero_()
+            way(cache)
+            rows = cache.read(0, 0, n)
+            if want is None:
+                want = rows
+                held = cache.kv.clone()
+            assert all(torch.equal(a, b) for a, b in zip(rows, want)), name
+            codes = 2 * 2 * B * Hkv * 4 * 64 * d + 2 * B * Hkv * 4 * 8                # (both layers' codes and scales)
+            assert torch.equal(cache.kv[:codes], held[:codes]), name
+            assert [cache.length(0, b) for b in range(B)] == [n] * B and cache.length(1, 0) == 0
+        finally:
+            cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sequences_of_different_length_grow_together(fmt):
+    """Open blocks at every fill, 70 sequences (more than a launch takes), blocks closing in some of them; reset of one and of all."""
+    B, Hkv, d, dtype = 70, 1, 32, wl.BF16
+    g = np.random.default_rng(21)
+    lens = [(7 * b) % 67 for b in range(B)]
+    cache, got = filled(lens, 1, Hkv, d, 200, dtype, fmt, seed=4)
+    try:
+        K, V = (draw(g, B, 5, Hkv, d, dtype=dtype) for _ in range(2))
+        cache.append(0, up(K, dtype), up(V, dtype))
+        for b in range(B):
+            k, v = cache.read(0, 0, lens[b] + 5, seq=b)
+            for x, old, new in ((k, got[b][0], K[b]), (v, got[b][1], V[b])):
+                whole = np.concatenate([old[0], wl.widen(new, dtype)[:, 0]])
+                np.testing.assert_array_equal(x[0, :, 0].float().cpu().numpy(), rounded(ref.held(whole, fmt), dtype), err_msg=str(b))
+        cache.reset(0, 3)
+        assert cache.length(0, 3) == 0 and cache.length(0, 4) == lens[4] + 5
+        cache.append(0, up(K, dtype)[3:4], up(V, dtype)[3:4], seq=3)
+        assert torch.equal(cache.read(0, 0, 5, seq=3)[0][0], up(K, dtype)[3])
+        cache.reset(0)
+        assert all(cache.length(0, b) == 0 for b in range(B))
+    finally:
+        cache.close()
+
+
+def test_read_leaves_what_it_does_not_own():
+    """Strided destinations, ranges that begin and end inside blocks: rows and columns beside them stay."""
+    d, dtype, Hkv, n = 64, wl.F16, 2, 150
+    cache, got = filled([n, n], Hkv, Hkv, d, n, dtype, ta.CODED_INT8)
+    try:
+        for first, m in ((0, 1), (63, 2), (64, 64), (10, 140), (128, 22)):
+            k, v = (torch.full((2, m + 2, Hkv + 1, d), 7.0, dtype=torch.float16, device=DEV) for _ in range(2))
+            ta.topk_attn_coded_read(cache.h, 0, -1, first, m, k[:, 1:].data_ptr(), v[:, 1:].data_ptr(), (m + 2) * (Hkv + 1) * d, (Hkv + 1) * d, d)
+            torch.cuda.synchronize()
+            for b in range(2):
+                np.testing.assert_array_equal(k[b, 1:-1, :Hkv].transpose(0, 1).float().cpu().numpy(), rounded(got[b][2], dtype)[:, first:first + m])
+                np.testing.assert_array_equal(v[b, 1:-1, :Hkv].transpose(0, 1).float().cpu().numpy(), rounded(got[b][3], dtype)[:, first:first + m])
+            for x in (k, v):
+                assert (x[:, 0] == 7).all() and (x[:, -1] == 7).all() and (x[:, :, Hkv] == 7).all()
+    finally:
+        cache.close()
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------
+def weight_error(q, K, d):
+    """Bound of a softmax weight's relative error before normalisation: the score's sum of d products in 32 bits (d u sum |q k|; fp32 queries are
+    two fp16 parts, 2^-23 more of a product), the roundings of its factor and of the difference to the maximum (4 u of the largest exponent),
+    the exponential (2 u), the value scale (2 u), and what two fp16 parts of a weight leave (2^-22)."""
+    Hkv = K.shape[0]
+    rows = q.reshape(-1, Hkv, q.shape[-2] // Hkv, d)
+    A = max((np.abs(K[h]) @ np.abs(rows[:, h].reshape(-1, d)).T).max() for h in range(Hkv)) / np.sqrt(d)
+    return (d + 10) * U * A + 4 * U + 2.0 ** -22
+
+
+def check_token(out, lse, q, K, V, sinks, window, label):
+    d, n = q.shape[-1], K.shape[1]
+    w_out, w_lse = ref.attend(q[None], K, V, sinks, window)
+    dw, sums = weight_error(q, K, d), (min(n, 4 * 64 * 4) / 16 + 64) * U
+    tol = 2 * (dw + sums) * np.abs(V).max()
+    off = np.abs(out - w_out[0]).max()
+    assert off <= tol, f"{label}: out off by {off:.3g}, {tol:.3g} allowed"
+    off, tol = np.abs(lse - w_lse[0]).max(), dw + sums + 4 * U * np.abs(w_lse).max()
+    assert off <= tol, f"{label}: lse off by {off:.3g}, {tol:.3g} allowed"
+
+
+DECODE = [  # dtype, Hq, Hkv, d, lens, cap, (sinks, window)
+    (wl.BF16, 4, 1, 64, [1], 1, (0, 0)),
+    (wl.F16, 8, 2, 128, [63, 64, 65], 70, (0, 0)),
+    (wl.BF16, 5, 1, 32, [64, 128, 31, 300], 300, (0, 0)),
+    (wl.F32, 8, 2, 64, [200, 1, 129], 203, (0, 0)),
+    (wl.F32, 16, 1, 256, [77, 448], 448, (0, 0)),
+    (wl.F32, 3, 3, 128, [1000], 1001, (3, 200)),
+    (wl.F16, 17, 1, 256, [130, 700], 700, (0, 0)),
+    (wl.BF16, 128, 1, 128, [1500], 1601, (0, 0)),
+    (wl.F16, 80, 2, 64, [300, 129, 5], 301, (70, 33)),
+    (wl.BF16, 32, 8, 128, [4097], 4100, (0, 0)),
+    (wl.F16, 4, 1, 128, [70001], 70001, (0, 0)),
+    (wl.F16, 6, 2, 32, [40007, 39999], 40010, (5, 20000)),
+    (wl.BF16, 4, 2, 64, [500, 499, 512], 520, (1, 1)),
+    (wl.BF16, 4, 2, 64, [500, 499, 512], 520, (0, 64)),
+    (wl.F16, 4, 2, 128, [640, 641, 703], 720, (64, 65)),
+    (wl.F16, 4, 2, 128, [640, 641, 703], 720, (600, 50)),
+    (wl.F32, 4, 2, 32, [640, 10, 703], 720, (690, 13)),
+]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,lens,cap,mask", DECODE)
+def test_decode(dtype, Hq, Hkv, d, lens, cap, mask, fmt):
+    cache, got = filled(lens, Hq, Hkv, d, cap, dtype, fmt, seed=cap)
+    try:
+        q = draw(np.random.default_rng(cap + 1), len(lens), Hq, d, dtype=dtype)
+        sinks, window = mask if mask[1] else (0, None)
+        out, lse = cache.decode(0, up(q, dtype), window=window, sinks=sinks)
+        for b, n in enumerate(lens):
+            check_token(out[b].cpu().numpy(), lse[b].cpu().numpy(), wl.widen(q[b], dtype).astype(np.float64), got[b][2], got[b][3], sinks, window or n,
+                        f"sequence {b} ({n} tokens)")
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
+def test_blocks_of_very_different_scales(dtype, fmt):
+    """Keys and values whose blocks differ by powers of two up to 2^60, the large values where the weights are small and the other way round."""
+    d, n, Hq = 64, 64 * 9 + 10, 4
+    g = np.random.default_rng(8)
+    for kind in range(3):
+        K, V = g.standard_normal((1, n, d)), g.standard_normal((1, n, d))
+        K[0, :, 0] = 0.0
+        for p in range(9):
+            rows = slice(64 * p, 64 * p + 64)
+            V[0, rows] *= 2.0 ** {0: 10 * p - 30, 1: -10 * p + 30, 2: (-1) ** p * 20}[kind]
+            K[0, rows] *= {0: 1.0, 1: 2.0 ** -p, 2: 2.0 ** (p - 6)}[kind]
+            K[0, rows, 0] = {0: -5.0 * p, 1: 5.0 * p, 2: 0.0}[kind]
+        K[0, 64 * 3:64 * 4] = 0.0
+        V[0, 64 * 5:64 * 6] = 0.0
+        rows = tuple(wl.quantize(x.astype(np.float32), dtype) for x in (K, V))
+        q = g.standard_normal((1, Hq, d)).astype(np.float32)
+        q[..., 0] = 8.0
+        q = wl.quantize(q, dtype)
+        cache, got = filled([n], Hq, 1, d, n, dtype, fmt, rows=[rows])
+        try:
+            out, lse = cache.decode(0, up(q, dtype))
+            q64, Kh, Vh = wl.widen(q[0], dtype).astype(np.float64), got[0][2], got[0][3]
+            s = q64 @ Kh[0].T / 8.0
+            w = np.exp(s - s.max(1, keepdims=True))
+            w /= w.sum(1, keepdims=True)
+            # every element against the sum of the magnitudes it is made of
+            size = w @ np.abs(Vh[0])
+            tol = (2 * weight_error(q64, Kh, d) + 200 * U) * size
+            off = np.abs(out[0].cpu().numpy() - w @ Vh[0])
+            assert (off <= tol).all(), f"kind {kind}: {np.max(off / size):.3g} of the magnitudes, {np.max(tol / size):.3g} allowed"
+        finally:
+            cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sums_of_many_equal_weights(fmt):
+    """131072 equal keys: a weight that does not end in 32 bits, added up without drift."""
+    d, n, dtype = 64, 131072, wl.F16
+    K, V = np.zeros((1, n, d), np.float16), np.zeros((1, n, d), np.float16)
+    K[0, :, 0] = 1.0
+    V[0, :, 1:] = np.float16(1.0) * (np.arange(n) % 3 == 0)[:, None]
+    V[0, :, 0] = 1.0
+    cache, got = filled([n], 1, 1, d, n, dtype, fmt, rows=[(K, V)])
+    try:
+        q = np.zeros((1, 1, d), np.float16)
+        q[0, 0, 0] = 2.7
+        out, lse = cache.decode(0, up(q, dtype))
+        w_out, w_lse = ref.attend(q.astype(np.float64), got[0][2], got[0][3], 0, n)
+        # additions that follow each other: 16 of a block, 64 blocks of a wave (compensated, twice that for the products), waves, splits
+        assert np.abs(out[0].cpu().numpy() - w_out[0]).max() <= (4 * 64 + 2 * 64 + 20) * U
+        assert np.abs(lse[0].cpu().numpy() - w_lse[0]).max() <= 64 * U + 4 * U * w_lse.max()
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_is_not_seen_has_no_effect(dtype, fmt):
+    """NaN and infinities outside the window, in blocks of their own, in the open rows and behind the sequence: the others' results as without them; a
+    block with one that is seen makes the heads NaN."""
+    d, Hq, n = 64, 4, 300
+    g = np.random.default_rng(2)
+    K, V = (draw(g, 1, n, d, dtype=dtype) for _ in range(2))
+    clean, _ = filled([n], Hq, 1, d, n, dtype, fmt, rows=[(K, V)])
+    Kb, Vb = K.copy(), V.copy()
+    bad = wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    for t, kind in ((0, 0), (70, 1), (130, 2), (257, 0), (270, 0)):
+        Kb[0, t, 3], Vb[0, t, 5] = bad[kind], bad[(kind + 1) % 3]
+    dirty, _ = filled([n], Hq, 1, d, n, dtype, fmt, rows=[(Kb, Vb)])
+    try:
+        q = up(draw(g, 1, Hq, d, dtype=dtype), dtype)
+        for window in (1, 29):                                     # of the open rows [256, 300)
+            a, b = clean.decode(0, q, window=window), dirty.decode(0, q, window=window)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), window
+        assert torch.isnan(dirty.decode(0, q, window=60)[0]).all()
+        assert torch.isnan(dirty.decode(0, q, window=29, sinks=1)[0]).all()
+        assert torch.isnan(dirty.decode(0, q)[0]).all()
+    finally:
+        clean.close()
+        dirty.close()
+
+
+# ---- prompts over the coded cache ------------------------------------------------------------------------------------
+def check_rows(out, lse, q, K, V, sinks, window, dtype, label):
+    d, n = q.shape[-1], K.shape[1]
+    w_out, w_lse = ref.attend(q, K, V, sinks, window)
+    # a weight's rounding (to fp16, over the open rows to their type), the output's to its own; the sums
+    dw, sums = weight_error(q, K, d) + (0 if dtype == wl.F32 else HALF[dtype]), (n / 16 + 64) * U
+    tol = 2 * (dw + sums) * np.abs(V).max() + HALF[dtype] * np.abs(w_out)
+    off = np.abs(out - w_out)
+    assert (off <= tol).all(), f"{label}: out off by {off.max():.3g}, {(off - tol).max():.3g} beyond what is allowed"
+    off, tol = np.abs(lse - w_lse).max(), weight_error(q, K, d) + sums + 4 * U * np.abs(w_lse).max()
+    assert off <= tol, f"{label}: lse off by {off:.3g}, {tol:.3g} allowed"
+
+
+PROMPT = [  # dtype, Hq, Hkv, d, lens, M, (sinks, window)
+    (wl.BF16, 4, 2, 64, [70], 70, (0, 0)),
+    (wl.F16, 4, 1, 128, [1], 1, (0, 0)),
+    (wl.F16, 8, 2, 128, [200, 333], 7, (0, 0)),
+    (wl.BF16, 5, 1, 32, [150, 129, 128], 100, (0, 0)),
+    (wl.F32, 2, 2, 64, [140, 192], 131, (4, 50)),
+    (wl.F32, 4, 1, 256, [130], 70, (0, 0)),
+    (wl.F32, 6, 2, 128, [190], 40, (0, 0)),
+    (wl.F16, 3, 1, 256, [320, 257], 257, (0, 64)),
+    (wl.BF16, 16, 1, 128, [700], 130, (10, 100)),
+    (wl.BF16, 32, 8, 128, [600, 640], 600, (0, 0)),
+    (wl.F16, 28, 4, 64, [1000], 500, (65, 128)),
+    (wl.BF16, 4, 2, 32, [3000], 3, (0, 0)),
+    (wl.F16, 1, 1, 32, [515], 515, (0, 1)),
+]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,lens,M,mask", PROMPT)
+def test_prompt(dtype, Hq, Hkv, d, lens, M, mask, fmt):
+    cache, got = filled(lens, Hq, Hkv, d, max(lens) + 1, dtype, fmt, seed=M)
+    try:
+        q = draw(np.random.default_rng(M + 1), len(lens), M, Hq, d, dtype=dtype)
+        sinks, window = mask if mask[1] else (0, None)
+        out, lse = cache.prompt(0, up(q, dtype), window=window, sinks=sinks)
+        for b, n in enumerate(lens):
+            check_rows(out[b].float().cpu().numpy(), lse[b].cpu().numpy(), wl.widen(q[b], dtype).astype(np.float64), got[b][2], got[b][3], sinks, window or n, dtype,
+                       f"sequence {b} ({n} tokens)")
+        out, lse = cache.prompt(0, up(q, dtype)[-1:], window=window, sinks=sinks, seq=len(lens) - 1)
+        check_rows(out[0].float().cpu().numpy(), lse[0].cpu().numpy(), wl.widen(q[-1], dtype).astype(np.float64), got[-1][2], got[-1][3], sinks, window or lens[-1],
+                   dtype, "the last sequence alone")
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_prompt_rows_do_not_notice_what_they_do_not_see(dtype, fmt):
+    d, Hq, n = 64, 4, 300
+    g = np.random.default_rng(2)
+    K, V = (draw(g, 1, n, d, dtype=dtype) for _ in range(2))
+    Kb, Vb = K.copy(), V.copy()
+    bad = wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    Kb[0, 100, 3], Vb[0, 110, 5], Vb[0, 280, 5], Vb[0, 281, 6], Kb[0, 290, 9] = bad[[0, 1, 2, 1, 0]]
+    clean, _ = filled([n], Hq, 1, d, n, dtype, fmt, rows=[(K, V)])
+    dirty, _ = filled([n], Hq, 1, d, n, dtype, fmt, rows=[(Kb, Vb)])
+    try:
+        q = up(draw(g, 1, n, Hq, d, dtype=dtype), dtype)
+        for sinks, window in ((0, 20), (0, None), (3, 40)):
+            a, b = (c.prompt(0, q, window=window, sinks=sinks) for c in (clean, dirty))
+            see = torch.from_numpy(ref.seen(n, n, sinks, window or n)).to(DEV)
+            touched = see[:, 64:128].any(1) | see[:, 280] | see[:, 281] | see[:, 290]
+            assert torch.equal(a[0][0][~touched], b[0][0][~touched]) and torch.equal(a[1][0][~touched], b[1][0][~touched])
+            block = see[:, 64:128].any(1) | see[:, 290]
+            assert torch.isnan(b[0][0][block]).all()
+            only = touched & ~block                                 # values 280, 281 alone: channels 5 and 6
+            if only.any():
+                rest = [c for c in range(d) if c not in (5, 6)]
+                assert not torch.isfinite(b[0][0][only & see[:, 280]][..., 5].float()).any()
+                assert torch.isfinite(b[0][0][only][..., rest].float()).all()
+    finally:
+        clean.close()
+        dirty.close()
+
+
+# ---- together, replayed, side by side --------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_prompt_in_chunks_and_steps_behind_it(fmt):
+    """As a program uses it: a prompt appended and attended chunk by chunk, then tokens one at a time; the chunks' results are the whole prompt's."""
+    B, Hq, Hkv, d, dtype, n, steps = 2, 8, 2, 64, wl.BF16, 150, 70
+    g = np.random.default_rng(12)
+    K, V = (draw(g, B, n + steps, Hkv, d, dtype=dtype) for _ in range(2))
+    q = draw(g, B, n + steps, Hq, d, dtype=dtype)
+    Kt, Vt, qt = up(K, dtype), up(V, dtype), up(q, dtype)
+    cache = ta.TopkAttnCodedCache(2, B, Hq, Hkv, d, n + steps, dtype, format=fmt)
+    try:
+        for layer in (1, 0):
+            outs, at = [], 0
+            for end in (64, 100, n):
+                cache.append(layer, Kt[:, at:end], Vt[:, at:end])
+                outs.append(cache.prompt(layer, qt[:, at:end].contiguous(), window=40, sinks=2))
+                for b in range(B):
+                    Kw, Vw = (wl.widen(x[b, :end], dtype).astype(np.float64).transpose(1, 0, 2) for x in (K, V))
+                    Kh, Vh = (np.stack([ref.held(x[h], fmt) for h in range(Hkv)]) for x in (Kw, Vw))
+                    check_rows(outs[-1][0][b].float().cpu().numpy(), outs[-1][1][b].cpu().numpy(), wl.widen(q[b, at:end], dtype).astype(np.float64), Kh, Vh, 2, 40,
+                               dtype, f"layer {layer}, tokens {at} to {end}")
+                at = end
+            for t in range(n, n + steps):
+                cache.append(layer, Kt[:, t:t + 1], Vt[:, t:t + 1])
+                out, lse = cache.decode(layer, qt[:, t].contiguous())
+                if t in (n, 191, 192, n + steps - 1):
+                    for b in range(B):
+                        Kw, Vw = (wl.widen(x[b, :t + 1], dtype).astype(np.float64).transpose(1, 0, 2) for x in (K, V))
+                        Kh, Vh = (np.stack([ref.held(x[h], fmt) for h in range(Hkv)]) for x in (Kw, Vw))
+                        check_token(out[b].cpu().numpy(), lse[b].cpu().numpy(), wl.widen(q[b, t], dtype).astype(np.float64), Kh, Vh, 0, t + 1, f"step {t}")
+    finally:
+        cache.close()
+
+
+def test_captured_calls_replay():
+    """Decode, prompt and read in a graph, replayed with other queries and with eager calls of the same handle between."""
+    Hq, Hkv, d, dtype, n, M = 8, 2, 128, wl.F16, 5000, 9
+    cache, _ = filled([n, n - 33], Hq, Hkv, d, n, dtype, ta.CODED_INT8)
+    g = np.random.default_rng(1)
+    try:
+        q, qm = up(draw(g, 2, Hq, d, dtype=dtype), dtype), up(draw(g, 2, M, Hq, d, dtype=dtype), dtype)
+
+        def calls():
+            return (*cache.decode(0, q), *cache.decode(0, q, window=100, sinks=4), *cache.prompt(0, qm), *cache.read(0, 100, 300))
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            calls()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = calls()
+        for _ in range(4):
+            q.copy_(up(draw(g, 2, Hq, d, dtype=dtype), dtype))
+            qm.copy_(up(draw(g, 2, M, Hq, d, dtype=dtype), dtype))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [x.clone() for x in outs]
+            for a, b in zip(got, calls()):
+                assert torch.equal(a, b)
+    finally:
+        cache.close()
+
+
+def test_two_handles_on_two_streams():
+    Hq, Hkv, d, dtype = 8, 2, 64, wl.BF16
+    caches = [filled([9000 - 100 * i], Hq, Hkv, d, 9000, dtype, ta.CODED_E4M3, seed=i)[0] for i in range(2)]
+    g = np.random.default_rng(5)
+    try:
+        qs = [up(draw(g, 1, Hq, d, dtype=dtype), dtype) for _ in caches]
+        want = [c.decode(0, q) for c, q in zip(caches, qs)]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in caches]
+        for _ in range(20):
+            got = []
+            for c, q, s in zip(caches, qs, streams):
+                with torch.cuda.stream(s):
+                    got.append(c.decode(0, q))
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for a, b in zip(want, got) for x, y in zip(a, b))
+    finally:
+        for c in caches:
+            c.close()
+
+
+def test_refusals():
+    Hq, Hkv, d, dtype = 4, 2, 64, wl.F16
+    cache, _ = filled([100, 90], Hq, Hkv, d, 128, dtype, ta.CODED_INT8)
+    L, h = ta.lib(), cache.h
+    try:
+        x = torch.zeros(1 << 16, dtype=torch.float16, device=DEV)
+        f = torch.zeros(1 << 16, device=DEV)
+        p, o = x.data_ptr(), f.data_ptr()
+        refused = [
+            (ta.EINVAL, L.topk_attn_coded_append(h, 1, 0, p, p, 1, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, 2, p, p, 1, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, -2, p, p, 1, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, 0, p, p, -1, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, 0, p, None, 1, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, 0, p + 2, p, 1, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, 0, p, p, 1, 0, 129, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_append(h, 0, 0, p, p, 1, 0, -128, 64, None)),
+            (ta.ECAPACITY, L.topk_attn_coded_append(h, 0, 0, p, p, 29, 0, 128, 64, None)),
+            (ta.ECAPACITY, L.topk_attn_coded_append(h, 0, -1, p, p, 30, 0, 128, 64, None)),
+            (ta.ECAPACITY, L.topk_attn_coded_append(h, 0, 0, p, p, 1 << 62, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_read(h, 0, 0, -1, 1, p, p, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_read(h, 0, 0, 100, 1, p, p, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_read(h, 0, -1, 0, 91, p, p, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_read(h, 0, 0, 0, 1, None, p, 0, 128, 64, None)),
+            (ta.EINVAL, L.topk_attn_coded_decode(h, 0, p, 0, 0, o, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_decode(h, 0, p, -1, 5, o, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_decode(h, 0, p + 2, 0, 5, o, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_decode(h, 0, p, 0, 5, None, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_prompt(h, 0, -1, p, 91, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_prompt(h, 0, 0, p, 101, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_prompt(h, 0, 0, p, 10, 0, 0, p, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_prompt(h, 0, 0, p, -1, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_prompt(h, 0, 0, p, 10, 0, 5, p + 8, None, None)),
+            (ta.EINVAL, L.topk_attn_coded_reset(h, 0, 2, None)),
+        ]
+        assert all(a == b for a, b in refused), refused
+        assert [cache.length(0, b) for b in range(2)] == [100, 90] and cache.length(0, -1) == -1
+        assert L.topk_attn_coded_append(h, 0, 0, None, None, 0, 0, 0, 0, None) == ta.OK
+        assert L.topk_attn_coded_read(h, 0, 0, 100, 0, None, None, 0, 0, 0, None) == ta.OK
+        assert L.topk_attn_coded_prompt(h, 0, 0, None, 0, 0, 1, None, None, None) == ta.OK
+        cache.reset(0, 1)
+        with pytest.raises(ta.TopkAttnError):
+            cache.decode(0, torch.zeros((2, Hq, d), dtype=torch.float16, device=DEV))
+    finally:
+        cache.close()

@@ -1,0 +1,308 @@
+"""Attention with a sliding window and first tokens that stay visible, and attention of a prompt's tokens, over a cache in its own type, on the GPU
+through the binding against oracle/coded_cache_ref.py in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import helpers as H
+from oracle import coded_cache_ref as ref
+from paper_2502_06766_amd import topk_attn as ta
+from paper_2502_06766_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda", 0) if torch.cuda.is_available() else None
+U = 2.0 ** -24                                                   # half a step of fp32 relative to the value
+HALF = {wl.F32: 2.0 ** -24, wl.F16: 2.0 ** -11, wl.BF16: 2.0 ** -8}
+TYPES = [wl.F32, wl.F16, wl.BF16]
+
+
+def draw(g, *shape, dtype):
+    return wl.quantize(g.standard_normal(shape).astype(np.float32), dtype)
+
+
+def up(x, dtype):
+    return H.to_torch(x, dtype, DEV)
+
+
+def wide(x, dtype):
+    return wl.widen(x, dtype).astype(np.float64)
+
+
+def filled(lens, Hq, Hkv, d, cap, dtype, seed=0, rows=None, layers=1, layer=0):
+    """A cache whose unused rows are NaN, sequence b of `layer` holding lens[b] tokens -> cache, K, V (widened), per sequence."""
+    g = np.random.default_rng(seed)
+    cache = ta.TopkAttnCache(layers, len(lens), Hq, Hkv, d, cap, 16, dtype)
+    cache.kv.fill_(255)
+    got = []
+    for b, n in enumerate(lens):
+        K, V = (draw(g, Hkv, n, d, dtype=dtype) for _ in range(2)) if rows is None else rows[b]
+        if n:
+            cache.append(layer, b, up(K, dtype), up(V, dtype), head_major=True)
+        got.append((wide(K, dtype), wide(V, dtype)))
+    return cache, got
+
+
+def weight_error(q, K, d):
+    """Bound of a softmax weight's relative error before normalisation: the score's sum of d products in 32 bits (d u sum |q k|), its product with the
+    scale and the difference to the maximum (6 u of the largest exponent), and the exponential (4 u)."""
+    Hkv = K.shape[0]
+    rows = q.reshape(-1, Hkv, q.shape[-2] // Hkv, d)
+    A = max((np.abs(K[h]) @ np.abs(rows[:, h].reshape(-1, d)).T).max() for h in range(Hkv)) / np.sqrt(d)
+    return (d + 6) * U * A + 4 * U
+
+
+def check(out, lse, q, K, V, sinks, window, dtype, token, label):
+    """q [m, Hq, d].  token: fp32 output, weights in parts that leave 2^-22 of them; else weights and output are rounded to the type once."""
+    d, n = q.shape[-1], K.shape[1]
+    w_out, w_lse = ref.attend(q, K, V, sinks, window)
+    dw, sums = weight_error(q, K, d), (n / 16 + 64) * U
+    rounding = 2.0 ** -22 if token else 0.0 if dtype == wl.F32 else HALF[dtype]
+    tol = 2 * (dw + rounding + sums) * np.abs(V).max() + (0 if token else HALF[dtype] * np.abs(w_out))
+    off = np.abs(out - w_out)
+    assert (off <= tol).all(), f"{label}: out off by {off.max():.3g}, {(off - tol).max():.3g} beyond what is allowed"
+    off, tol = np.abs(lse - w_lse).max(), dw + sums + 2.0 ** -22 + 4 * U * np.abs(w_lse).max()
+    assert off <= tol, f"{label}: lse off by {off:.3g}, {tol:.3g} allowed"
+
+
+SINKS = [  # dtype, Hq, Hkv, d, lens, sinks, window
+    (wl.BF16, 32, 8, 128, [500], 4, 100),
+    (wl.F16, 4, 1, 64, [1, 2, 63], 0, 1),
+    (wl.BF16, 5, 1, 32, [64, 65, 31, 133], 1, 40),
+    (wl.F32, 8, 2, 64, [1, 200, 129], 64, 65),
+    (wl.F32, 16, 1, 256, [77, 400], 3, 64),
+    (wl.F16, 16, 1, 128, [999, 3], 100, 129),
+    (wl.BF16, 17, 1, 256, [130, 700], 17, 600),
+    (wl.F16, 80, 2, 64, [300, 129, 5], 0, 33),
+    (wl.BF16, 64, 8, 128, [8191, 700, 1, 2048, 64], 128, 1000),
+    (wl.F16, 4, 1, 128, [70001], 5, 33333),
+    (wl.F32, 4, 2, 32, [1000, 999], 0, 63),
+    (wl.BF16, 4, 2, 128, [1000, 1200], 990, 10),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,lens,sinks,window", SINKS)
+def test_decode_sinks(dtype, Hq, Hkv, d, lens, sinks, window):
+    cache, got = filled(lens, Hq, Hkv, d, max(lens), dtype, seed=window)
+    try:
+        q = draw(np.random.default_rng(window + 1), len(lens), Hq, d, dtype=dtype)
+        out, lse = cache.decode_sinks(0, up(q, dtype), window, sinks)
+        for b, n in enumerate(lens):
+            check(out[b].cpu().numpy()[None], lse[b].cpu().numpy()[None], wide(q[b], dtype)[None], *got[b], sinks, window, dtype, True, f"sequence {b} ({n} tokens)")
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_window_over_everything_is_the_dense_decode(dtype):
+    lens, Hq, Hkv, d = [700, 64, 1], 8, 2, 64
+    cache, _ = filled(lens, Hq, Hkv, d, 700, dtype)
+    try:
+        q = up(draw(np.random.default_rng(1), 3, Hq, d, dtype=dtype), dtype)
+        want = cache.decode_dense(0, q)
+        for window, sinks in ((700, 0), (1 << 62, 0), (600, 100), (1, 699), (1, 1 << 62)):
+            got = cache.decode_sinks(0, q, window, sinks)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (window, sinks)
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tokens_outside_the_window_have_no_effect(dtype):
+    """NaN and infinities at every token that is not seen, single tokens and rows of a prompt alike."""
+    d, Hq, n = 64, 4, 333
+    g = np.random.default_rng(2)
+    K, V = (draw(g, 1, n, d, dtype=dtype) for _ in range(2))
+    q = up(draw(g, 1, n, Hq, d, dtype=dtype), dtype)
+    bad = wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    clean, _ = filled([n], Hq, 1, d, n, dtype, rows=[(K, V)])
+    try:
+        for sinks, window in ((0, 1), (3, 70), (64, 64), (1, 129)):
+            Kb, Vb = K.copy(), V.copy()
+            hidden = np.arange(sinks, n - window)
+            Kb[0, hidden], Vb[0, hidden] = bad[hidden % 3, None], bad[(hidden // 3) % 3, None]
+            dirty, _ = filled([n], Hq, 1, d, n, dtype, rows=[(Kb, Vb)])
+            try:
+                a, b = (c.decode_sinks(0, q[:, -1].contiguous(), window, sinks) for c in (clean, dirty))
+                assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), (sinks, window)
+                a, b = (c.prompt(0, q, window=window, sinks=sinks) for c in (clean, dirty))
+                see = torch.from_numpy(ref.seen(n, n, sinks, window)[:, hidden].any(1)).to(DEV)
+                assert torch.equal(a[0][0][~see], b[0][0][~see]) and torch.equal(a[1][0][~see], b[1][0][~see]), (sinks, window)
+                assert torch.isnan(b[0][0][see]).any(-1).all(), (sinks, window)
+            finally:
+                dirty.close()
+    finally:
+        clean.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_value_that_is_no_number_reaches_those_that_see_it(dtype):
+    """Infinities and NaN among the values of a prompt: rows before them as without, rows that see them as the formula has it, channel by channel."""
+    d, Hq, n = 64, 4, 200
+    g = np.random.default_rng(4)
+    K, V = (draw(g, 1, n, d, dtype=dtype) for _ in range(2))
+    q = up(draw(g, 1, n, Hq, d, dtype=dtype), dtype)
+    Vb = V.copy()
+    bad = wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    for t, c, kind in ((30, 5, 1), (31, 6, 0), (90, 7, 2), (130, 5, 2), (199, 8, 1)):
+        Vb[0, t, c] = bad[kind]
+    clean, _ = filled([n], Hq, 1, d, n, dtype, rows=[(K, V)])
+    dirty, got = filled([n], Hq, 1, d, n, dtype, rows=[(K, Vb)])
+    try:
+        for sinks, window in ((0, n), (0, 25), (31, 40)):
+            a, b = (c.prompt(0, q, window=window, sinks=sinks)[0][0].float().cpu().numpy() for c in (clean, dirty))
+            want, _ = ref.attend(q[0].double().cpu().numpy(), *got[0], sinks, window)
+            number = np.isfinite(want)
+            np.testing.assert_array_equal(np.isnan(b), np.isnan(want))
+            np.testing.assert_array_equal(b[np.isinf(want)], want[np.isinf(want)])
+            np.testing.assert_array_equal(b[number], a[number])
+    finally:
+        clean.close()
+        dirty.close()
+
+
+PROMPT = [  # dtype, Hq, Hkv, d, lens, M, sinks, window
+    (wl.BF16, 4, 2, 64, [70], 70, 0, 70),
+    (wl.F16, 4, 1, 128, [1], 1, 0, 1),
+    (wl.F16, 8, 2, 128, [200, 333], 7, 0, 333),
+    (wl.BF16, 5, 1, 32, [150, 129, 128], 100, 0, 150),
+    (wl.F32, 2, 2, 64, [140, 192], 131, 4, 50),
+    (wl.F32, 4, 1, 256, [130], 70, 0, 130),
+    (wl.F32, 6, 2, 128, [190], 40, 0, 190),
+    (wl.F32, 16, 1, 32, [300], 300, 1, 64),
+    (wl.F16, 3, 1, 256, [320, 257], 257, 0, 64),
+    (wl.BF16, 128, 1, 128, [300], 130, 10, 100),
+    (wl.BF16, 32, 8, 128, [600, 640], 600, 0, 640),
+    (wl.F16, 28, 4, 64, [1000], 500, 65, 128),
+    (wl.F16, 28, 28, 64, [999], 999, 0, 200),
+    (wl.BF16, 4, 2, 32, [3000], 3, 0, 3000),
+    (wl.BF16, 4, 1, 256, [5000], 20, 70, 2000),
+    (wl.F16, 1, 1, 32, [515], 515, 0, 1),
+    (wl.F16, 40, 40, 32, [300, 299, 298, 297, 296, 295, 294], 200, 5, 64),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,lens,M,sinks,window", PROMPT)
+def test_prompt(dtype, Hq, Hkv, d, lens, M, sinks, window):
+    cache, got = filled(lens, Hq, Hkv, d, max(lens) + 1, dtype, seed=M)
+    try:
+        q = draw(np.random.default_rng(M + 1), len(lens), M, Hq, d, dtype=dtype)
+        out, lse = cache.prompt(0, up(q, dtype), window=window, sinks=sinks)
+        for b, n in enumerate(lens):
+            check(out[b].float().cpu().numpy(), lse[b].cpu().numpy(), wide(q[b], dtype), *got[b], sinks, window, dtype, False, f"sequence {b} ({n} tokens)")
+        out, lse = cache.prompt(0, up(q, dtype)[-1:], window=window, sinks=sinks, seq=len(lens) - 1)
+        check(out[0].float().cpu().numpy(), lse[0].cpu().numpy(), wide(q[-1], dtype), *got[-1], sinks, window, dtype, False, "the last sequence alone")
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_prompt_of_peaked_and_rising_scores(dtype):
+    """One key far above the others, all keys equal, scores rising along the cache (the running maximum changes at every tile) and falling."""
+    d, n = 64, 300
+    g = np.random.default_rng(5)
+    q = np.zeros((1, n, 4, d), np.float32)
+    q[..., 0] = 16.0
+    for kind in ("peak", "flat", "rise", "fall"):
+        K = np.zeros((1, n, d), np.float32)
+        K[0, :, 0] = {"peak": np.where(np.arange(n) == 170, 40.0, 0.0), "flat": np.full(n, 3.0), "rise": np.arange(n) / 8.0, "fall": -np.arange(n) / 8.0}[kind]
+        V = draw(g, 1, n, d, dtype=dtype)
+        cache, got = filled([n], 4, 1, d, n, dtype, rows=[(wl.quantize(K, dtype), V)])
+        try:
+            qd = wl.quantize(q, dtype)
+            out, lse = cache.prompt(0, up(qd, dtype))
+            check(out[0].float().cpu().numpy(), lse[0].cpu().numpy(), wide(qd[0], dtype), *got[0], 0, n, dtype, False, kind)
+        finally:
+            cache.close()
+
+
+def test_a_prompt_through_the_cache():
+    """As a program uses it, over two layers: projections normalised, rotated and appended, the prompt's tokens attended, then steps of one token with a
+    window; evicted caches go by rows."""
+    B, Hq, Hkv, d, n, dtype = 2, 8, 2, 64, 130, wl.BF16
+    g = np.random.default_rng(6)
+    cache = ta.TopkAttnCache(2, B, Hq, Hkv, d, 200, 16, dtype)
+    half = (cache.kv.numel() // 2)
+    freq = torch.from_numpy((10000.0 ** (-np.arange(d // 2) / (d // 2))).astype(np.float32)).to(DEV)
+    try:
+        for layer in range(2):
+            k, v, q = (up(draw(g, B, n, h, d, dtype=dtype), dtype) for h in (Hkv, Hkv, Hq))
+            qr = cache.append_rotary(layer, q, k, v, freq)
+            out, lse = cache.prompt(layer, qr, window=50, sinks=4)
+            K, V = (cache.kv[i * half:(i + 1) * half].view(torch.bfloat16).view(2, B, Hkv, 200, d)[layer] for i in range(2))
+            for b in range(B):
+                check(out[b].float().cpu().numpy(), lse[b].cpu().numpy(), qr[b].double().cpu().numpy(), K[b, :, :n].double().cpu().numpy(),
+                      V[b, :, :n].double().cpu().numpy(), 4, 50, dtype, False, f"layer {layer}, sequence {b}")
+            for t in range(3):
+                k, v, q = (up(draw(g, B, 1, h, d, dtype=dtype), dtype) for h in (Hkv, Hkv, Hq))
+                qr = cache.append_rotary(layer, q, k, v, freq)
+                out, lse = cache.decode_sinks(layer, qr[:, 0].contiguous(), 50, 4)
+                m = n + t + 1
+                for b in range(B):
+                    check(out[b].cpu().numpy()[None], lse[b].cpu().numpy()[None], qr[b].double().cpu().numpy(), K[b, :, :m].double().cpu().numpy(),
+                          V[b, :, :m].double().cpu().numpy(), 4, 50, dtype, True, f"layer {layer}, step {t}, sequence {b}")
+                # a prompt of one token is that token's decode, rounded
+                rows, _ = cache.prompt(layer, qr, window=50, sinks=4)
+                assert (rows[:, 0].float() - out).abs().max() <= 2 * (HALF[dtype] + 2 * HALF[dtype]) * V[:, :, :m].float().abs().max()
+    finally:
+        cache.close()
+
+
+def test_captured_calls_replay():
+    Hq, Hkv, d, dtype, n, M = 8, 2, 128, wl.F16, 5000, 9
+    cache, _ = filled([n, n - 33], Hq, Hkv, d, n, dtype)
+    g = np.random.default_rng(1)
+    try:
+        q, qm = up(draw(g, 2, Hq, d, dtype=dtype), dtype), up(draw(g, 2, M, Hq, d, dtype=dtype), dtype)
+
+        def calls():
+            return (*cache.decode_sinks(0, q, 1000, 4), *cache.prompt(0, qm), *cache.prompt(0, qm, window=500, sinks=7), *cache.decode_dense(0, q))
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            calls()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = calls()
+        for _ in range(4):
+            q.copy_(up(draw(g, 2, Hq, d, dtype=dtype), dtype))
+            qm.copy_(up(draw(g, 2, M, Hq, d, dtype=dtype), dtype))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [x.clone() for x in outs]
+            for a, b in zip(got, calls()):
+                assert torch.equal(a, b)
+    finally:
+        cache.close()
+
+
+def test_refusals():
+    Hq, Hkv, d, dtype = 4, 2, 64, wl.F16
+    cache, _ = filled([100, 90], Hq, Hkv, d, 128, dtype)
+    L, h = ta.lib(), cache.h
+    try:
+        x = torch.zeros(1 << 16, dtype=torch.float16, device=DEV)
+        f = torch.zeros(1 << 16, device=DEV)
+        p, o = x.data_ptr(), f.data_ptr()
+        refused = [
+            (ta.EINVAL, L.topk_attn_decode_sinks(h, 0, p, 0, 0, o, None, None)),
+            (ta.EINVAL, L.topk_attn_decode_sinks(h, 0, p, -1, 5, o, None, None)),
+            (ta.EINVAL, L.topk_attn_decode_sinks(h, 1, p, 0, 5, o, None, None)),
+            (ta.EINVAL, L.topk_attn_decode_sinks(h, 0, p + 2, 0, 5, o, None, None)),
+            (ta.EINVAL, L.topk_attn_decode_sinks(h, 0, p, 0, 5, None, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, -1, p, 91, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 0, p, 101, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 2, p, 10, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, -1, 0, p, 10, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 0, p, 10, 0, 0, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 0, p, 10, -1, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 0, p, -1, 0, 5, p, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 0, p, 10, 0, 5, p + 8, None, None)),
+            (ta.EINVAL, L.topk_attn_prompt(h, 0, 0, None, 10, 0, 5, p, None, None)),
+        ]
+        assert all(a == b for a, b in refused), refused
+        assert L.topk_attn_prompt(h, 0, 0, None, 0, 0, 1, None, None, None) == ta.OK
+        cache.reset(0, 1)
+        with pytest.raises(ta.TopkAttnError):
+            cache.decode_sinks(0, torch.zeros((2, Hq, d), dtype=torch.float16, device=DEV), 5)
+    finally:
+        cache.close()
