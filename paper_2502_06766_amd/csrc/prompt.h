@@ -4,7 +4,7 @@
 //   out_m = sum_t w_t V_t / sum_t w_t,  w_t = exp(q_m . K_t / sqrt(d)),  t <= p_m and (t < sinks or t > p_m - window)
 //
 // A row is a query and a head of the group, m G + g: the heads of a group read the same keys, and a block of rows covers few queries, so little of what
-// it computes is masked.  A wave has 32 rows (or twice that), the workgroup walks the keys in tiles of 64 through LDS.  Products are taken transposed (keys x channels
+// it computes is masked.  A wave has 32 rows, the workgroup walks the keys in tiles of 64 through LDS.  Products are taken transposed (keys x channels
 // times channels x rows, then channels x keys times keys x rows): a lane holds scores and weighted sums of one row, lane % 32, the running maximum is
 // a number per lane, and the scores come out of the first product in the order in which the second one takes the weights:
 //   score register i of a 32-key tile is key 8 (i / 4) + 4 (lane / 32) + i % 4; step x of 16 keys takes registers 8 x .. 8 x + 7.
@@ -44,8 +44,7 @@ inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int6
 // Rows of a block, and the splits of its keys.  (room: bytes there are for partial sums)
 inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu) {
     const int64_t rows = a->M * a->G, streams = (int64_t)a->S * a->Hkv;
-    const bool wide = a->dtype != DT_F32 && a->D <= 128;
-    a->block_rows = rows <= 32 ? 32 : wide && streams * ((rows + 255) / 256) >= n_cu ? 256 : 128;
+    a->block_rows = rows <= 32 ? 32 : 128;
     a->row_blocks = (int)((rows + a->block_rows - 1) / a->block_rows);
     int64_t tiles = 1;
     for (int b = 0; b < a->S; ++b) {
@@ -91,16 +90,16 @@ __device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
 // Queries of a wave's rows as the second operand: 16 bits, 16 channels of a row in eight-channel halves; 32 bits, 8 channels in four-channel halves.
-template <int CT, int D, int NR, int PQ> struct QueryFrag {
+template <int CT, int D, int PQ> struct QueryFrag {
     using type = typename std::conditional<CT == DT_F32, f32x4, typename std::conditional<CT == DT_BF16, bf16x8, f16x8>::type>::type;
     static constexpr int N = CT == DT_F32 ? D / 8 : D / 16;
-    type v[PQ][NR][N];
+    type v[PQ][N];
 };
 
-template <int D, int NR> struct RowState {
-    f32x16 acc[NR][D / 32];
-    float m[NR], l[NR], e[NR];  // running maximum (whole), sum of weights relative to it, power of two of the weighted sum
-    int pos[NR], hidden[NR];    // token of the row; the newest one its window leaves out
+template <int D> struct RowState {
+    f32x16 acc[D / 32];
+    float m, l, e;              // what the weights are relative to (a power of two), their sum, power of two of the weighted sum
+    int pos, hidden;            // token of the row; the newest one its window leaves out
 };
 
 __device__ __forceinline__ float other_half_max(float v) {
@@ -140,89 +139,112 @@ template <int CT> __device__ __forceinline__ bool has_no_number(uint32_t w) {
     return finite_halves<CT>(w) != w;
 }
 
+// The maximum that the weights are relative to follows the scores' only when those are more than 2^kSlack above: the weighted sums are scaled seldom
+// (8192 tokens: at 2 of 100 tiles, at 40 with no slack), and a weight stays below 2^kSlack.
+constexpr float kSlack = 8.f, kSumSlack = 5.f, kSumShift = 10.f;       // (of weights times a value scale: below 2^15 in fp16)
+
 // One tile of 64 keys from token t0 on.  f (and f_lo, of 32-bit rows): score times this is the exponent of two.  VSCALE: the values are times `sv` (a block's scale),
-// the weighted sum has a power of two of its own (coded_decode.hip).  `masked`: not all rows of the wave see all keys.
-template <int CT, bool FRAG, bool VSCALE, bool EXACT, int D, int NR, int PQ, int PP>
-__device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, const QueryFrag<CT, D, NR, PQ>& q, RowState<D, NR>& st,
-                                            const float (&f)[NR], const float (&f_lo)[NR], float sv, bool masked, int t0, int sinks) {
-    constexpr int EB = TileType<CT>::bytes, ROWB = D * EB;
+// the weighted sum has a power of two of its own (coded_decode.hip).  MASKED: not all rows of the workgroup see all keys.
+template <int CT, bool FRAG, bool VSCALE, bool EXACT, bool MASKED, int D, int PQ, int PP>
+__device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, const QueryFrag<CT, D, PQ>& q, RowState<D>& st, float f, float f_lo, float sv,
+                                            int t0, int sinks) {
+    constexpr int EB = TileType<CT>::bytes, ROWB = D * EB, N = QueryFrag<CT, D, PQ>::N, T = D / 32;
     const int lane = lane_id(), hh = lane >> 5, row = lane & 31;
-    f32x16 s[2][NR];
+    f32x16 s[2];
+    if constexpr (CT == DT_F32) {
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+        for (int sub = 0; sub < 2; ++sub) {
+            s[sub] = f32x16{};
 #pragma unroll
-        for (int r = 0; r < NR; ++r) s[sub][r] = f32x16{};
-        const char* const base = ldsK + (32 * sub + row) * ROWB;
+            for (int c = 0; c < N; ++c) {
+                const u32x4 k = *reinterpret_cast<const u32x4*>(ldsK + (32 * sub + row) * ROWB + key_piece<ROWB>(32 * sub + row, 2 * c + hh) * 16);
 #pragma unroll
-        for (int c = 0; c < QueryFrag<CT, D, NR, PQ>::N; ++c) {
-            const u32x4 k = *reinterpret_cast<const u32x4*>(base + key_piece<ROWB>(32 * sub + row, 2 * c + hh) * 16);
+                for (int y = 0; y < 4; ++y) s[sub] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[y]), q.v[0][c][y], s[sub], 0, 0, 0);
+            }
+        }
+    } else {
+        // (all reads of a pass first: a product that waits for its own read stalls the wave for the trip)
+        constexpr int PASS = D <= 128 ? 2 : 1;                       // 32-key tiles whose operands are in registers at a time
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                if constexpr (CT == DT_F32) {
+        for (int s0 = 0; s0 < 2; s0 += PASS) {
+            u32x4 k[PASS][N];
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) s[sub][r] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[y]), q.v[0][r][c][y], s[sub][r], 0, 0, 0);
-                } else {
+            for (int u = 0; u < PASS; ++u) {
 #pragma unroll
-                    for (int z = 0; z < PQ; ++z) s[sub][r] = mfma32(__builtin_bit_cast(typename TileType<CT>::v8, k), q.v[z][r][c], s[sub][r]);
+                for (int c = 0; c < N; ++c)
+                    k[u][c] = *reinterpret_cast<const u32x4*>(ldsK + (32 * (s0 + u) + row) * ROWB + key_piece<ROWB>(32 * (s0 + u) + row, 2 * c + hh) * 16);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < PASS; ++u) {
+                s[s0 + u] = f32x16{};
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+#pragma unroll
+                    for (int z = 0; z < PQ; ++z) s[s0 + u] = mfma32(__builtin_bit_cast(typename TileType<CT>::v8, k[u][c]), q.v[z][c], s[s0 + u]);
                 }
             }
         }
     }
+    u32x4 v[2][T];                                                   // values of the first step: on their way during the weights
+    if constexpr (CT != DT_F32) {
+#pragma unroll
+        for (int ct = 0; ct < T; ++ct) v[0][ct] = value_frag<D, FRAG>(ldsV, ct, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     // ---- weights, in place of the scores ----
-    float g[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        if (masked) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int t = t0 + 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hh + i % 4;
-                if (t > st.pos[r] || (t <= st.hidden[r] && t >= sinks)) s[i / 16][r][i % 16] = -INFINITY;
-            }
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i / 16][r][i % 16]);
-        top = other_half_max(top);
-        const bool none = top == -INFINITY;
-        const float bm = ceilf(top * f[r]), m_new = fmaxf(st.m[r], none ? -INFINITY : bm), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float down = __builtin_amdgcn_exp2f(st.m[r] - ref);
-        float sum[2] = {0.f, 0.f};
+    if (MASKED) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const float x = s[i / 16][r][i % 16];
-            float w = __builtin_amdgcn_exp2f(EXACT ? fmaf(x, f[r], fmaf(x, f_lo[r], -ref)) : fmaf(x, f[r], -ref));
-            if ((VSCALE || EXACT) && masked && x == -INFINITY) w = 0.f;          // (a factor of zero, or of two parts)
-            s[i / 16][r][i % 16] = w;
-            sum[i & 1] += w;
-        }
-        st.l[r] = fmaf(st.l[r], down, sum[0] + sum[1]);
-        float turn = down;                                          // of the weighted sum
-        g[r] = 1.f;
-        if (VSCALE) {
-            const int ke = (int)(__float_as_uint(sv) >> 23) - 126;  // sv < 2^ke
-            const float e_new = sv > 0.f && !none ? fmaxf(st.e[r], bm + (float)ke) : st.e[r];
-            g[r] = sv;
-            if (sv > 0.f) g[r] = ldexpf(sv, (int)fmaxf(fminf(ref - e_new + kShift, (float)(127 - ke)), -300.f));
-            if (none) g[r] = 0.f;                                   // (a block of NaN that the row does not see)
-            turn = st.e[r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.e[r] - e_new);
-            st.e[r] = e_new;
-        }
-        st.m[r] = m_new;
-        if (__any(turn != 1.f)) {
-#pragma unroll
-            for (int ct = 0; ct < D / 32; ++ct) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st.acc[r][ct][i] *= turn;
-            }
-        }
-        if (VSCALE) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) s[i / 16][r][i % 16] *= g[r];
+            const int t = t0 + 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hh + i % 4;
+            if (t > st.pos || (t <= st.hidden && t >= sinks)) s[i / 16][i % 16] = -INFINITY;
         }
     }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
+    top = other_half_max(top);
+    const bool none = top == -INFINITY;                              // (also of nothing but NaN: the weights are NaN then)
+    const float bm = none ? -INFINITY : ceilf(top * f);
+    const float m_new = bm > st.m + kSlack || st.m == -INFINITY ? bm : st.m, ref = m_new == -INFINITY ? 0.f : m_new;
+    float turn = __builtin_amdgcn_exp2f(st.m - ref), e_new = 0.f;
+    int ke = 0;
+    st.l *= turn;
+    if (VSCALE) {                                                    // (the weighted sum goes by its own)
+        ke = (int)(__float_as_uint(sv) >> 23) - 126;                 // sv < 2^ke
+        const float e_tile = bm + (float)ke;
+        e_new = sv > 0.f && !none && (e_tile > st.e + kSumSlack || st.e == -INFINITY) ? e_tile : st.e;
+        turn = st.e == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.e - e_new);
+    }
+    if (__any(turn != 1.f)) {
+#pragma unroll
+        for (int ct = 0; ct < T; ++ct) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.acc[ct][i] *= turn;
+        }
+    }
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const float x = s[i / 16][i % 16];
+        float w = __builtin_amdgcn_exp2f(EXACT ? fmaf(x, f, fmaf(x, f_lo, -ref)) : fmaf(x, f, -ref));
+        if ((VSCALE || EXACT) && MASKED && x == -INFINITY) w = 0.f;  // (a factor of zero, or of two parts)
+        s[i / 16][i % 16] = w;
+        sum[i & 1] += w;
+    }
+    st.l += sum[0] + sum[1];
+    if (VSCALE) {
+        float g = sv;
+        if (sv > 0.f) g = ldexpf(sv, (int)fmaxf(fminf(ref - e_new + kSumShift, (float)(127 - ke)), -300.f));
+        if (none) g = 0.f;                                           // (a block of NaN that the row does not see)
+        st.e = e_new;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i / 16][i % 16] *= g;
+    }
+    st.m = m_new;
     // ---- values that are no numbers, in a tile that not all rows see ----
     bool poison = false;
-    if (!FRAG && masked) {
+    if constexpr (!FRAG && MASKED) {
         uint64_t keys = 0;
         for (int at = 0; at < 64 * ROWB; at += 1024) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(ldsV + at + lane * 16);
@@ -240,26 +262,23 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
             const int key = __builtin_ctzll(keys);
             keys &= keys - 1;
             const int reg = (key >> 5) * 16 + ((key & 31) >> 3) * 4 + (key & 3), t = t0 + key;
+            float p = 0.f;
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                float p = 0.f;
+            for (int i = 0; i < 32; ++i)
+                if (i == reg) p = s[i / 16][i % 16];
+            p = __shfl(p, row + 32 * ((key >> 2) & 1), 64);
+            const bool sees = !(t > st.pos || (t <= st.hidden && t >= sinks));
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i == reg) p = s[i / 16][r][i % 16];
-                p = __shfl(p, row + 32 * ((key >> 2) & 1), 64);
-                const bool sees = !(t > st.pos[r] || (t <= st.hidden[r] && t >= sinks));
+            for (int ct = 0; ct < T; ++ct) {
 #pragma unroll
-                for (int ct = 0; ct < D / 32; ++ct) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int ch = 32 * ct + 8 * (i / 4) + 4 * hh + i % 4;
-                        const char* at = ldsV + key * ROWB + value_piece<ROWB, EB>(key, ch * EB / 16) * 16 + ch * EB % 16;
-                        float v;
-                        if (CT == DT_F32) v = *reinterpret_cast<const float*>(at);
-                        else if (CT == DT_F16) v = (float)*reinterpret_cast<const _Float16*>(at);
-                        else v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
-                        if (sees && !(fabsf(v) < INFINITY)) st.acc[r][ct][i] = fmaf(p, v, st.acc[r][ct][i]);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const int ch = 32 * ct + 8 * (i / 4) + 4 * hh + i % 4;
+                    const char* at = ldsV + key * ROWB + value_piece<ROWB, EB>(key, ch * EB / 16) * 16 + ch * EB % 16;
+                    float x;
+                    if (CT == DT_F32) x = *reinterpret_cast<const float*>(at);
+                    else if (CT == DT_F16) x = (float)*reinterpret_cast<const _Float16*>(at);
+                    else x = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
+                    if (sees && !(fabsf(x) < INFINITY)) st.acc[ct][i] = fmaf(p, x, st.acc[ct][i]);
                 }
             }
         }
@@ -267,46 +286,44 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     // ---- weighted sum ----
     if constexpr (CT == DT_F32) {
 #pragma unroll
-        for (int ct = 0; ct < D / 32; ++ct) {
+        for (int ct = 0; ct < T; ++ct) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const int key = 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hh + i % 4, ch = 32 * ct + row;
-                float v = *reinterpret_cast<const float*>(ldsV + key * ROWB + value_piece<ROWB, 4>(key, ch >> 2) * 16 + (ch & 3) * 4);
-                if (poison && !(fabsf(v) < INFINITY)) v = 0.f;
-#pragma unroll
-                for (int r = 0; r < NR; ++r) st.acc[r][ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i / 16][r][i % 16], st.acc[r][ct], 0, 0, 0);
+                float x = *reinterpret_cast<const float*>(ldsV + key * ROWB + value_piece<ROWB, 4>(key, ch >> 2) * 16 + (ch & 3) * 4);
+                if (poison && !(fabsf(x) < INFINITY)) x = 0.f;
+                st.acc[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[i / 16][i % 16], st.acc[ct], 0, 0, 0);
             }
         }
     } else {
         using v8 = typename TileType<CT>::v8;
         using E = typename std::conditional<CT == DT_F16, _Float16, __bf16>::type;
-        v8 p[PP][NR][4];
+        v8 p[PP][4];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
+        for (int i = 0; i < 32; ++i) {
+            float rest = s[i / 16][i % 16];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                float rest = s[i / 16][r][i % 16];
-#pragma unroll
-                for (int z = 0; z < PP; ++z) {
-                    p[z][r][i / 8][i % 8] = (E)rest;
-                    rest -= (float)p[z][r][i / 8][i % 8];
-                }
+            for (int z = 0; z < PP; ++z) {
+                p[z][i / 8][i % 8] = (E)rest;
+                rest -= (float)p[z][i / 8][i % 8];
             }
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
+            if (x < 3) {
 #pragma unroll
-            for (int ct = 0; ct < D / 32; ++ct) {
-                u32x4 v = value_frag<D, FRAG>(ldsV, ct, x);
+                for (int ct = 0; ct < T; ++ct) v[(x + 1) & 1][ct] = value_frag<D, FRAG>(ldsV, ct, x + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int ct = 0; ct < T; ++ct) {
+                u32x4 w = v[x & 1][ct];
                 if (!FRAG && poison) {
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) v[y] = finite_halves<CT>(v[y]);
+                    for (int y = 0; y < 4; ++y) w[y] = finite_halves<CT>(w[y]);
                 }
 #pragma unroll
-                for (int r = 0; r < NR; ++r) {
-#pragma unroll
-                    for (int z = 0; z < PP; ++z) st.acc[r][ct] = mfma32(__builtin_bit_cast(v8, v), p[z][r][x], st.acc[r][ct]);
-                }
+                for (int z = 0; z < PP; ++z) st.acc[ct] = mfma32(__builtin_bit_cast(v8, w), p[z][x], st.acc[ct]);
             }
         }
     }
@@ -326,15 +343,15 @@ __device__ __forceinline__ void fetch_rows(const char* from, int rows, char* lds
     }
 }
 
-// DT: type of queries, output and open rows; FMT: the coded cache's format, or -1: rows of DT.  NW waves of 32 NR rows.
-template <int DT, int FMT, int D, int NW, int NR>
-__global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
+// DT: type of queries, output and open rows; FMT: the coded cache's format, or -1: rows of DT.  NW waves of 32 rows.
+template <int DT, int FMT, int D, int NW>
+__global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ? 2 : 1)) prompt_kernel(PromptCall a) {
     constexpr bool CODED = FMT >= 0;
     constexpr int CT = CODED ? DT_F16 : DT, PARTS = CODED && DT == DT_F32 ? 2 : 1;
     constexpr int EB = TileType<CT>::bytes, ROWB = D * EB, TILE = 64 * ROWB, OPEN_ROWB = D * TileType<DT>::bytes;
     constexpr int NBUF = 4 * TILE <= 131072 ? 2 : 1;
     constexpr int LDS = 2 * NBUF * TILE > 128 * OPEN_ROWB || !CODED ? 2 * NBUF * TILE : 128 * OPEN_ROWB;
-    constexpr int NT = 64 * NW, ROWS = 32 * NW * NR, FM = CODED ? FMT : CODED_E4M3;
+    constexpr int NT = 64 * NW, ROWS = 32 * NW, FM = CODED ? FMT : CODED_E4M3;
     __shared__ __align__(16) char lds[LDS];
     const int lane = lane_id(), hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -348,7 +365,7 @@ __global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
     const auto query_of = [&](int row) { return (row < n_rows ? row : n_rows - 1) / a.G; };
     const auto hidden_of = [&](int p) { return a.window <= p ? p - (int)a.window : -1; };
 
-    // tiles that some row of the workgroup sees
+    // tiles that some row of the workgroup sees: `front` of the sinks, then from .. to
     const int p_lo = before + query_of(row0), p_hi = before + query_of(row0 + ROWS - 1);
     const int first = hidden_of(p_lo) + 1;
     int front = ((sinks < p_hi + 1 ? sinks : p_hi + 1) + 63) / 64, from = first / 64;
@@ -361,49 +378,49 @@ __global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
     const int n_tiles = front + to - from;
     const int i0 = (int)((int64_t)split * n_tiles / a.n_split), i1 = (int)((int64_t)(split + 1) * n_tiles / a.n_split);
     const auto tile_of = [&](int i) { return i < front ? i : from + (i - front); };
+    // Of those, all rows see all keys of [0, all0) (sinks), and of [all1, all2): behind the newest token that a window leaves out, up to the first row's.
+    const int last_hidden = hidden_of(p_hi), up_to = (p_lo + 1) / 64;
+    const auto index_of = [&](int tile) { const int i = tile - from + front; return i < 0 ? 0 : i > n_tiles ? n_tiles : i; };
+    int all0 = sinks / 64 < up_to ? sinks / 64 : up_to;
+    if (from > 0 && all0 > front) all0 = front;
+    if (all0 > n_tiles) all0 = n_tiles;
+    int all1 = index_of(last_hidden < 0 ? 0 : last_hidden / 64 + 1), all2 = index_of(up_to);
+    if (all1 < front) all1 = front;
+    if (all1 < all0) all1 = all0;
+    if (all2 < all1) all2 = all1;
+    const auto within = [&](int i) { return i < i0 ? i0 : i > i1 ? i1 : i; };
+    const int end0 = within(all0), end1 = within(all1), end2 = within(all2);
 
-    RowState<D, NR> st;
-    int wave_lo = 0x7FFFFFFF, wave_hi = 0;
+    RowState<D> st;
+    const int at0 = row0 + 32 * wave, wave_lo = before + query_of(at0), wave_hi = before + query_of(at0 + 31);
+    st.m = st.e = -INFINITY;
+    st.l = 0.f;
+    st.pos = before + query_of(at0 + (lane & 31));
+    st.hidden = hidden_of(st.pos);
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int at = row0 + 32 * (NR * wave + r);
-        st.m[r] = st.e[r] = -INFINITY;
-        st.l[r] = 0.f;
-        st.pos[r] = before + query_of(at + (lane & 31));
-        st.hidden[r] = hidden_of(st.pos[r]);
-#pragma unroll
-        for (int ct = 0; ct < D / 32; ++ct) st.acc[r][ct] = f32x16{};
-        if (r == 0) wave_lo = before + query_of(at);
-        wave_hi = before + query_of(at + 31);
-    }
-    const bool idle = row0 + 32 * NR * wave >= n_rows;
-    const int wave_first = hidden_of(wave_lo) + 1, wave_last = hidden_of(wave_hi);     // oldest token a window of the wave has, newest one that some window leaves out
-    // Whether a row of the wave sees a key of the tile, and whether all see all.
+    for (int ct = 0; ct < D / 32; ++ct) st.acc[ct] = f32x16{};
+    const bool idle = at0 >= n_rows;
+    const int wave_first = hidden_of(wave_lo) + 1;                  // oldest token that a window of the wave has
     const auto seen = [&](int t0) { return !idle && t0 <= wave_hi && (t0 + 63 >= wave_first || t0 < sinks); };
-    const auto whole = [&](int t0) { return t0 + 63 <= wave_lo && (t0 > wave_last || t0 + 63 < sinks); };
 
     constexpr double kScale = 1.4426950408889634 / (D == 32 ? 5.656854249492381 : D == 64 ? 8.0 : D == 128 ? 11.313708498984761 : 16.0);
     constexpr float kScaleHi = (float)kScale, kScaleLo = (float)(kScale - (double)kScaleHi);
 
-    const auto query_row = [&](int r) {
-        int row = row0 + 32 * (NR * wave + r) + (lane & 31);
-        row = row < n_rows ? row : n_rows - 1;
-        const int m = row / a.G;
-        return (((int64_t)b * M + m) * a.Hq + kvh * a.G + (row - m * a.G)) * D;
-    };
-    const auto load_rows = [&](auto& frag) {                        // queries in their own type
+    int64_t query_row;                                              // the lane's row in q and out, in elements
+    {
+        const int row = at0 + (lane & 31) < n_rows ? at0 + (lane & 31) : n_rows - 1, m = row / a.G;
+        query_row = (((int64_t)b * M + m) * a.Hq + kvh * a.G + (row - m * a.G)) * D;
+    }
+    const char* const query = static_cast<const char*>(a.q) + query_row * TileType<DT>::bytes;
+    const auto load_row = [&](auto& frag) {                         // the query in its own type
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            const char* p = static_cast<const char*>(a.q) + query_row(r) * TileType<DT>::bytes;
-#pragma unroll
-            for (int c = 0; c < D * TileType<DT>::bytes / 32; ++c)
-                frag.v[0][r][c] = __builtin_bit_cast(typename std::remove_reference<decltype(frag.v[0][r][c])>::type, *reinterpret_cast<const u32x4*>(p + 32 * c + 16 * hh));
-        }
+        for (int c = 0; c < D * TileType<DT>::bytes / 32; ++c)
+            frag.v[0][c] = __builtin_bit_cast(typename std::remove_reference<decltype(frag.v[0][c])>::type, *reinterpret_cast<const u32x4*>(query + 32 * c + 16 * hh));
     };
 
     if constexpr (!CODED) {
-        QueryFrag<DT, D, NR, 1> q;
-        load_rows(q);
+        QueryFrag<DT, D, 1> q;
+        load_row(q);
         const char* const Kh = a.K + (int64_t)stream * a.Ncap * ROWB;
         const char* const Vh = a.V + (int64_t)stream * a.Ncap * ROWB;
         const auto fetch = [&](int i, int buf) {
@@ -411,38 +428,41 @@ __global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
             fetch_rows<ROWB, NW, false, EB>(Kh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE);
             fetch_rows<ROWB, NW, true, EB>(Vh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE + TILE);
         };
-        float f[NR], f_lo[NR];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) { f[r] = kScaleHi; f_lo[r] = kScaleLo; }
         if (NBUF == 2 && i0 < i1) fetch(i0, 0);
-        for (int i = i0; i < i1; ++i) {
-            const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
-            if (NBUF == 1) {
+        const auto walk = [&](auto masked, int lo, int hi) {
+            for (int i = lo; i < hi; ++i) {
+                const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
+                if (NBUF == 1) {
+                    __syncthreads();
+                    fetch(i, 0);
+                }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
-                fetch(i, 0);
+                if (NBUF == 2 && i + 1 < i1) fetch(i + 1, buf ^ 1);
+                const int t0 = 64 * tile_of(i);
+                const char* const at = lds + buf * 2 * TILE;
+                if (decltype(masked)::value ? seen(t0) : !idle)
+                    prompt_tile<DT, false, false, DT == DT_F32, decltype(masked)::value, D, 1, 1>(at, at + TILE, q, st, kScaleHi, kScaleLo, 1.f, t0, sinks);
             }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (NBUF == 2 && i + 1 < i1) fetch(i + 1, buf ^ 1);
-            const int t0 = 64 * tile_of(i);
-            if (seen(t0))
-                prompt_tile<DT, false, false, DT == DT_F32, D, NR, 1, 1>(lds + buf * 2 * TILE, lds + buf * 2 * TILE + TILE, q, st, f, f_lo, 1.f, !whole(t0), t0, sinks);
+        };
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+            walk(std::false_type{}, x ? end1 : i0, x ? end2 : end0);
+            walk(std::true_type{}, x ? end2 : end0, x ? i1 : end1);
         }
     } else {
         // ---- blocks: codes through registers, into LDS as fp16 ----
-        float unit_q[NR];
+        float unit_q;
         {
-            QueryFrag<DT_F16, D, NR, PARTS> q;
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                const char* p = static_cast<const char*>(a.q) + query_row(r) * TileType<DT>::bytes;
+            QueryFrag<DT_F16, D, PARTS> q;
+            {
                 float amax = 0.f;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     float x[8];
 #pragma unroll
                     for (int y = 0; y < 8; y += Elem<DT>::kPerLoad)
-                        Elem<DT>::widen(*reinterpret_cast<const u32x4*>(p + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
+                        Elem<DT>::widen(*reinterpret_cast<const u32x4*>(query + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
 #pragma unroll
                     for (int y = 0; y < 8; ++y) amax = fmaxf(amax, fabsf(x[y]));
                 }
@@ -450,20 +470,20 @@ __global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
                 int up = 13 - ((int)(__float_as_uint(amax) >> 23) - 127);       // amax times 2^up lies in [2^13, 2^14)
                 up = amax == 0.f || up > 120 ? 120 : up < -114 ? -114 : up;
                 const float by = __uint_as_float((uint32_t)(up + 127) << 23);
-                unit_q[r] = __uint_as_float((uint32_t)(127 - up) << 23) * CodeUnit<FM>::value;
+                unit_q = __uint_as_float((uint32_t)(127 - up) << 23) * CodeUnit<FM>::value;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
                     float x[8];
 #pragma unroll
                     for (int y = 0; y < 8; y += Elem<DT>::kPerLoad)
-                        Elem<DT>::widen(*reinterpret_cast<const u32x4*>(p + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
+                        Elem<DT>::widen(*reinterpret_cast<const u32x4*>(query + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
 #pragma unroll
                     for (int y = 0; y < 8; ++y) {
                         float left = x[y] * by;
 #pragma unroll
                         for (int z = 0; z < PARTS; ++z) {
-                            q.v[z][r][c][y] = (_Float16)left;
-                            left -= (float)q.v[z][r][c][y];
+                            q.v[z][c][y] = (_Float16)left;
+                            left -= (float)q.v[z][c][y];
                         }
                     }
                 }
@@ -515,34 +535,32 @@ __global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
                 load(i0);
                 place(0);
             }
-            for (int i = i0; i < i1; ++i) {
-                const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
-                scale = next;
-                if (i + 1 < i1) load(i + 1);
-                __syncthreads();
-                const int t0 = 64 * tile_of(i);
-                if (seen(t0)) {
-                    float f[NR], f_lo[NR];
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) {
-                        const float by = scale.x * unit_q[r];
-                        f[r] = by * kScaleHi;
-                        f_lo[r] = fmaf(by, kScaleHi, -f[r]) + by * kScaleLo;
+            const auto walk = [&](auto masked, int lo, int hi) {
+                for (int i = lo; i < hi; ++i) {
+                    const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
+                    scale = next;
+                    if (i + 1 < i1) load(i + 1);
+                    __syncthreads();
+                    const int t0 = 64 * tile_of(i);
+                    const char* const at = lds + buf * 2 * TILE;
+                    if (decltype(masked)::value ? seen(t0) : !idle) {
+                        const float by = scale.x * unit_q, f = by * kScaleHi, f_lo = fmaf(by, kScaleHi, -f) + by * kScaleLo;
+                        prompt_tile<DT_F16, true, true, DT == DT_F32, decltype(masked)::value, D, PARTS, PARTS>(at, at + TILE, q, st, f, f_lo, scale.y, t0, sinks);
                     }
-                    prompt_tile<DT_F16, true, true, DT == DT_F32, D, NR, PARTS, PARTS>(lds + buf * 2 * TILE, lds + buf * 2 * TILE + TILE, q, st, f, f_lo, scale.y,
-                                                                                       !whole(t0), t0, sinks);
+                    if (NBUF == 1) __syncthreads();
+                    if (i + 1 < i1) place(NBUF == 2 ? buf ^ 1 : 0);
                 }
-                if (NBUF == 1) __syncthreads();
-                if (i + 1 < i1) place(NBUF == 2 ? buf ^ 1 : 0);
+            };
+#pragma unroll 1
+            for (int x = 0; x < 2; ++x) {
+                walk(std::false_type{}, x ? end1 : i0, x ? end2 : end0);
+                walk(std::true_type{}, x ? end2 : end0, x ? i1 : end1);
             }
         }
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
+        for (int ct = 0; ct < D / 32; ++ct) {
 #pragma unroll
-            for (int ct = 0; ct < D / 32; ++ct) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st.acc[r][ct][i] *= CodeUnit<FM>::value;
-            }
+            for (int i = 0; i < 16; ++i) st.acc[ct][i] *= CodeUnit<FM>::value;
         }
         // ---- open rows, in their own type, with the last split ----
         const int t0 = 64 * full;
@@ -554,63 +572,56 @@ __global__ void __launch_bounds__(64 * NW, 1) prompt_kernel(PromptCall a) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (seen(t0)) {
-                QueryFrag<DT, D, NR, 1> q;
-                load_rows(q);
-                float f[NR], f_lo[NR];
-#pragma unroll
-                for (int r = 0; r < NR; ++r) { f[r] = kScaleHi; f_lo[r] = kScaleLo; }
-                prompt_tile<DT, false, true, DT == DT_F32, D, NR, 1, 1>(lds, lds + 64 * OPEN_ROWB, q, st, f, f_lo, 1.f, true, t0, sinks);
+                QueryFrag<DT, D, 1> q;
+                load_row(q);
+                prompt_tile<DT, false, true, DT == DT_F32, true, D, 1, 1>(lds, lds + 64 * OPEN_ROWB, q, st, kScaleHi, kScaleLo, 1.f, t0, sinks);
             }
         }
     }
     // ---- what the rows leave ----
+    float l = st.l, m = st.m;
+    {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    const int at = 32 * wave + (lane & 31);
+    float by = 1.f;                                                 // brings the weighted sum to 2^m
+    if (CODED) by = st.e == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e - kSumShift - (m == -INFINITY ? 0.f : m));
+    if (row0 + at >= n_rows) return;
+    if (a.n_split == 1) {
+        const float inv = by / l;
+        char* const o = static_cast<char*>(a.out) + query_row * TileType<DT>::bytes;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        float l = st.l[r];
-        {
-            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-            l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-        }
-        float m = st.m[r];
-        const int at = 32 * (NR * wave + r) + (lane & 31), row = row0 + at;
-        float by = 1.f;                                             // brings the weighted sum to 2^m
-        if (CODED) by = st.e[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e[r] - kShift - (m == -INFINITY ? 0.f : m));
-        if (row >= n_rows) continue;
-        if (a.n_split == 1) {
-            const float inv = by / l;
-            char* const o = static_cast<char*>(a.out) + query_row(r) * TileType<DT>::bytes;
+        for (int ct = 0; ct < D / 32; ++ct) {
 #pragma unroll
-            for (int ct = 0; ct < D / 32; ++ct) {
+            for (int x = 0; x < 4; ++x) {
+                const int ch = 32 * ct + 8 * x + 4 * hh;
+                float y[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int ch = 32 * ct + 8 * x + 4 * hh;
-                    float y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = st.acc[r][ct][4 * x + e] * inv;
-                    if constexpr (DT == DT_F32) {
-                        *reinterpret_cast<f32x4*>(o + ch * 4) = f32x4{y[0], y[1], y[2], y[3]};
-                    } else {
-                        using E = typename std::conditional<DT == DT_F16, _Float16, __bf16>::type;
-                        typedef E e4 __attribute__((ext_vector_type(4)));
-                        *reinterpret_cast<e4*>(o + ch * 2) = e4{(E)y[0], (E)y[1], (E)y[2], (E)y[3]};
-                    }
+                for (int e = 0; e < 4; ++e) y[e] = st.acc[ct][4 * x + e] * inv;
+                if constexpr (DT == DT_F32) {
+                    *reinterpret_cast<f32x4*>(o + ch * 4) = f32x4{y[0], y[1], y[2], y[3]};
+                } else {
+                    using E = typename std::conditional<DT == DT_F16, _Float16, __bf16>::type;
+                    typedef E e4 __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<e4*>(o + ch * 2) = e4{(E)y[0], (E)y[1], (E)y[2], (E)y[3]};
                 }
             }
-            if (hh == 0 && a.lse) a.lse[query_row(r) / D] = (m + log2f(l)) * 0.69314718055994531f;
-        } else {
-            // (a maximum passes over NaN: a split of nothing but NaN would count as one without a key)
-            if (l != l) m = INFINITY;
-            const int64_t slot = ((int64_t)(stream * a.row_blocks + rb) * a.n_split + split) * ROWS + at;
-            float* const o = a.part_acc + slot * D;
-#pragma unroll
-            for (int ct = 0; ct < D / 32; ++ct) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    *reinterpret_cast<f32x4*>(o + 32 * ct + 8 * x + 4 * hh) =
-                        f32x4{st.acc[r][ct][4 * x] * by, st.acc[r][ct][4 * x + 1] * by, st.acc[r][ct][4 * x + 2] * by, st.acc[r][ct][4 * x + 3] * by};
-            }
-            if (hh == 0) { a.part_lm[2 * slot] = l; a.part_lm[2 * slot + 1] = m; }
         }
+        if (hh == 0 && a.lse) a.lse[query_row / D] = (m + log2f(l)) * 0.69314718055994531f;
+    } else {
+        // (a maximum passes over NaN: a split of nothing but NaN would count as one without a key)
+        if (l != l) m = INFINITY;
+        const int64_t slot = ((int64_t)(stream * a.row_blocks + rb) * a.n_split + split) * ROWS + at;
+        float* const o = a.part_acc + slot * D;
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<f32x4*>(o + 32 * ct + 8 * x + 4 * hh) =
+                    f32x4{st.acc[ct][4 * x] * by, st.acc[ct][4 * x + 1] * by, st.acc[ct][4 * x + 2] * by, st.acc[ct][4 * x + 3] * by};
+        }
+        if (hh == 0) { a.part_lm[2 * slot] = l; a.part_lm[2 * slot + 1] = m; }
     }
 }
 
