@@ -20,9 +20,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          # packed-fp32 VALU forms are kept off on the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
-# Accumulators of these kernels' matrix instructions in vector registers: the vector unit scales them now and then, and from the accumulation registers
+# Accumulators of the prompt kernels' matrix instructions in vector registers: the vector unit scales them now and then, and from the accumulation registers
 # each of them would be moved over and back (prompt of 4096 tokens, head dimension 256: 183 us against 258).
-SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("prompt.hip", "coded_prompt.hip")}
+SOURCE_FLAGS = {"prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def source_hash() -> str:

@@ -36,6 +36,7 @@ struct PromptCall {
     int S, Hq, Hkv, G, D, dtype, format;
     int n_split, row_blocks, block_rows;
 };
+constexpr int kPromptSplits = 64;
 // Tiles of 64 keys that the rows of the last block, which see most, see of a sequence of N tokens.
 inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int64_t window) {
     const int64_t oldest = N - last_queries - window, from = oldest < 0 ? 0 : oldest / 64, front = ((sinks < N ? sinks : N) + 63) / 64;
@@ -52,11 +53,11 @@ inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu
         if (n > tiles) tiles = n;
     }
     const int64_t wgs = streams * a->row_blocks, want = 2 * n_cu;
-    int64_t split = wgs >= n_cu ? 1 : (want + wgs - 1) / wgs;
+    int64_t split = 2 * wgs >= want ? 1 : (want + wgs - 1) / wgs;
     const int64_t most = (int64_t)(room / ((size_t)wgs * a->block_rows * (a->D + 2) * sizeof(float)));
     if (split > tiles / 4) split = tiles / 4;
     if (split > most) split = most;
-    if (split > 64) split = 64;
+    if (split > kPromptSplits) split = kPromptSplits;
     a->n_split = split < 1 ? 1 : (int)split;
 }
 inline void place_prompt_parts(PromptCall* a, void* room) {
@@ -329,17 +330,36 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     }
 }
 
-// 64 rows of a type into LDS, straight from memory; rows behind `rows` are zeros.  Not waited for.
+// 64 rows of a type into LDS, straight from memory; rows behind `rows` are zeros.  Not waited for: s_waitcnt vmcnt(0) in front of the barrier.  (The instruction is
+// written out, since for the builtin the compiler waits in front of the next transposed read from LDS, whichever part of it that reads: the next tile was waited for
+// in the middle of this one.  It has no register output; nothing else here uses m0.)
+template <int ROWB, int NW, bool VALUES, int EB> struct RowFetch {
+    static constexpr int I = 64 * ROWB / 1024 / NW, STEP = NW * 1024;       // loads of a wave; bytes from one to the next
+    static constexpr bool SAME = STEP / ROWB % 16 == 0;             // pieces are moved alike in all of a wave's rows
+    static_assert(I >= 1, "a load for every wave");
+    int at0;
+    // where the piece comes from that lane's load u puts into its place
+    static __device__ __forceinline__ int source(int u) {
+        const uint32_t at = ((threadIdx.x >> 6) + NW * u) * 64 + (threadIdx.x & 63), row = at / (ROWB / 16), piece = at % (ROWB / 16);
+        return (int)(row * ROWB) + (VALUES ? value_piece<ROWB, EB>((int)row, (int)piece) : key_piece<ROWB>((int)row, (int)piece)) * 16;
+    }
+    __device__ __forceinline__ RowFetch() : at0(source(0)) { asm volatile("" : "+v"(at0)); }
+    __device__ __forceinline__ void operator()(const char* from, int rows, char* lds) const;
+};
 template <int ROWB, int NW, bool VALUES, int EB>
-__device__ __forceinline__ void fetch_rows(const char* from, int rows, char* lds) {
-    constexpr int PIECES = ROWB / 16, I = 64 * ROWB / 1024;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id();
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, rows * ROWB, 0x00020000);
+__device__ __forceinline__ void RowFetch<ROWB, NW, VALUES, EB>::operator()(const char* from, int rows, char* lds) const {
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const uint64_t base = (uint64_t)from;
+    i32x4 rsrc = {(int)(uint32_t)base, (int)((uint32_t)(base >> 32) & 0xFFFFu), rows * ROWB, 0x00020000};
 #pragma unroll
-    for (int u = 0; u < (I + NW - 1) / NW; ++u) {
-        const int in = wave + NW * u, at = in * 64 + lane, row = at / PIECES, piece = at % PIECES;
-        const int off = row * ROWB + (VALUES ? value_piece<ROWB, EB>(row, piece) : key_piece<ROWB>(row, piece)) * 16;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + in * 1024), 16, off, 0, 0, 0);
+    for (int y = 0; y < 4; ++y) rsrc[y] = __builtin_amdgcn_readfirstlane(rsrc[y]);
+    const uint32_t to = (uint32_t)(uint64_t)(__attribute__((address_space(3))) char*)lds;
+#pragma unroll
+    for (int u = 0; u < I; ++u) {
+        const int off = SAME ? at0 : source(u), ahead = SAME ? u * STEP : 0;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :: "s"(__builtin_amdgcn_readfirstlane((int)(to + (wave + NW * u) * 1024))), "v"(off), "s"(rsrc), "s"(ahead) : "memory");
     }
 }
 
@@ -421,12 +441,17 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
     if constexpr (!CODED) {
         QueryFrag<DT, D, 1> q;
         load_row(q);
+        // (arrived before the loop: the compiler, which does not know the loads of the tiles, would wait for them with the queries)
+#pragma unroll
+        for (int c = 0; c < QueryFrag<DT, D, 1>::N; ++c) asm volatile("" : "+v"(q.v[0][c]));
         const char* const Kh = a.K + (int64_t)stream * a.Ncap * ROWB;
         const char* const Vh = a.V + (int64_t)stream * a.Ncap * ROWB;
+        const RowFetch<ROWB, NW, false, EB> keys;
+        const RowFetch<ROWB, NW, true, EB> values;
         const auto fetch = [&](int i, int buf) {
             const int t0 = 64 * tile_of(i), rows = N - t0 < 64 ? N - t0 : 64;
-            fetch_rows<ROWB, NW, false, EB>(Kh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE);
-            fetch_rows<ROWB, NW, true, EB>(Vh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE + TILE);
+            keys(Kh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE);
+            values(Vh + (int64_t)t0 * ROWB, rows, lds + buf * 2 * TILE + TILE);
         };
         if (NBUF == 2 && i0 < i1) fetch(i0, 0);
         const auto walk = [&](auto masked, int lo, int hi) {
@@ -567,8 +592,8 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
         if (split == a.n_split - 1 && p_hi >= t0) {
             const char* const open = a.c.open + (int64_t)stream * 2 * 64 * OPEN_ROWB;
             __syncthreads();
-            fetch_rows<OPEN_ROWB, NW, false, TileType<DT>::bytes>(open, N - t0, lds);
-            fetch_rows<OPEN_ROWB, NW, true, TileType<DT>::bytes>(open + 64 * OPEN_ROWB, N - t0, lds + 64 * OPEN_ROWB);
+            RowFetch<OPEN_ROWB, NW, false, TileType<DT>::bytes>()(open, N - t0, lds);
+            RowFetch<OPEN_ROWB, NW, true, TileType<DT>::bytes>()(open + 64 * OPEN_ROWB, N - t0, lds + 64 * OPEN_ROWB);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (seen(t0)) {

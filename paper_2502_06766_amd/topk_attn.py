@@ -711,7 +711,7 @@ class TopkAttnCodedCache(_WindowAttention):
         import torch
         self.torch = torch
         self.n_seqs, self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype = n_seqs, n_q_heads, n_kv_heads, head_dim, dtype
-        self.device = torch.device("cuda", device)
+        self.device, self._rows_dtype = torch.device("cuda", device), self.torch_dtype()
         cfg = make_coded_config(n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens, dtype, format, device)
         kvb, wsb = topk_attn_coded_kv_bytes(cfg), topk_attn_coded_workspace_bytes(cfg)
         if kvb == 0 or wsb == 0:
@@ -728,12 +728,16 @@ class TopkAttnCodedCache(_WindowAttention):
     def append(self, layer, k_new, v_new, seq=-1):
         """k_new/v_new: [S, n, Hkv, d] device tensors, strided alike in any order (rows of a head together): n tokens for all sequences of the layer, or
         for `seq` (S = 1)."""
-        assert k_new.device == self.device and v_new.device == self.device and k_new.dtype == v_new.dtype == self.torch_dtype()
-        S, n, heads, d = k_new.shape
-        assert (heads, d) == (self.n_kv_heads, self.head_dim) and S == (self.n_seqs if seq < 0 else 1) and v_new.shape == k_new.shape
-        # (of one sequence, token or head: any stride)
-        (ks, kt, kh, kc), (vs, vt, vh, vc) = (tuple(st if m > 1 else 0 for st, m in zip(x.stride(), x.shape)) for x in (k_new, v_new))
-        assert kc == vc == 1 and (ks, kt, kh) == (vs, vt, vh)
+        shape, (ks, kt, kh, kc) = k_new.shape, k_new.stride()
+        S, n, heads, d = shape
+        assert k_new.device == v_new.device == self.device and k_new.dtype == v_new.dtype == self._rows_dtype
+        assert (heads, d) == (self.n_kv_heads, self.head_dim) and S == (self.n_seqs if seq < 0 else 1) and v_new.shape == shape
+        if v_new.stride() != (ks, kt, kh, kc) or kc != 1 or 1 in shape:
+            vs, vt, vh, vc = v_new.stride()                # (of one sequence, token or head: any stride)
+            ks, vs = (ks, vs) if S > 1 else (0, 0)
+            kt, vt = (kt, vt) if n > 1 else (0, 0)
+            kh, vh = (kh, vh) if heads > 1 else (0, 0)
+            assert kc == vc == 1 and (ks, kt, kh) == (vs, vt, vh)
         topk_attn_coded_append(self.h, layer, seq, k_new.data_ptr(), v_new.data_ptr(), n, ks, kt, kh, self._stream())
 
     def read(self, layer, first, n, seq=-1):
