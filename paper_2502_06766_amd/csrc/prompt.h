@@ -144,11 +144,35 @@ template <int CT> __device__ __forceinline__ bool has_no_number(uint32_t w) {
 // (8192 tokens: at 2 of 100 tiles, at 40 with no slack), and a weight stays below 2^kSlack.
 constexpr float kSlack = 8.f, kSumSlack = 5.f, kSumShift = 10.f;       // (of weights times a value scale: below 2^15 in fp16)
 
+// Whether some of a lane's words has an infinity or a NaN: the largest magnitudes, two halves at a time.
+template <int CT, int N>
+__device__ __forceinline__ bool any_no_number(const u32x4 (&w)[N]) {
+    if (CT == DT_F32) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) { const uint32_t m = w[u][y] & 0x7FFFFFFFu; top = m > top ? m : top; }
+        }
+        return top >= 0x7F800000u;
+    }
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[u][y] & 0x7FFF7FFFu));
+    }
+    constexpr uint16_t E = CT == DT_F16 ? 0x7C00 : 0x7F80;
+    return top[0] >= E || top[1] >= E;
+}
+
 // One tile of 64 keys from token t0 on.  f (and f_lo, of 32-bit rows): score times this is the exponent of two.  VSCALE: the values are times `sv` (a block's scale),
-// the weighted sum has a power of two of its own (coded_decode.hip).  MASKED: not all rows of the workgroup see all keys.
+// the weighted sum has a power of two of its own (coded_decode.hip).  MASKED: not all rows of the workgroup see all keys;
+// suspect: some value of the tile is no number.
 template <int CT, bool FRAG, bool VSCALE, bool EXACT, bool MASKED, int D, int PQ, int PP>
 __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, const QueryFrag<CT, D, PQ>& q, RowState<D>& st, float f, float f_lo, float sv,
-                                            int t0, int sinks) {
+                                            int t0, int sinks, bool suspect) {
     constexpr int EB = TileType<CT>::bytes, ROWB = D * EB, N = QueryFrag<CT, D, PQ>::N, T = D / 32;
     const int lane = lane_id(), hh = lane >> 5, row = lane & 31;
     f32x16 s[2];
@@ -247,7 +271,7 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     bool poison = false;
     if constexpr (!FRAG && MASKED) {
         uint64_t keys = 0;
-        for (int at = 0; at < 64 * ROWB; at += 1024) {
+        for (int at = 0; suspect && at < 64 * ROWB; at += 1024) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(ldsV + at + lane * 16);
             const uint64_t bad = __ballot(has_no_number<CT>(w.x) || has_no_number<CT>(w.y) || has_no_number<CT>(w.z) || has_no_number<CT>(w.w));
             if (bad) {
@@ -344,6 +368,13 @@ template <int ROWB, int NW, bool VALUES, int EB> struct RowFetch {
         return (int)(row * ROWB) + (VALUES ? value_piece<ROWB, EB>((int)row, (int)piece) : key_piece<ROWB>((int)row, (int)piece)) * 16;
     }
     __device__ __forceinline__ RowFetch() : at0(source(0)) { asm volatile("" : "+v"(at0)); }
+    // Whether some number that the wave itself has fetched (and waited for) is none.
+    template <int CT> static __device__ __forceinline__ bool no_number(const char* lds) {
+        u32x4 w[I];
+#pragma unroll
+        for (int u = 0; u < I; ++u) w[u] = *reinterpret_cast<const u32x4*>(lds + (((int)threadIdx.x >> 6) + NW * u) * 1024 + lane_id() * 16);
+        return __any(any_no_number<CT, I>(w));
+    }
     __device__ __forceinline__ void operator()(const char* from, int rows, char* lds) const;
 };
 template <int ROWB, int NW, bool VALUES, int EB>
@@ -373,8 +404,15 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
     constexpr int LDS = 2 * NBUF * TILE > 128 * OPEN_ROWB || !CODED ? 2 * NBUF * TILE : 128 * OPEN_ROWB;
     constexpr int NT = 64 * NW, ROWS = 32 * NW, FM = CODED ? FMT : CODED_E4M3;
     __shared__ __align__(16) char lds[LDS];
+    __shared__ uint32_t suspects[2][NW];                            // waves that have fetched a value that is no number
     const int lane = lane_id(), hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const auto any_suspect = [&](int buf) {
+        uint32_t x = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) x |= suspects[buf][w];
+        return __builtin_amdgcn_readfirstlane((int)x) != 0;
+    };
     // Streams next to each other (workgroups go to the XCDs in turn: a stream stays on one where their number is a multiple of eight), the last rows, which see most, first.
     const int streams = a.S * a.Hkv, stream = (int)blockIdx.x % streams, rest = (int)blockIdx.x / streams;
     const int split = rest % a.n_split, rb = a.row_blocks - 1 - rest / a.n_split;
@@ -461,13 +499,18 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
                     __syncthreads();
                     fetch(i, 0);
                 }
+                const char* const at = lds + buf * 2 * TILE;
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if (decltype(masked)::value) {
+                    const bool bad = RowFetch<ROWB, NW, true, EB>::template no_number<DT>(at + TILE);
+                    if (lane == 0) suspects[buf][wave] = bad;
+                }
                 __syncthreads();
                 if (NBUF == 2 && i + 1 < i1) fetch(i + 1, buf ^ 1);
                 const int t0 = 64 * tile_of(i);
-                const char* const at = lds + buf * 2 * TILE;
                 if (decltype(masked)::value ? seen(t0) : !idle)
-                    prompt_tile<DT, false, false, DT == DT_F32, decltype(masked)::value, D, 1, 1>(at, at + TILE, q, st, kScaleHi, kScaleLo, 1.f, t0, sinks);
+                    prompt_tile<DT, false, false, DT == DT_F32, decltype(masked)::value, D, 1, 1>(at, at + TILE, q, st, kScaleHi, kScaleLo, 1.f, t0, sinks,
+                                                                                                   decltype(masked)::value && any_suspect(buf));
             }
         };
 #pragma unroll 1
@@ -570,7 +613,7 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
                     const char* const at = lds + buf * 2 * TILE;
                     if (decltype(masked)::value ? seen(t0) : !idle) {
                         const float by = scale.x * unit_q, f = by * kScaleHi, f_lo = fmaf(by, kScaleHi, -f) + by * kScaleLo;
-                        prompt_tile<DT_F16, true, true, DT == DT_F32, decltype(masked)::value, D, PARTS, PARTS>(at, at + TILE, q, st, f, f_lo, scale.y, t0, sinks);
+                        prompt_tile<DT_F16, true, true, DT == DT_F32, decltype(masked)::value, D, PARTS, PARTS>(at, at + TILE, q, st, f, f_lo, scale.y, t0, sinks, false);
                     }
                     if (NBUF == 1) __syncthreads();
                     if (i + 1 < i1) place(NBUF == 2 ? buf ^ 1 : 0);
@@ -595,11 +638,13 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
             RowFetch<OPEN_ROWB, NW, false, TileType<DT>::bytes>()(open, N - t0, lds);
             RowFetch<OPEN_ROWB, NW, true, TileType<DT>::bytes>()(open + 64 * OPEN_ROWB, N - t0, lds + 64 * OPEN_ROWB);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const bool bad = RowFetch<OPEN_ROWB, NW, true, TileType<DT>::bytes>::template no_number<DT>(lds + 64 * OPEN_ROWB);
+            if (lane == 0) suspects[0][wave] = bad;
             __syncthreads();
             if (seen(t0)) {
                 QueryFrag<DT, D, 1> q;
                 load_row(q);
-                prompt_tile<DT, false, true, DT == DT_F32, true, D, 1, 1>(lds, lds + 64 * OPEN_ROWB, q, st, kScaleHi, kScaleLo, 1.f, t0, sinks);
+                prompt_tile<DT, false, true, DT == DT_F32, true, D, 1, 1>(lds, lds + 64 * OPEN_ROWB, q, st, kScaleHi, kScaleLo, 1.f, t0, sinks, any_suspect(0));
             }
         }
     }
