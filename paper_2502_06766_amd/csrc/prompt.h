@@ -34,7 +34,8 @@ struct PromptCall {
     float* part_acc;            // [S Hkv][row_blocks][n_split][rows of a block][D], where keys are split
     float* part_lm;             // [...][rows of a block][2]
     int S, Hq, Hkv, G, D, dtype, format;
-    int n_split, row_blocks, block_rows;
+    int n_split, chunk;         // most splits of a row block's keys, tiles of 64 keys in each
+    int row_blocks, block_rows;
 };
 constexpr int kPromptSplits = 64;
 // Tiles of 64 keys that the rows of the last block, which see most, see of a sequence of N tokens.
@@ -42,23 +43,28 @@ inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int6
     const int64_t oldest = N - last_queries - window, from = oldest < 0 ? 0 : oldest / 64, front = ((sinks < N ? sinks : N) + 63) / 64;
     return (N + 63) / 64 - from + (front < from ? front : from);
 }
-// Rows of a block, and the splits of its keys.  (room: bytes there are for partial sums)
+// Rows of a block, and the splits of its keys: runs of `chunk` tiles, as many as there are compute units, twice that where the matrix unit has
+// most of the time (512 queries at 32768 tokens: 340 and 291 us).  (room: bytes there are for partial sums.  Eight queries of four
+// sequences of 1k to 20k tokens in runs of 6 / 10 / 14 / 20 / 28 / 40 tiles, one of 20 to a compute unit: 65 / 54 / 57 / 45 / 52 / 62 us; in as many runs for every
+// sequence, the longest's of 20: 48.  64 queries of one sequence of 20000, 20 tiles to a compute unit: 55 / 47 / 47 / 41 / 48 / 61.)
 inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu) {
     const int64_t rows = a->M * a->G, streams = (int64_t)a->S * a->Hkv;
     a->block_rows = rows <= 32 ? 32 : 128;
     a->row_blocks = (int)((rows + a->block_rows - 1) / a->block_rows);
-    int64_t tiles = 1;
+    int64_t longest = 1, all = 0;
     for (int b = 0; b < a->S; ++b) {
         const int64_t n = prompt_tiles(len[b], (a->block_rows + a->G - 1) / a->G, a->sinks, a->window);
-        if (n > tiles) tiles = n;
+        longest = n > longest ? n : longest;
+        all += n;
     }
-    const int64_t wgs = streams * a->row_blocks, want = 2 * n_cu;
-    int64_t split = 2 * wgs >= want ? 1 : (want + wgs - 1) / wgs;
-    const int64_t most = (int64_t)(room / ((size_t)wgs * a->block_rows * (a->D + 2) * sizeof(float)));
-    if (split > tiles / 4) split = tiles / 4;
-    if (split > most) split = most;
-    if (split > kPromptSplits) split = kPromptSplits;
-    a->n_split = split < 1 ? 1 : (int)split;
+    const int64_t wgs = streams * a->row_blocks, want = rows >= 512 ? 2 * n_cu : n_cu;
+    int64_t most = (int64_t)(room / ((size_t)wgs * a->block_rows * (a->D + 2) * sizeof(float)));     // splits
+    if (most > kPromptSplits) most = kPromptSplits;
+    int64_t chunk = wgs >= n_cu || most < 2 ? longest : (all * a->Hkv * a->row_blocks + want - 1) / want;
+    if (chunk < 4) chunk = 4;
+    if (most > 1 && chunk < (longest + most - 1) / most) chunk = (longest + most - 1) / most;
+    a->chunk = (int)(chunk < longest ? chunk : longest);
+    a->n_split = (int)((longest + a->chunk - 1) / a->chunk);
 }
 inline void place_prompt_parts(PromptCall* a, void* room) {
     a->part_acc = static_cast<float*>(room);
@@ -359,15 +365,23 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
 // in the middle of this one.  It has no register output; nothing else here uses m0.)
 template <int ROWB, int NW, bool VALUES, int EB> struct RowFetch {
     static constexpr int I = 64 * ROWB / 1024 / NW, STEP = NW * 1024;       // loads of a wave; bytes from one to the next
-    static constexpr bool SAME = STEP / ROWB % 16 == 0;             // pieces are moved alike in all of a wave's rows
+    // pieces are moved alike 16 rows on: in every VARIANTS-th of a wave's loads (kept in registers where those are few)
+    static constexpr int VARIANTS = 16 * ROWB > STEP ? 16 * ROWB / STEP : 1;
+    static constexpr bool KEPT = VARIANTS <= 4;
     static_assert(I >= 1, "a load for every wave");
-    int at0;
+    int at[KEPT ? VARIANTS : 1];
     // where the piece comes from that lane's load u puts into its place
     static __device__ __forceinline__ int source(int u) {
         const uint32_t at = ((threadIdx.x >> 6) + NW * u) * 64 + (threadIdx.x & 63), row = at / (ROWB / 16), piece = at % (ROWB / 16);
         return (int)(row * ROWB) + (VALUES ? value_piece<ROWB, EB>((int)row, (int)piece) : key_piece<ROWB>((int)row, (int)piece)) * 16;
     }
-    __device__ __forceinline__ RowFetch() : at0(source(0)) { asm volatile("" : "+v"(at0)); }
+    __device__ __forceinline__ RowFetch() {
+#pragma unroll
+        for (int u = 0; u < (KEPT ? VARIANTS : 1); ++u) {
+            at[u] = source(u);
+            asm volatile("" : "+v"(at[u]));
+        }
+    }
     // Whether some number that the wave itself has fetched (and waited for) is none.
     template <int CT> static __device__ __forceinline__ bool no_number(const char* lds) {
         u32x4 w[I];
@@ -388,7 +402,7 @@ __device__ __forceinline__ void RowFetch<ROWB, NW, VALUES, EB>::operator()(const
     const uint32_t to = (uint32_t)(uint64_t)(__attribute__((address_space(3))) char*)lds;
 #pragma unroll
     for (int u = 0; u < I; ++u) {
-        const int off = SAME ? at0 : source(u), ahead = SAME ? u * STEP : 0;
+        const int off = KEPT ? at[u % VARIANTS] : source(u), ahead = KEPT ? u / VARIANTS * VARIANTS * STEP : 0;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                      :: "s"(__builtin_amdgcn_readfirstlane((int)(to + (wave + NW * u) * 1024))), "v"(off), "s"(rsrc), "s"(ahead) : "memory");
     }
@@ -434,7 +448,8 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
     if (to > full) to = full;
     if (from > to) from = to;
     const int n_tiles = front + to - from;
-    const int i0 = (int)((int64_t)split * n_tiles / a.n_split), i1 = (int)((int64_t)(split + 1) * n_tiles / a.n_split);
+    // (a block that sees more tiles than the call was planned for, as after a replay on a longer sequence: the last split takes them)
+    const int i0 = split * a.chunk < n_tiles ? split * a.chunk : n_tiles, i1 = split + 1 < a.n_split && i0 + a.chunk < n_tiles ? i0 + a.chunk : n_tiles;
     const auto tile_of = [&](int i) { return i < front ? i : from + (i - front); };
     // Of those, all rows see all keys of [0, all0) (sinks), and of [all1, all2): behind the newest token that a window leaves out, up to the first row's.
     const int last_hidden = hidden_of(p_hi), up_to = (p_lo + 1) / 64;
@@ -630,9 +645,9 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
 #pragma unroll
             for (int i = 0; i < 16; ++i) st.acc[ct][i] *= CodeUnit<FM>::value;
         }
-        // ---- open rows, in their own type, with the last split ----
+        // ---- open rows, in their own type, with the last blocks ----
         const int t0 = 64 * full;
-        if (split == a.n_split - 1 && p_hi >= t0) {
+        if (p_hi >= t0 && (i1 == n_tiles && (i0 < i1 || split == 0))) {
             const char* const open = a.c.open + (int64_t)stream * 2 * 64 * OPEN_ROWB;
             __syncthreads();
             RowFetch<OPEN_ROWB, NW, false, TileType<DT>::bytes>()(open, N - t0, lds);
@@ -684,6 +699,8 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
         if (l != l) m = INFINITY;
         const int64_t slot = ((int64_t)(stream * a.row_blocks + rb) * a.n_split + split) * ROWS + at;
         float* const o = a.part_acc + slot * D;
+        if (hh == 0) { a.part_lm[2 * slot] = l; a.part_lm[2 * slot + 1] = m; }
+        if (m == -INFINITY) return;                                 // (no key that the row sees: the joint does not look at the sum)
 #pragma unroll
         for (int ct = 0; ct < D / 32; ++ct) {
 #pragma unroll
@@ -691,7 +708,6 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
                 *reinterpret_cast<f32x4*>(o + 32 * ct + 8 * x + 4 * hh) =
                     f32x4{st.acc[ct][4 * x] * by, st.acc[ct][4 * x + 1] * by, st.acc[ct][4 * x + 2] * by, st.acc[ct][4 * x + 3] * by};
         }
-        if (hh == 0) { a.part_lm[2 * slot] = l; a.part_lm[2 * slot + 1] = m; }
     }
 }
 
