@@ -240,7 +240,10 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
             f16x8 hi[2], lo[2];
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-                const float w = p[x] * g;
+                // (the product is a number of its own: rounded to 16 bits together with the multiplication in one place and after it in the other, the two
+                // parts did not make up the weight now and then, 2^-11 of one key's)
+                float w = p[x] * g;
+                asm("" : "+v"(w));
                 hi[x / 8][x % 8] = (_Float16)w;
                 lo[x / 8][x % 8] = (_Float16)(w - (float)hi[x / 8][x % 8]);      // (two parts: 2^-22 of a weight)
             }

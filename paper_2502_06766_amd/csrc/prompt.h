@@ -333,6 +333,7 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             float rest = s[i / 16][i % 16];
+            if (PP > 1) asm("" : "+v"(rest));                        // (not rounded together with the multiplication in front of it: coded_decode.hip)
 #pragma unroll
             for (int z = 0; z < PP; ++z) {
                 p[z][i / 8][i % 8] = (E)rest;
@@ -562,7 +563,7 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
                         Elem<DT>::widen(*reinterpret_cast<const u32x4*>(query + (16 * c + 8 * hh + y) * TileType<DT>::bytes), x + y);
 #pragma unroll
                     for (int y = 0; y < 8; ++y) {
-                        float left = x[y] * by;
+                        float left = x[y] * by;                     // (exact)
 #pragma unroll
                         for (int z = 0; z < PARTS; ++z) {
                             q.v[z][c][y] = (_Float16)left;

@@ -311,6 +311,36 @@ def test_sums_of_many_equal_weights(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,prompt", [(wl.F32, False), (wl.F16, False), (wl.BF16, False), (wl.F32, True)])
+def test_every_weight_to_its_last_bits(dtype, prompt, fmt):
+    """A block of 64 keys whose values have a channel each: every weight shows by itself, 8192 of them a call.  One channel of scores: their sum is exact, what is
+    left are the roundings of the exponent (10 u of it), of the exponential and the value scale (6 u), of the parts a weight is held in (2^-22; those of
+    a prompt of 16-bit rows are rounded once: test_prompt), of 64 additions and of the quotient."""
+    d = n = 64
+    Hq = 128
+    g = np.random.default_rng(31)
+    for _ in range(12):
+        K, V = np.zeros((1, n, d)), np.zeros((1, n, d))
+        K[0, :, 0] = g.standard_normal(n)
+        V[0, np.arange(n), g.permutation(d)] = g.uniform(0.5, 1.0)
+        rows = tuple(wl.quantize(x.astype(np.float32), dtype) for x in (K, V))
+        q = np.zeros((1, Hq, d))
+        q[0, :, 0] = 16.0 * g.standard_normal(Hq)
+        q = wl.quantize(q.astype(np.float32), dtype)
+        cache, got = filled([n], Hq, 1, d, n, dtype, fmt, rows=[rows])
+        try:
+            out = cache.prompt(0, up(q, dtype)[:, None])[0][0, 0] if prompt else cache.decode(0, up(q, dtype))[0][0]
+            want, _ = ref.attend(wl.widen(q, dtype).astype(np.float64), got[0][2], got[0][3], 0, n)
+            s = np.abs(wl.widen(q[0], dtype)[:, 0]).max() * np.abs(got[0][2]).max() / 8.0
+            tol = 2 * (10 * U * s + 6 * U + 2.0 ** -22) + (64 + 3) * U
+            off = np.abs(out.float().cpu().numpy() - want[0])
+            small = 2.0 ** -30 * np.abs(got[0][3]).max()             # (weights are held relative to the largest: 2^-38 of it)
+            assert (off <= tol * np.abs(want[0]) + small).all(), f"{np.max(off / (np.abs(want[0]) + small)):.3g} of a weight, {tol:.3g} allowed"
+        finally:
+            cache.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_what_is_not_seen_has_no_effect(dtype, fmt):
     """NaN and infinities outside the window, in blocks of their own, in the open rows and behind the sequence: the others' results as without them; a
