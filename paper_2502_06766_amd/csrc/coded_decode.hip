@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
         const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            p[i] = there[i] ? __builtin_amdgcn_exp2f(fmaf(s[i], kScaleHi, fmaf(s[i], kScaleLo, -ref))) : 0.f;
+            p[i] = there[i] && s[i] != -INFINITY ? __builtin_amdgcn_exp2f(fmaf(s[i], kScaleHi, fmaf(s[i], kScaleLo, -ref))) : 0.f;
             l += p[i];
         }
         e_w = m;

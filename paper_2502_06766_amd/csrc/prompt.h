@@ -259,7 +259,7 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     for (int i = 0; i < 32; ++i) {
         const float x = s[i / 16][i % 16];
         float w = __builtin_amdgcn_exp2f(EXACT ? fmaf(x, f, fmaf(x, f_lo, -ref)) : fmaf(x, f, -ref));
-        if ((VSCALE || EXACT) && MASKED && x == -INFINITY) w = 0.f;  // (a factor of zero, or of two parts)
+        if (((VSCALE && MASKED) || EXACT) && x == -INFINITY) w = 0.f;  // (a factor of zero, or of two parts)
         s[i / 16][i % 16] = w;
         sum[i & 1] += w;
     }

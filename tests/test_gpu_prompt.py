@@ -306,3 +306,40 @@ def test_refusals():
             cache.decode_sinks(0, torch.zeros((2, Hq, d), dtype=torch.float16, device=DEV), 5)
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_keys_of_minus_infinity_have_no_weight(dtype, coded, d):
+    """A key whose score is -inf counts for nothing, in tiles that all rows see too; one whose score is +inf makes the row NaN."""
+    Hq, Hkv, n, M = 4, 2, 170, 40
+    g = np.random.default_rng(11)
+    K, V, q = draw(g, Hkv, n, d, dtype=dtype), draw(g, Hkv, n, d, dtype=dtype), draw(g, 1, M, Hq, d, dtype=dtype)
+    at = [133, 140] if coded else [5, 70, 133]                   # (rows of full blocks would make the block NaN)
+    for t in at:
+        K[:, t, 3] = wl.quantize(np.array([-np.inf], np.float32), dtype)[0]
+    q[..., 3] = wl.quantize(np.abs(wl.widen(q[..., 3], dtype)).astype(np.float32) + np.float32(0.5), dtype)
+    q[:, :, 1, 3] = wl.quantize(-np.abs(wl.widen(q[:, :, 1, 3], dtype)).astype(np.float32), dtype)
+    if coded:
+        cache = ta.TopkAttnCodedCache(1, 1, Hq, Hkv, d, 256, dtype)
+        cache.append(0, *(up(np.ascontiguousarray(x.transpose(1, 0, 2))[None], dtype) for x in (K, V)))
+        seen = [np.stack([ref.held(wide(x, dtype)[h], ref.INT8) for h in range(Hkv)]) for x in (K, V)]
+    else:
+        cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, 256, 16, dtype)
+        cache.append(0, 0, up(K, dtype), up(V, dtype), head_major=True)
+        seen = wide(K, dtype), wide(V, dtype)
+    out, lse = cache.prompt(0, up(q, dtype))
+    one, one_lse = (cache.decode if coded else lambda *a: cache.decode_sinks(*a, 10 ** 6))(0, up(q[:, -1], dtype))
+    for o, l, qq, token in ((out, lse, q, False), (one[:, None], one_lse[:, None], q[:, -1:], True)):
+        o, l = o[0].double().cpu().numpy(), l[0].double().cpu().numpy()
+        reached = np.arange(n - qq.shape[1], n) >= at[0]
+        assert np.isnan(o[reached][:, 1]).all()
+        keep = [h for h in range(Hq) if h != 1]
+        with np.errstate(invalid="ignore"):
+            w_out, w_lse = ref.attend(wide(qq, dtype)[0], *seen, 0, n)
+        K0 = np.where(np.isinf(seen[0]), 0, seen[0])
+        tol = 2 * (weight_error(wide(q, dtype)[0], K0, d) + (n / 16 + 64) * U + 2.0 ** -22 + (0 if token or dtype == wl.F32 else HALF[dtype])) * np.abs(seen[1]).max()
+        tol = tol + (0 if token else HALF[dtype]) * np.abs(w_out[:, keep])
+        assert np.isfinite(w_out[:, keep]).all() and (np.abs(o - w_out)[:, keep] <= tol).all()
+        assert (np.abs(l - w_lse)[:, keep] <= weight_error(wide(q, dtype)[0], K0, d) + (n / 16 + 64) * U + 8 * U * (1 + np.abs(w_lse[:, keep]))).all()
