@@ -350,9 +350,11 @@ int topk_attn_decode_layers(topk_attn_t* h, int layer0, int n_layers, const void
  *   INT8  scale = amax / 127 rounded to 32 bits and then to 16 significant ones (down, where 127 scale would overflow); code = the integer nearest to x / scale, ties to even: within scale / 2
  *   E4M3  scale = the smallest power of two with amax <= 448 scale; code = x / scale rounded to e4m3 (4 exponent bits, 3 of fraction): within 2^-4 of x, and
  *         within 2^-10 scale where x is below 2^-6 scale.  For rows with a few channels far above the others.
- * A row reads as code * scale, in 32 bits or more; amax below 2^-100 reads as zeros; a block with a NaN or an infinity reads as NaN, all of it.
+ * A row reads as code * scale, in 32 bits or more; amax below 2^-100 reads as zeros; a block with a NaN or an infinity reads as NaN, all of it.  (E4M3: a number within
+ * 2^-4 of the largest one of `dtype` may be rounded beyond it, and read back as an infinity.)
  * The handle is one of its own beside topk_attn_t, with the same rules: caller-owned memory, nothing allocated or synchronised after create, calls on a handle must not
- * overlap, argument errors leave it unchanged, appends and resets are not to be replayed from a HIP graph. */
+ * overlap, argument errors leave it unchanged, appends and resets are not to be replayed from a HIP graph, reads,
+ * decodes and prompts as topk_attn_decode_dense. */
 typedef struct topk_attn_coded topk_attn_coded_t;
 enum { TOPK_ATTN_CODED_INT8 = 0, TOPK_ATTN_CODED_E4M3 = 1 };
 typedef struct {
@@ -379,7 +381,7 @@ int topk_attn_coded_destroy(topk_attn_coded_t* h);
 
 /* Append n_new tokens to sequence `seq` of `layer`, or to each of its sequences (seq = -1): element (s, t, h, c) of the call's s-th sequence at
  * base[s * seq_stride + t * token_stride + h * head_stride + c] in `dtype` (strides in elements, rows 16-byte aligned, in any order: parts of a fused projection or another
- * cache's heads).  Errors: EINVAL (null, range, misaligned, a negative stride), ECAPACITY (nothing is enqueued then), EUNSUPPORTED (2^24 or more workgroups: two per 64 tokens
+ * cache's heads).  Errors: EINVAL (null, range, misaligned, a stride below 0 or from 2^40 on), ECAPACITY (nothing is enqueued then), EUNSUPPORTED (2^24 or more workgroups: two per 64 tokens
  * and KV head).  n_new == 0 is a no-op. */
 int topk_attn_coded_append(topk_attn_coded_t* h, int layer, int seq, const void* k_new, const void* v_new, int64_t n_new,
                            int64_t seq_stride, int64_t token_stride, int64_t head_stride, void* hip_stream);

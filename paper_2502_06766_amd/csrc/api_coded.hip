@@ -98,10 +98,10 @@ CodedArrays arrays_of(const topk_attn_coded* h, int layer, int seq) {
 bool range_ok(const topk_attn_coded_t* h, int layer, int seq) {
     return h && layer >= 0 && layer < h->cfg.n_layers && seq >= -1 && seq < h->cfg.n_seqs;
 }
-// strides in elements that a call's rows may have: pieces of 16 bytes
+// strides in elements that a call's rows may have: pieces of 16 bytes, below 2^40 (times 65535 sequences they fit 64 bits)
 bool strides_ok(int64_t seq, int64_t token, int64_t head, int e) {
     for (const int64_t x : {seq, token, head})
-        if (x < 0 || x > INT64_MAX / 8 || ((x * e) & 15)) return false;
+        if (x < 0 || x >= (int64_t)1 << 40 || ((x * e) & 15)) return false;
     return true;
 }
 
