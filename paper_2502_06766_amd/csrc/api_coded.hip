@@ -70,7 +70,7 @@ Workspace workspace_of(const topk_attn_coded_config* c) {
     size_t o = 0;
     const auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes); return at; };
     w.len = take((size_t)c->n_layers * c->n_seqs * sizeof(int32_t));
-    w.arrive = take((size_t)units * sizeof(uint32_t));
+    w.arrive = take((size_t)c->n_seqs * c->n_kv_heads * (size_t)std::max<int64_t>((G + 15) / 16, kFewRows / 16) * sizeof(uint32_t));
     // splits that fill the chip, and no more than 256 blocks a split (64 a wave, whose sums follow each other); one of open rows
     w.max_splits = std::min<int64_t>(kMaxSplits, 1 + std::min<int64_t>(std::max<int64_t>(blocks, 1), std::max<int64_t>(4096 / units, blocks / 256) + 1));
     size_t parts = (size_t)c->n_seqs * c->n_q_heads * (size_t)w.max_splits * (c->head_dim + 2) * sizeof(float);
@@ -103,6 +103,45 @@ bool strides_ok(int64_t seq, int64_t token, int64_t head, int e) {
     for (const int64_t x : {seq, token, head})
         if (x < 0 || x >= (int64_t)1 << 40 || ((x * e) & 15)) return false;
     return true;
+}
+
+// Splits of `rows` rows of each key stream that there is room for.
+int64_t split_room(const topk_attn_coded_config& c, const Workspace& ws, int seqs, int64_t rows) {
+    return (int64_t)(ws.parts_bytes / ((size_t)seqs * c.n_kv_heads * (size_t)rows * (c.head_dim + 2) * sizeof(float)));
+}
+
+// The kernel over few rows of each of B sequences from b0 on.
+int decode_rows(topk_attn_coded* h, int layer, int b0, CodedDecodeCall a, void* hip_stream) {
+    const topk_attn_coded_config& c = h->cfg;
+    const int64_t* const len = &h->len[(size_t)layer * c.n_seqs + b0];
+    int64_t longest = 0;
+    int open = 0;
+    for (int b = 0; b < a.B; ++b) {
+        const CodedWalk w(len[b], a.sinks, a.reach);
+        longest = std::max(longest, w.blocks());
+        open |= w.open();
+    }
+    const Workspace ws = workspace_of(&c);
+    a.a = arrays_of(h, layer, b0);
+    a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = c.n_q_heads / c.n_kv_heads; a.D = c.head_dim; a.dtype = c.dtype; a.format = c.format;
+    a.row_blocks = (a.rows + 15) / 16;
+    int64_t sample[16];                          // (of a larger batch some sequences stand for all)
+    const int n_sample = std::min(a.B, 16);
+    for (int i = 0; i < n_sample; ++i) sample[i] = std::max<int64_t>(1, CodedWalk(len[(int64_t)i * a.B / n_sample], a.sinks, a.reach).blocks());
+    // splits that there is room for, one of them of open rows
+    const int64_t most = std::min<int64_t>(a.M ? kMaxSplits : ws.max_splits, split_room(c, ws, a.B, a.rows)) - 1;
+    a.chunk = longest ? (int)pages_per_split(sample, n_sample, (double)a.B / n_sample * a.Hkv * a.row_blocks, longest, most, h->n_cu, (double)c.head_dim) : 1;
+    a.chunk = (int)std::min<int64_t>(a.chunk, std::max<int64_t>(256, (longest + most - 1) / most));
+    a.n_split = (int)((longest + a.chunk - 1) / a.chunk) + open;
+    char* const base = static_cast<char*>(c.workspace);
+    a.part_acc = reinterpret_cast<float*>(base + ws.parts);
+    a.part_lm = a.part_acc + (size_t)a.B * a.Hkv * a.rows * a.n_split * a.D;
+    a.arrive = reinterpret_cast<uint32_t*>(base + ws.arrive);
+    a.join_later = (int64_t)a.n_split * std::min(a.rows, 16) * a.D * 4 > kJoinBytes;
+    if (coded_decode_wgs(a) > kMostWorkgroups || (int64_t)a.B * a.Hkv * a.rows > kMostWorkgroups) return TOPK_ATTN_EUNSUPPORTED;
+    const DeviceOf device(c.device);
+    if (!device.ok()) return TOPK_ATTN_EDEVICE;
+    return launch_coded_decode(a, (hipStream_t)hip_stream) == hipSuccess ? TOPK_ATTN_OK : TOPK_ATTN_EDEVICE;
 }
 
 __global__ void set_lens_kernel(int32_t* len, int n) {
@@ -234,38 +273,12 @@ int topk_attn_coded_read(topk_attn_coded_t* h, int layer, int seq, int64_t first
 
 int topk_attn_coded_decode(topk_attn_coded_t* h, int layer, const void* q, int64_t sinks, int64_t window, float* out, float* lse, void* hip_stream) {
     if (!h || !q || !out || layer < 0 || layer >= h->cfg.n_layers || ((uintptr_t)q & 15) || sinks < 0 || window < 1) return TOPK_ATTN_EINVAL;
-    const topk_attn_coded_config& c = h->cfg;
-    const int64_t* const len = &h->len[(size_t)layer * c.n_seqs];
-    int64_t longest = 0;
-    int open = 0;
-    for (int b = 0; b < c.n_seqs; ++b) {
-        if (len[b] < 1) return TOPK_ATTN_EINVAL;
-        const CodedWalk w(len[b], sinks, window);
-        longest = std::max(longest, w.blocks());
-        open |= w.open();
-    }
-    const Workspace ws = workspace_of(&c);
+    for (int b = 0; b < h->cfg.n_seqs; ++b)
+        if (h->len[(size_t)layer * h->cfg.n_seqs + b] < 1) return TOPK_ATTN_EINVAL;
     CodedDecodeCall a{};
-    a.a = arrays_of(h, layer, 0);
-    a.q = q; a.out = out; a.lse = lse; a.sinks = sinks; a.window = window;
-    a.B = c.n_seqs; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = c.n_q_heads / c.n_kv_heads; a.D = c.head_dim; a.dtype = c.dtype; a.format = c.format;
-    a.row_blocks = (a.G + 15) / 16;
-    int64_t sample[16];                          // (of a larger batch some sequences stand for all)
-    const int n_sample = std::min(c.n_seqs, 16);
-    for (int i = 0; i < n_sample; ++i) sample[i] = std::max<int64_t>(1, CodedWalk(len[(int64_t)i * c.n_seqs / n_sample], sinks, window).blocks());
-    const int64_t most = ws.max_splits - 1;      // (one of open rows)
-    a.chunk = longest ? (int)pages_per_split(sample, n_sample, (double)c.n_seqs / n_sample * a.Hkv * a.row_blocks, longest, most, h->n_cu, (double)c.head_dim) : 1;
-    a.chunk = (int)std::min<int64_t>(a.chunk, std::max<int64_t>(256, (longest + most - 1) / most));
-    a.n_split = (int)((longest + a.chunk - 1) / a.chunk) + open;
-    char* const base = static_cast<char*>(c.workspace);
-    a.part_acc = reinterpret_cast<float*>(base + ws.parts);
-    a.part_lm = a.part_acc + (size_t)a.B * a.Hq * a.n_split * a.D;
-    a.arrive = reinterpret_cast<uint32_t*>(base + ws.arrive);
-    a.join_later = (int64_t)a.n_split * std::min(a.G, 16) * a.D * 4 > kJoinBytes;
-    if (coded_decode_wgs(a) > kMostWorkgroups || (int64_t)a.B * a.Hq > kMostWorkgroups) return TOPK_ATTN_EUNSUPPORTED;
-    const DeviceOf device(c.device);
-    if (!device.ok()) return TOPK_ATTN_EDEVICE;
-    return launch_coded_decode(a, (hipStream_t)hip_stream) == hipSuccess ? TOPK_ATTN_OK : TOPK_ATTN_EDEVICE;
+    a.q = q; a.out = out; a.lse = lse; a.sinks = sinks; a.window = a.reach = window;
+    a.B = h->cfg.n_seqs; a.rows = h->cfg.n_q_heads / h->cfg.n_kv_heads;
+    return decode_rows(h, layer, 0, a, hip_stream);
 }
 
 int topk_attn_coded_prompt(topk_attn_coded_t* h, int layer, int seq, const void* q, int64_t n_queries, int64_t sinks, int64_t window, void* out,
@@ -279,6 +292,14 @@ int topk_attn_coded_prompt(topk_attn_coded_t* h, int layer, int seq, const void*
     if (n_queries == 0) return TOPK_ATTN_OK;
     if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return TOPK_ATTN_EINVAL;
     const Workspace ws = workspace_of(&c);
+    const int64_t rows = n_queries * (c.n_q_heads / c.n_kv_heads);
+    if (rows <= few_rows(c.dtype, c.head_dim) && split_room(c, ws, S, rows) >= 2) {      // (blocks and open rows)
+        CodedDecodeCall a{};
+        a.q = q; a.out_rows = out; a.lse = lse; a.sinks = sinks; a.window = window;
+        a.reach = std::min(window, (int64_t)1 << 40) + n_queries - 1;
+        a.B = S; a.M = (int)n_queries; a.rows = (int)rows;
+        return decode_rows(h, layer, b0, a, hip_stream);
+    }
     PromptCall a{};
     a.c = arrays_of(h, layer, b0);
     a.q = q; a.out = out; a.lse = lse; a.len = a.c.len;

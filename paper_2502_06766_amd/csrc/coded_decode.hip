@@ -7,6 +7,8 @@
 // to finish joins them.
 //
 // Bound by the read of the codes: 16 KB per 64 keys and KV head (d = 128) against 48 MFMA and some 500 vector instructions, a sixth of the time the read takes.
+#include <type_traits>
+
 #include "coded.h"
 #include "scan_tiles.h"
 #include "split_join.h"
@@ -25,9 +27,29 @@ __device__ __forceinline__ float top_of_rows(float v) {        // largest of lan
 // 2^x for a whole number x (0 for -inf)
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Where 16 rows of a key stream go, from the row0-th on, if they are those of a prompt's tokens.
+template <int DT> struct JoinedRows {
+    const CodedDecodeCall& a;
+    int stream, row0;
+    __device__ __forceinline__ int64_t at(int h) const {
+        const int row = row0 + h, m = row / a.G, b = stream / a.Hkv;
+        return ((int64_t)b * a.M + m) * a.Hq + (stream - b * a.Hkv) * a.G + (row - m * a.G);
+    }
+    __device__ __forceinline__ void one(int h, int c, float v) const {
+        using E = typename std::conditional<DT == DT_F32, float, typename std::conditional<DT == DT_F16, _Float16, __bf16>::type>::type;
+        static_cast<E*>(a.out_rows)[at(h) * a.D + c] = (E)v;
+    }
+    __device__ __forceinline__ void sum(int h, int c, f32x4 v) const {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) one(h, c + y, v[y]);
+    }
+    __device__ __forceinline__ void lse(int h, float v) const { if (a.lse) a.lse[at(h)] = v; }
+};
+
 }  // namespace
 
-template <int DT, int D, int FMT>
+// ROWS: of the last M tokens.
+template <int DT, int D, int FMT, bool ROWS>
 __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded_decode_kernel(CodedDecodeCall a) {
     constexpr int T = D / 16, C = D / 32, UK = D / 16, ROW = D * Elem<DT>::kBytes, EPL = Elem<DT>::kPerLoad, PARTS = QueryParts<DT>::value;
     constexpr int NW = 4, NT = NW * kWave, RED = NW * 16 * (D + 4), JOIN = 16 * kMaxSplits + 8 * NT;
@@ -50,15 +72,23 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
     int stream = unit - split * streams - split % streams;
     if (stream < 0) stream += streams;
     const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
-    const CodedWalk seen(a.a.len[b], a.sinks, a.window);
+    const CodedWalk seen(a.a.len[b], a.sinks, ROWS ? a.reach : a.window);
     const int open = seen.open() ? 1 : 0;
     const int64_t blocks = seen.blocks();
     int ns = (int)((blocks + a.chunk - 1) / a.chunk);
     ns = (ns < a.n_split - open ? ns : a.n_split - open) + open;
     if (split >= ns) return;
-    const int heads = a.G - 16 * rb < 16 ? a.G - 16 * rb : 16;
-    const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G + 16 * rb;
-    const char* const query = static_cast<const char*>(a.q) + (head0 + (n < heads ? n : 0)) * ROW;
+    const int heads = a.rows - 16 * rb < 16 ? a.rows - 16 * rb : 16;
+    const int64_t head0 = (int64_t)stream * a.rows + 16 * rb;
+    const JoinedRows<DT> to_rows{a, stream, 16 * rb};
+    const char* const query = static_cast<const char*>(a.q) + (ROWS ? to_rows.at(n < heads ? n : 0) : head0 + (n < heads ? n : 0)) * ROW;
+    // what the lane's row sees, and what all rows do
+    const int64_t pos = ROWS ? seen.N - a.M + (16 * rb + (n < heads ? n : 0)) / a.G : 0;
+    const auto sees = [&](int64_t t) { return ROWS ? t <= pos && (t < a.sinks || t > pos - a.window) : seen.sees(t); };
+    const auto all_see = [&](int64_t block) {
+        const int64_t t0 = block * kCodedBlock, t1 = t0 + kCodedBlock;
+        return ROWS ? t1 <= seen.N - a.M + 1 && (t0 > seen.N - 1 - a.window || t1 <= a.sinks) : seen.whole(block);
+    };
     // log2(e) / sqrt(D) as two numbers: the rounding of one would be a part of every score
     constexpr double kScale = 1.4426950408889634 / (D == 32 ? 5.656854249492381 : D == 64 ? 8.0 : D == 128 ? 11.313708498984761 : 16.0);
     constexpr float kScaleHi = (float)kScale, kScaleLo = (float)(kScale - (double)kScaleHi);
@@ -92,7 +122,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
         bool there[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            there[i] = 16 * wave + 4 * j + i < rows && seen.sees(t0 + i);
+            there[i] = 16 * wave + 4 * j + i < rows && sees(t0 + i);
             if (there[i]) top = fmaxf(top, s[i] * kScaleHi);
         }
         m = ceilf(top_of_rows(top));
@@ -105,19 +135,40 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
         e_w = m;
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            // (a row that is not seen is taken as zeros: no weight of zero meets an infinity)
+            // (a row that is not seen is taken as zeros: no weight of zero meets an infinity.  Where rows see different tokens, what is no number is, and
+            // goes to those that see it, one token at a time.)
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int off = (16 * wave + 4 * j + i) * ROW + (16 * t + n) * Elem<DT>::kBytes;
-                float v;
+            const auto value = [&](int key, int c) {
+                const int off = (16 * wave + key) * ROW + c * Elem<DT>::kBytes;
                 if constexpr (DT == DT_F32) {
-                    v = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0));
+                    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0));
                 } else {
                     const uint16_t bits = __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, 0);
-                    v = DT == DT_F16 ? (float)__builtin_bit_cast(_Float16, bits) : __uint_as_float((uint32_t)bits << 16);
+                    return DT == DT_F16 ? (float)__builtin_bit_cast(_Float16, bits) : __uint_as_float((uint32_t)bits << 16);
                 }
-                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(there[i] ? v : 0.f, p[i], acc, 0, 0, 0);
+            };
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v = value(4 * j + i, 16 * t + n);
+                const bool number = fabsf(v) < INFINITY;
+                odd |= !number;
+                if (ROWS ? !number : !there[i]) v = 0.f;
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[i], acc, 0, 0, 0);
+            }
+            if (ROWS && __any(odd)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    for (int y = 0; y < 4; ++y) {
+                        const float w = __shfl(p[i], 16 * y + n, 64);
+                        const bool sees_it = __shfl((int)there[i], 16 * y + n, 64);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float v = value(4 * y + i, 16 * t + 4 * j + r);
+                            if (sees_it && !(fabsf(v) < INFINITY)) acc[r] = fmaf(w, v, acc[r]);
+                        }
+                    }
+                }
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) red[wave][n][16 * t + 4 * j + r] = acc[r];
@@ -192,12 +243,12 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
             }
             // score times log2(e) / sqrt(D), in two parts: f + f_lo is the factor to 2^-48
             const float by = t.scale.x * unit_q, f = by * kScaleHi, f_lo = fmaf(by, kScaleHi, -f) + by * kScaleLo;
-            const bool whole = seen.whole(block);
+            const bool whole = all_see(block);
             float top = -INFINITY, p[16];
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
                 float v = s[x / 4][x % 4] * f;
-                if (!whole && !seen.sees(block * kCodedBlock + 16 * (x / 4) + 4 * j + x % 4)) v = -INFINITY;
+                if (!whole && !sees(block * kCodedBlock + 16 * (x / 4) + 4 * j + x % 4)) v = -INFINITY;
                 p[x] = v;
                 top = fmaxf(top, v);
             }
@@ -228,6 +279,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
                 const float up = fminf(ref - e_new + kShift, (float)(127 - ke));
                 g = ldexpf(sv, (int)fmaxf(up, -300.f));
             }
+            if (ROWS && bm == -INFINITY) g = 0.f;                    // (a block of NaN that the row does not see)
             if (__any(e_new != e_w)) {
                 const float f_w = e_w == -INFINITY ? 1.f : power2(e_w - e_new);
 #pragma unroll
@@ -308,8 +360,14 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
         }
         const int64_t bh = head0 + h;
         if (alone && !a.join_later) {
-            a.out[bh * D + c] = sum * (1.0f / total);
-            if (c == 0 && a.lse) a.lse[bh] = (top + log2f(total)) * 0.69314718055994531f;
+            const float o = sum * (1.0f / total), lse = (top + log2f(total)) * 0.69314718055994531f;
+            if (ROWS) {
+                to_rows.one(h, c, o);
+                if (c == 0) to_rows.lse(h, lse);
+            } else {
+                a.out[bh * D + c] = o;
+                if (c == 0 && a.lse) a.lse[bh] = lse;
+            }
         } else {
             put(&a.part_acc[(bh * a.n_split + split) * D + c], sum);
             if (c == 0) {
@@ -327,33 +385,48 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
     __syncthreads();
     if (arrived + 1u != (uint32_t)ns) return;
     if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    join_splits<NT>(a, head0, heads, ns, 0.f, lds, reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits));
+    f32x4* const room = reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits);
+    if constexpr (ROWS) join_splits<NT>(a, head0, to_rows, heads, ns, 0.f, lds, room);
+    else join_splits<NT>(a, head0, heads, ns, 0.f, lds, room);
 }
 
-// A workgroup per head: many splits of many heads.
+// A workgroup per head: many splits of many heads.  ROWS: of the last tokens' rows, of type DT.
+template <int DT, bool ROWS>
 __global__ void __launch_bounds__(256) coded_join_kernel(CodedDecodeCall a) {
     __shared__ float f[kMaxSplits];
     __shared__ f32x4 sums[512];
     const int64_t head = blockIdx.x;
-    const CodedWalk seen(a.a.len[head / a.Hq], a.sinks, a.window);
+    const int stream = (int)(head / a.rows);
+    const CodedWalk seen(a.a.len[stream / a.Hkv], a.sinks, ROWS ? a.reach : a.window);
     const int open = seen.open() ? 1 : 0;
     int ns = (int)((seen.blocks() + a.chunk - 1) / a.chunk);
     ns = (ns < a.n_split - open ? ns : a.n_split - open) + open;
-    join_splits<256>(a, head, 1, ns, 0.f, f, sums);
+    if constexpr (ROWS) join_splits<256>(a, head, JoinedRows<DT>{a, stream, (int)(head - (int64_t)stream * a.rows)}, 1, ns, 0.f, f, sums);
+    else join_splits<256>(a, head, 1, ns, 0.f, f, sums);
 }
 
 hipError_t launch_coded_decode(const CodedDecodeCall& a, hipStream_t st) {
     const dim3 grid((unsigned)coded_decode_wgs(a)), wg(256);
+#define TKA_DECODE_(DT_, D_, FMT_)                                                                                        \
+    do {                                                                                                                  \
+        if (a.M) hipLaunchKernelGGL((coded_decode_kernel<DT_, D_, FMT_, true>), grid, wg, 0, st, a);                      \
+        else hipLaunchKernelGGL((coded_decode_kernel<DT_, D_, FMT_, false>), grid, wg, 0, st, a);                         \
+    } while (0)
 #define TKA_DECODE(DT_, D_)                                                                                               \
     do {                                                                                                                  \
-        if (a.format == CODED_INT8) hipLaunchKernelGGL((coded_decode_kernel<DT_, D_, CODED_INT8>), grid, wg, 0, st, a);   \
-        else hipLaunchKernelGGL((coded_decode_kernel<DT_, D_, CODED_E4M3>), grid, wg, 0, st, a);                          \
+        if (a.format == CODED_INT8) TKA_DECODE_(DT_, D_, CODED_INT8);                                                     \
+        else TKA_DECODE_(DT_, D_, CODED_E4M3);                                                                            \
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_DECODE, a.dtype, a.D);
 #undef TKA_DECODE
+#undef TKA_DECODE_
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.join_later) return e;
-    hipLaunchKernelGGL(coded_join_kernel, dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, st, a);
+    const dim3 heads((unsigned)((int64_t)a.B * a.Hkv * a.rows));
+    if (!a.M) hipLaunchKernelGGL((coded_join_kernel<DT_F32, false>), heads, wg, 0, st, a);
+    else if (a.dtype == DT_F32) hipLaunchKernelGGL((coded_join_kernel<DT_F32, true>), heads, wg, 0, st, a);
+    else if (a.dtype == DT_F16) hipLaunchKernelGGL((coded_join_kernel<DT_F16, true>), heads, wg, 0, st, a);
+    else hipLaunchKernelGGL((coded_join_kernel<DT_BF16, true>), heads, wg, 0, st, a);
     return hipGetLastError();
 }
 

@@ -49,7 +49,7 @@ inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int6
 // sequence, the longest's of 20: 48.  64 queries of one sequence of 20000, 20 tiles to a compute unit: 55 / 47 / 47 / 41 / 48 / 61.)
 inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu) {
     const int64_t rows = a->M * a->G, streams = (int64_t)a->S * a->Hkv;
-    a->block_rows = rows <= 32 ? 32 : 128;
+    a->block_rows = rows <= 32 && a->format < 0 ? 32 : 128;          // (few rows of the 8-bit cache: coded_decode.hip)
     a->row_blocks = (int)((rows + a->block_rows - 1) / a->block_rows);
     int64_t longest = 1, all = 0;
     for (int b = 0; b < a->S; ++b) {

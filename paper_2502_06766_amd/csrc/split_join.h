@@ -41,10 +41,21 @@ __device__ __forceinline__ float head_log2_sum(const SplitParts& a, int64_t bh, 
     }
     return (top - shift) + log2f(sum);
 }
+// Where the heads of a joint go: out [heads][D] and lse [heads] of the call.
+struct JoinedHeads {
+    const SplitParts& a;
+    int64_t head0;
+    __device__ __forceinline__ void sum(int h, int c, f32x4 v) const {
+        float* const out = a.out + (head0 + h) * a.D + c;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) out[y] = v[y];
+    }
+    __device__ __forceinline__ void lse(int h, float v) const { if (a.lse) a.lse[head0 + h] = v; }
+};
 // Weighted sum of the splits of `quads` groups of four channels.  Four sums, by split modulo four, whichever thread takes them: the result does
 // not depend on how many heads are joined at a time.
-template <int NT, int SHARES>
-__device__ __forceinline__ void sum_splits(const SplitParts& a, int64_t head0, int quads, int n_split, const float* f, f32x4* part) {
+template <int NT, int SHARES, typename To>
+__device__ __forceinline__ void sum_splits(const SplitParts& a, int64_t head0, const To& to, int quads, int n_split, const float* f, f32x4* part) {
     constexpr int U = 16, SUMS = 4 / SHARES;                       // splits in flight (a trip to memory each otherwise); sums of a thread
     const __amdgpu_buffer_rsrc_t rsrc =
         __builtin_amdgcn_make_buffer_rsrc(a.part_acc + head0 * a.n_split * a.D, 0, 16 * a.n_split * a.D * 4, 0x00020000);
@@ -74,35 +85,35 @@ __device__ __forceinline__ void sum_splits(const SplitParts& a, int64_t head0, i
 #pragma unroll
             for (int y = 0; y < SUMS; ++y) part[(first + y * SHARES) * quads + i] = sum[y];
         } else {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) a.out[(head0 + h) * a.D + c + y] = (sum[0][y] + sum[1 % SUMS][y]) + (sum[2 % SUMS][y] + sum[3 % SUMS][y]);
+            to.sum(h, c, (sum[0] + sum[1 % SUMS]) + (sum[2 % SUMS] + sum[3 % SUMS]));
         }
     }
     if (SHARES > 1) {
         __syncthreads();
         if ((int)threadIdx.x < quads) {
             const f32x4* q = part + threadIdx.x;
-            const f32x4 sum = (q[0] + q[quads]) + (q[2 * quads] + q[3 * quads]);
-            float* out = a.out + (head0 + (int)threadIdx.x / quarter) * a.D + 4 * ((int)threadIdx.x % quarter);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) out[y] = sum[y];
+            to.sum((int)threadIdx.x / quarter, 4 * ((int)threadIdx.x % quarter), (q[0] + q[quads]) + (q[2 * quads] + q[3 * quads]));
         }
     }
 }
-// out and lse of `heads` neighbouring heads (at most 16) from their splits; a workgroup of NT threads, f: [heads][n_split] in LDS.
-template <int NT>
-__device__ __forceinline__ void join_splits(const SplitParts& a, int64_t head0, int heads, int n_split, float shift, float* f, f32x4* part) {
+// Sums and lse of `heads` neighbouring heads (at most 16) from their splits; a workgroup of NT threads, f: [heads][n_split] in LDS.
+template <int NT, typename To>
+__device__ __forceinline__ void join_splits(const SplitParts& a, int64_t head0, const To& to, int heads, int n_split, float shift, float* f, f32x4* part) {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     for (int h = wave; h < heads; h += NT / kWave) {
         const float lg2 = head_log2_sum(a, head0 + h, n_split, shift, f + h * n_split);
-        if (lane_id() == 0 && a.lse) a.lse[head0 + h] = lg2 * 0.69314718055994531f;
+        if (lane_id() == 0) to.lse(h, lg2 * 0.69314718055994531f);
     }
     __syncthreads();
     // Four channels a thread; with few of them two or four threads share a group's splits.
     const int quads = heads * (a.D / 4);
-    if (quads <= NT / 4) sum_splits<NT, 4>(a, head0, quads, n_split, f, part);
-    else if (quads <= NT / 2) sum_splits<NT, 2>(a, head0, quads, n_split, f, part);
-    else sum_splits<NT, 1>(a, head0, quads, n_split, f, part);
+    if (quads <= NT / 4) sum_splits<NT, 4>(a, head0, to, quads, n_split, f, part);
+    else if (quads <= NT / 2) sum_splits<NT, 2>(a, head0, to, quads, n_split, f, part);
+    else sum_splits<NT, 1>(a, head0, to, quads, n_split, f, part);
+}
+template <int NT>
+__device__ __forceinline__ void join_splits(const SplitParts& a, int64_t head0, int heads, int n_split, float shift, float* f, f32x4* part) {
+    join_splits<NT>(a, head0, JoinedHeads{a, head0}, heads, n_split, shift, f, part);
 }
 
 }  // namespace tka

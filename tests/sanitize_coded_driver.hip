@@ -43,6 +43,16 @@ static bool within(const void* p, double bytes, const char* base, size_t room) {
 static size_t prompt_room;                   // bytes for a plain cache's partial sums, from `ws` on
 static int64_t longest_tiles, most_blocks;
 static int any_open;
+static std::vector<int64_t> lens;            // of the layer
+static int64_t walk_sinks;
+static void find_longest(int64_t reach) {
+    most_blocks = any_open = 0;
+    for (int64_t n : lens) {
+        const tka::CodedWalk w(n, walk_sinks, reach);
+        most_blocks = std::max(most_blocks, w.blocks());
+        any_open |= w.open();
+    }
+}
 
 namespace tka {
 static void check_arrays(const CodedArrays& a, int streams) {
@@ -73,10 +83,12 @@ hipError_t launch_coded_decode(const CodedDecodeCall& a, hipStream_t) {
     ++launches;
     check_arrays(a.a, a.B * a.Hkv);
     CHECK(a.chunk >= 1 && a.n_split >= 1 && a.n_split <= kMaxSplits && a.window >= 1);
-    const double heads = (double)a.B * a.Hq * a.n_split;
+    CHECK(a.rows == (a.M ? a.M * a.G : a.G) && a.row_blocks == (a.rows + 15) / 16 && a.reach >= a.window - (a.window > ((int64_t)1 << 40) ? a.window : 0));
+    const double heads = (double)a.B * a.Hkv * a.rows * a.n_split;
     CHECK(within(a.part_acc, heads * a.D * 4, ws, cfg.workspace_bytes) && within(a.part_lm, heads * 8, ws, cfg.workspace_bytes));
-    CHECK((char*)a.part_lm == (char*)a.part_acc + (size_t)a.B * a.Hq * a.n_split * a.D * 4);
+    CHECK((char*)a.part_lm == (char*)a.part_acc + (size_t)a.B * a.Hkv * a.rows * a.n_split * a.D * 4);
     CHECK(within(a.arrive, (double)a.B * a.Hkv * a.row_blocks * 4, ws, (char*)a.part_acc - ws));
+    if (a.M) find_longest(a.reach);
     CHECK((int64_t)(a.n_split - any_open) * a.chunk >= most_blocks && (int64_t)(a.n_split - any_open - 1) * a.chunk < std::max<int64_t>(most_blocks, 1));
     return hipSuccess;
 }
@@ -179,12 +191,8 @@ int main() {
         int64_t least = INT64_MAX;
         for (int64_t n : len) least = std::min(least, n);
         const int64_t sinks = rnd(2) ? 0 : part(2 * cap), window = rnd(2) ? (int64_t)1 << 62 : 1 + part(cap);
-        most_blocks = any_open = 0;
-        for (int64_t n : len) {
-            const tka::CodedWalk w(n, sinks, window);
-            most_blocks = std::max(most_blocks, w.blocks());
-            any_open |= w.open();
-        }
+        lens = len; walk_sinks = sinks;
+        find_longest(window);
         if (there) {
             CHECK(topk_attn_coded_decode(h, 1, rows, sinks, window, fp, fp, nullptr) == TOPK_ATTN_OK);
             const int64_t M = rnd(2) ? 1 + part(std::min<int64_t>(least, 70)) : 1 + part(least);

@@ -445,6 +445,61 @@ def test_prompt_rows_do_not_notice_what_they_do_not_see(dtype, fmt):
         dirty.close()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_rows_do_not_notice_what_they_do_not_see(dtype, fmt):
+    """The last eight tokens' rows (the kernel of single tokens): open rows ahead of some or behind their windows, and a block behind some windows."""
+    d, Hq, n, M = 64, 4, 136, 8
+    g = np.random.default_rng(3)
+    K, V = (draw(g, 1, n, d, dtype=dtype) for _ in range(2))
+    bad = wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    q = up(draw(g, 1, M, Hq, d, dtype=dtype), dtype)
+    clean, _ = filled([n], Hq, 1, d, n, dtype, fmt, rows=[(K, V)])
+    try:
+        for at, value, keys in (((130, 5), 0, False), ((133, 7), 1, False), ((129, 0), 2, False), ((132, 9), 0, True), ((100, 3), 0, False), ((70, 3), 1, True)):
+            Kb, Vb = K.copy(), V.copy()
+            (Kb if keys else Vb)[0, at[0], at[1]] = bad[value]
+            dirty, _ = filled([n], Hq, 1, d, n, dtype, fmt, rows=[(Kb, Vb)])
+            try:
+                for sinks, window in ((0, 3), (0, 4), (0, None), (3, 6), (66, 2)):
+                    a, b = (c.prompt(0, q, window=window, sinks=sinks) for c in (clean, dirty))
+                    see = torch.from_numpy(ref.seen(n, M, sinks, window or n)).to(DEV)
+                    touched = see[:, 64:128].any(1) if at[0] < 128 else see[:, at[0]]
+                    assert torch.equal(a[0][0][~touched], b[0][0][~touched]) and torch.equal(a[1][0][~touched], b[1][0][~touched]), (at, sinks, window)
+                    if not touched.any():
+                        continue
+                    if keys or at[0] < 128:
+                        assert torch.isnan(b[0][0][touched]).all(), (at, sinks, window)
+                    else:
+                        one = b[0][0][touched][..., at[1]].float()
+                        assert (torch.isnan(one) if value == 0 else torch.isinf(one) & ((one > 0) == (value == 1))).all(), (at, sinks, window)
+                        rest = [c for c in range(d) if c != at[1]]
+                        assert torch.equal(a[0][0][..., rest], b[0][0][..., rest]) and torch.equal(a[1], b[1]), (at, sinks, window)
+            finally:
+                dirty.close()
+    finally:
+        clean.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,M", [(wl.F16, 8, 2, 128, 8), (wl.F16, 8, 2, 128, 9), (wl.BF16, 16, 1, 64, 2), (wl.BF16, 16, 1, 64, 3), (wl.F32, 8, 2, 32, 16),
+                                              (wl.F32, 8, 2, 32, 17), (wl.BF16, 4, 2, 256, 64), (wl.BF16, 4, 2, 256, 65), (wl.F32, 3, 1, 256, 42), (wl.F32, 3, 1, 256, 43)])
+def test_rows_at_the_change_of_kernels(dtype, Hq, Hkv, d, M, fmt):
+    """As many rows as go through the kernel of single tokens, and some more; sequences whose lengths end in a block, at its end, and shortly behind it."""
+    lens = [M, 700, 128, 65 + M, 1985]
+    lens = [max(n, M) for n in lens]
+    cache, got = filled(lens, Hq, Hkv, d, max(lens), dtype, fmt, seed=M)
+    try:
+        q = draw(np.random.default_rng(M + 1), len(lens), M, Hq, d, dtype=dtype)
+        for sinks, window in ((0, None), (0, 1), (5, 70), (70, 64), (0, 200)):
+            out, lse = cache.prompt(0, up(q, dtype), window=window, sinks=sinks)
+            for b, n in enumerate(lens):
+                check_rows(out[b].float().cpu().numpy(), lse[b].cpu().numpy(), wl.widen(q[b], dtype).astype(np.float64), got[b][2], got[b][3], sinks, window or n, dtype,
+                           f"sequence {b} ({n} tokens), {sinks} and {window}")
+    finally:
+        cache.close()
+
+
 # ---- together, replayed, side by side --------------------------------------------------------------------------------
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_a_prompt_in_chunks_and_steps_behind_it(fmt):
