@@ -91,7 +91,7 @@ WsLayout ws_layout(const topk_attn_config* c, int batch_layers) {
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes); return at; };
     w.len = take((size_t)c->n_layers * c->n_seqs * sizeof(int32_t));
     // (in front of the per-call arrays: the library's own copy of those has no need of it)
-    w.arrive = take((size_t)c->n_seqs * c->n_kv_heads * ((c->n_q_heads / c->n_kv_heads + 15) / 16) * sizeof(uint32_t));
+    w.arrive = take((size_t)c->n_seqs * c->n_kv_heads * std::max((c->n_q_heads / c->n_kv_heads + 15) / 16, kFewRows / 16) * sizeof(uint32_t));
     w.thr = take(BH * sizeof(float));
     w.bins = take(BH * 2 * sizeof(float));
     w.samp = take(BH * kSampMax * sizeof(float));

@@ -40,7 +40,7 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     if (some) pages = n_blocks;
     // (sequences that are seen whole: as the dense decode)
     if (window && WindowWalk(longest, sinks, window).first > 0) {
-        a.sinks = sinks; a.window = window;
+        a.sinks = sinks; a.window = a.reach = window;
         pages = WindowWalk(longest, sinks, window).pages();
         for (int b = 0; b < c.n_seqs; ++b)               // (a shorter sequence may have more pages: its sinks and its window meet)
             pages = std::max(pages, WindowWalk(h->len[(size_t)layer * c.n_seqs + b], sinks, window).pages());
@@ -48,6 +48,7 @@ int decode_all(topk_attn_t* h, int layer, const void* q, int n_blocks, float* ou
     a.walk = pages * 64;
     a.score_stride = c.max_tokens;               // (of a list: whole pages, one less than the cache has at least)
     a.scores = scratch_at<float>(h, h->ws.scores);
+    a.rows = a.G;
     a.row_blocks = (a.G + 15) / 16;
     // partial sums in the candidate lists' place
     const size_t room = (size_t)h->ws.cand_cap * sizeof(uint64_t) / ((size_t)c.head_dim * sizeof(float) + 2 * sizeof(float));

@@ -104,13 +104,12 @@ struct CodedDecodeCall : SplitParts {
     int join_later;
     int row_blocks;             // blocks of 16 rows
 };
-// Rows of a key stream up to which a prompt's tokens go through the kernel of single tokens, which takes the codes from memory to the products in
+// Rows of a key stream (kFewRows at most) up to which a prompt's tokens go through the kernel of single tokens, which takes the codes from memory to the products in
 // registers, 16 rows at a time; the prompt kernel widens them into LDS once for 128 rows.  The two, in us, of 16 / 32 / 48 / 64 / 96 / 128 rows:
 //   d = 128, bf16, 8 KV heads, 24000 tokens           20.9 / 24.4 / 31.6 / 36.8 / 49.6 / 58.5 and 38.2 / 38.8 / 31.3 / 32.4 / 33.2 / 34.4
 //   d = 64, fp16, 8 sequences of 16000                34.9 / 56.2 / 62.0 / 96.4 / 107 / 128   and 99.0 / 99.5 / 73.7 / 73.8 / 73.4 / 73.2
 //   d = 256, fp16, 4 sequences of 8000                36.2 / 42.3 / 55.9 / 58.7 / 75.5 / 87.9 and 211 / 208 / 98.2 / 99.2 / 111 / 128
 //   d = 128, fp32, 30000                              24.8 / 30.4 / 38.2 / 43.9 / 62.4 / 75.8 and 57.2 / 57.9 / 51.0 / 52.1 / 53.4 / 55.2
-constexpr int kFewRows = 128;   // (the most)
 inline int few_rows(int dtype, int D) { return D == 256 ? kFewRows : dtype == DT_F32 ? 64 : 32; }
 inline int64_t coded_decode_wgs(const CodedDecodeCall& a) {
     const int64_t units = (int64_t)a.B * a.Hkv * a.n_split;

@@ -7,8 +7,6 @@
 // to finish joins them.
 //
 // Bound by the read of the codes: 16 KB per 64 keys and KV head (d = 128) against 48 MFMA and some 500 vector instructions, a sixth of the time the read takes.
-#include <type_traits>
-
 #include "coded.h"
 #include "scan_tiles.h"
 #include "split_join.h"
@@ -26,25 +24,6 @@ __device__ __forceinline__ float top_of_rows(float v) {        // largest of lan
 
 // 2^x for a whole number x (0 for -inf)
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Where 16 rows of a key stream go, from the row0-th on, if they are those of a prompt's tokens.
-template <int DT> struct JoinedRows {
-    const CodedDecodeCall& a;
-    int stream, row0;
-    __device__ __forceinline__ int64_t at(int h) const {
-        const int row = row0 + h, m = row / a.G, b = stream / a.Hkv;
-        return ((int64_t)b * a.M + m) * a.Hq + (stream - b * a.Hkv) * a.G + (row - m * a.G);
-    }
-    __device__ __forceinline__ void one(int h, int c, float v) const {
-        using E = typename std::conditional<DT == DT_F32, float, typename std::conditional<DT == DT_F16, _Float16, __bf16>::type>::type;
-        static_cast<E*>(a.out_rows)[at(h) * a.D + c] = (E)v;
-    }
-    __device__ __forceinline__ void sum(int h, int c, f32x4 v) const {
-#pragma unroll
-        for (int y = 0; y < 4; ++y) one(h, c + y, v[y]);
-    }
-    __device__ __forceinline__ void lse(int h, float v) const { if (a.lse) a.lse[at(h)] = v; }
-};
 
 }  // namespace
 
@@ -80,7 +59,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
     if (split >= ns) return;
     const int heads = a.rows - 16 * rb < 16 ? a.rows - 16 * rb : 16;
     const int64_t head0 = (int64_t)stream * a.rows + 16 * rb;
-    const JoinedRows<DT> to_rows{a, stream, 16 * rb};
+    const JoinedRows<DT, CodedDecodeCall> to_rows{a, stream, 16 * rb};
     const char* const query = static_cast<const char*>(a.q) + (ROWS ? to_rows.at(n < heads ? n : 0) : head0 + (n < heads ? n : 0)) * ROW;
     // what the lane's row sees, and what all rows do
     const int64_t pos = ROWS ? seen.N - a.M + (16 * rb + (n < heads ? n : 0)) / a.G : 0;
@@ -401,7 +380,7 @@ __global__ void __launch_bounds__(256) coded_join_kernel(CodedDecodeCall a) {
     const int open = seen.open() ? 1 : 0;
     int ns = (int)((seen.blocks() + a.chunk - 1) / a.chunk);
     ns = (ns < a.n_split - open ? ns : a.n_split - open) + open;
-    if constexpr (ROWS) join_splits<256>(a, head, JoinedRows<DT>{a, stream, (int)(head - (int64_t)stream * a.rows)}, 1, ns, 0.f, f, sums);
+    if constexpr (ROWS) join_splits<256>(a, head, JoinedRows<DT, CodedDecodeCall>{a, stream, (int)(head - (int64_t)stream * a.rows)}, 1, ns, 0.f, f, sums);
     else join_splits<256>(a, head, 1, ns, 0.f, f, sums);
 }
 

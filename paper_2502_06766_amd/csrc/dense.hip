@@ -62,7 +62,8 @@ __device__ __forceinline__ float max_over_rows(float v) {      // largest of lan
 // 2^-38 of that at most.
 template <int DT> struct WeightShift { static constexpr float value = DT == DT_F16 ? 13.f : 0.f; };
 
-constexpr int kWalkAll = 0, kWalkList = 1, kWalkWindow = 2;        // what is attended: all tokens, a list of pages, the first and the newest ones
+// what is attended: all tokens, a list of pages, the first and the newest ones, or those by the last M tokens
+constexpr int kWalkAll = 0, kWalkList = 1, kWalkWindow = 2, kWalkRows = 3;
 
 constexpr int kFold = 64;        // steps of a wave whose sums follow each other
 
@@ -70,7 +71,7 @@ constexpr int kFold = 64;        // steps of a wave whose sums follow each other
 // sequence has grown, though its contract says otherwise: the last split then takes what there is, and the splits that are waited for are
 // those that come.)
 __device__ __forceinline__ int64_t attend_pages(const AttendCall& a, int64_t N) {
-    if (a.window) return WindowWalk(N, a.sinks, a.window).pages();
+    if (a.reach) return WindowWalk(N, a.sinks, a.reach).pages();
     const int64_t pages = (N + 63) / 64;
     return a.list && a.n_list < pages ? a.n_list : pages;
 }
@@ -80,10 +81,21 @@ __device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t pages)
 }
 // FOLD: for splits of more than kFold steps a wave.  (Shorter ones without the code for it, which takes registers: 32 sequences of 800 to 16384
 // tokens of d = 64 with mass 167 us, 176 with it.)
+// Whether some value of the wave's step (32 bits) is an infinity or a NaN.
+template <int D> __device__ __forceinline__ bool any_odd(const AttendTile<DT_F32, D>& t) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < AttendTile<DT_F32, D>::KEYS; ++e) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) top = max(top, t.v[e][c] & 0x7FFFFFFFu);
+    }
+    return __any(top >= 0x7F800000u);
+}
+
 template <int DT, int D, int WALK, bool MASS, bool FOLD>
 __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) attend_kernel(AttendCall a) {
     using Tile = AttendTile<DT, D>;
-    constexpr bool LIST = WALK == kWalkList;
+    constexpr bool LIST = WALK == kWalkList, ROWS = WALK == kWalkRows, WINDOW = WALK == kWalkWindow || ROWS;
     constexpr int SUB = Tile::SUB, STEP = Tile::STEP, KEYS = Tile::KEYS, KCH = Tile::KCH, T = Tile::T, ROW = Tile::ROW, EV = Tile::EV;
     constexpr int SPP = 64 / STEP;
     constexpr int NW = 4, NT = NW * kWave, RED = NW * 16 * (D + 4), JOIN = 16 * kMaxSplits + 8 * NT;
@@ -110,14 +122,19 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     if (stream < 0) stream += streams;
     const int b = stream / a.Hkv, kvh = stream - b * a.Hkv;
     const int64_t N = a.len[b];
-    const WindowWalk seen(N, a.sinks, WALK == kWalkWindow ? a.window : N);
+    const WindowWalk seen(N, a.sinks, WINDOW ? a.reach : N);
     const int64_t pages = attend_pages(a, N);
     const int ns = attend_splits(a, pages);
     if (split >= ns) return;                                  // (the join knows how many splits a sequence has)
     const int64_t p0 = (int64_t)split * a.chunk, p1 = split + 1 < ns ? p0 + a.chunk : pages;
     const int n_steps = (int)(p1 - p0) * SPP;
-    const int heads = a.G - 16 * rb < 16 ? a.G - 16 * rb : 16;
-    const int64_t head0 = (int64_t)b * a.Hq + (int64_t)kvh * a.G + 16 * rb;
+    const int heads = a.rows - 16 * rb < 16 ? a.rows - 16 * rb : 16;
+    const int64_t head0 = (int64_t)stream * a.rows + 16 * rb;
+    const JoinedRows<DT, AttendCall> to_rows{a, stream, 16 * rb};
+    // what the lane's row sees, and whether all rows see STEP tokens from t0 on
+    const int64_t pos = ROWS ? N - a.M + (16 * rb + (n < heads ? n : 0)) / a.G : 0;
+    const auto sees = [&](int64_t t) { return t <= pos && (t < a.sinks || t > pos - a.window); };
+    const auto all_see = [&](int64_t t0) { return !ROWS || (t0 + STEP <= N - a.M + 1 && (t0 > N - 1 - a.window || t0 + STEP <= a.sinks)); };
     const char* const Kh = a.K + (int64_t)stream * a.Ncap * ROW;
     const char* const Vh = a.V + (int64_t)stream * a.Ncap * ROW;
     const int32_t* const list = LIST ? a.list + (int64_t)stream * a.list_stride + p0 : nullptr;
@@ -125,7 +142,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     // queries: lane (j, head) holds the channels its lane (j, key) holds of a key row
     u32x4 q[KCH];
     {
-        const char* p = static_cast<const char*>(a.q) + (head0 + (n < heads ? n : 0)) * ROW + j * 16;
+        const char* p = static_cast<const char*>(a.q) + (ROWS ? to_rows.at(n < heads ? n : 0) : head0 + (n < heads ? n : 0)) * ROW + j * 16;
 #pragma unroll
         for (int s = 0; s < KCH; ++s) {
             q[s] = *reinterpret_cast<const u32x4*>(p + 64 * s);
@@ -143,7 +160,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     // First row of the wave's step i (steps wave, wave + NW, ... of the split), asked for in order.
     auto row_of = [&](int i) -> int64_t {
         const int s = wave + NW * i;
-        if (WALK == kWalkWindow) return seen.row(p0 + s / SPP) + (s % SPP) * STEP;
+        if (WINDOW) return seen.row(p0 + s / SPP) + (s % SPP) * STEP;
         if (!LIST) return p0 * 64 + (int64_t)s * STEP;
         if ((i & 63) == 0) {
             const int at = wave + NW * (i + lane);
@@ -153,7 +170,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         return (int64_t)page * 64 + (s % SPP) * STEP;
     };
     auto rows_from = [&](int64_t row0, int s) -> int {          // rows of step s that are seen
-        const int64_t left = s < n_steps ? (WALK == kWalkWindow ? seen.end(p0 + s / SPP) : N) - row0 : 0;
+        const int64_t left = s < n_steps ? (WINDOW ? seen.end(p0 + s / SPP) : N) - row0 : 0;
         int r = (int)(left < 0 ? 0 : left > STEP ? STEP : left);
         r = __builtin_amdgcn_readfirstlane(r);
         asm("" : "+s"(r));
@@ -182,7 +199,7 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
 #pragma unroll
     for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;                              // (m: raw score times scale; l: this lane's keys)
-    auto use = [&](const Tile& t, int i, int rows) {
+    auto use = [&](Tile& t, int i, int rows) {
         f32x4 s[SUB];
 #pragma unroll
         for (int g = 0; g < SUB; ++g) {
@@ -221,10 +238,13 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         }
         float p[KEYS];
         float top = -INFINITY;
+        const int64_t t0 = ROWS ? row_of(i) : 0;
+        const bool all = all_see(t0);
 #pragma unroll
         for (int e = 0; e < KEYS; ++e) {
             p[e] = s[e / 4][e % 4];
             if (rows < STEP && 16 * (e / 4) + 4 * j + e % 4 >= rows) p[e] = -INFINITY;
+            if (ROWS && !all && !sees(t0 + 16 * (e / 4) + 4 * j + e % 4)) p[e] = -INFINITY;
             top = fmaxf(top, p[e]);
         }
         const float m_new = fmaxf(m, max_over_rows(top) * a.scale_log2e);
@@ -240,6 +260,34 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         for (int c = 0; c < T; ++c) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[c][r] *= alpha;
+        }
+        if constexpr (ROWS) {
+            if (!all && any_odd(t)) {
+                // Some rows do not see a value that is no number: it goes to those that see it, one token at a time, and the products take zero in its place.
+                for (int key = 0; key < rows; ++key) {
+                    float w = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (x == (key & 3)) w = p[x];
+                    w = __shfl(w, 16 * (key >> 2) + n, 64);
+                    const bool sees_it = sees(t0 + key);
+                    const float* const row = reinterpret_cast<const float*>(Vh + (t0 + key) * ROW);
+#pragma unroll
+                    for (int c = 0; c < T; ++c) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float v = row[Tile::channel(c, 4 * j + r)];
+                            if (sees_it && !(fabsf(v) < INFINITY)) acc[c][r] = fmaf(w, v, acc[c][r]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < KEYS; ++e) {
+#pragma unroll
+                    for (int c = 0; c < T; ++c)
+                        if (!(fabsf(__uint_as_float(t.v[e][c])) < INFINITY)) t.v[e][c] = 0;
+                }
+            }
         }
         if constexpr (DT == DT_F32) {
 #pragma unroll
@@ -352,8 +400,14 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
         }
         const int64_t bh = head0 + h;
         if (whole) {
-            a.out[bh * D + c] = sum * (1.0f / total);              // (as join_splits() has it)
-            if (c == 0 && a.lse) a.lse[bh] = ((top - WeightShift<DT>::value) + log2f(total)) * 0.69314718055994531f;
+            const float o = sum * (1.0f / total), lse = ((top - WeightShift<DT>::value) + log2f(total)) * 0.69314718055994531f;     // (as join_splits() has it)
+            if (ROWS) {
+                to_rows.one(h, c, o);
+                if (c == 0) to_rows.lse(h, lse);
+            } else {
+                a.out[bh * D + c] = o;
+                if (c == 0 && a.lse) a.lse[bh] = lse;
+            }
         } else {
             put(&a.part_acc[(bh * a.n_split + split) * D + c], sum);
         }
@@ -371,7 +425,19 @@ __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) 
     __syncthreads();
     if (arrived + 1u != (uint32_t)ns) return;
     if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    join_splits<NT>(a, head0, heads, ns, WeightShift<DT>::value, lds, reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits));
+    f32x4* const room = reinterpret_cast<f32x4*>(lds + 16 * kMaxSplits);
+    if constexpr (ROWS) join_splits<NT>(a, head0, to_rows, heads, ns, WeightShift<DT>::value, lds, room);
+    else join_splits<NT>(a, head0, heads, ns, WeightShift<DT>::value, lds, room);
+}
+
+// Many splits of the last tokens' rows (of 32 bits): a workgroup per row.
+__global__ void __launch_bounds__(256) attend_rows_join_kernel(AttendCall a) {
+    __shared__ float f[kMaxSplits];
+    __shared__ f32x4 sums[512];
+    const int64_t row = blockIdx.x;
+    const int stream = (int)(row / a.rows);
+    join_splits<256>(a, row, JoinedRows<DT_F32, AttendCall>{a, stream, (int)(row - (int64_t)stream * a.rows)}, 1,
+                     attend_splits(a, attend_pages(a, a.len[stream / a.Hkv])), 0.f, f, sums);
 }
 
 // The first workgroups put a head's, or a block of heads', splits together; the others add each key's weights, the heads of the group in order, from the
@@ -441,7 +507,10 @@ hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
     } while (0)
 #define TKA_ATTEND(DT_, D_)                                                                                             \
     do {                                                                                                                \
-        if (a.list && a.mass) TKA_ATTEND_(DT_, D_, kWalkList, true);                                                    \
+        if (a.M) {                                                                                                      \
+            if constexpr (DT_ == DT_F32) TKA_ATTEND_(DT_, D_, kWalkRows, false);                                        \
+            else return hipErrorInvalidValue;                                                                           \
+        } else if (a.list && a.mass) TKA_ATTEND_(DT_, D_, kWalkList, true);                                                    \
         else if (a.list) TKA_ATTEND_(DT_, D_, kWalkList, false);                                                        \
         else if (a.mass) TKA_ATTEND_(DT_, D_, kWalkAll, true);                                                          \
         else if (a.window) TKA_ATTEND_(DT_, D_, kWalkWindow, false);                                                    \
@@ -452,6 +521,10 @@ hipError_t launch_attend(const AttendCall& a, hipStream_t st) {
 #undef TKA_ATTEND_
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || n_join + n_mass == 0) return e;
+    if (a.M) {
+        hipLaunchKernelGGL(attend_rows_join_kernel, dim3((unsigned)n_join), wg, 0, st, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(attend_later_kernel, dim3((unsigned)(n_join + n_mass)), dim3(256), 0, st, a, a.dtype == DT_F16 ? 13.f : 0.f, (int)n_join);
     return hipGetLastError();
 }

@@ -48,7 +48,8 @@ struct SplitParts {
     int D;
 };
 
-// Attention of one query per sequence and head over all cached tokens, the newest and the first ones, or a list of pages of 64 tokens.
+// Attention of one query per sequence and head over all cached tokens, the newest and the first ones, or a list of pages of 64 tokens; or of the last
+// M tokens' queries (few of them, 32 bits), each over what it sees: then a row is a query and a head of the group, m G + g, as in prompt.h.
 struct AttendCall : SplitParts {
     const char* K;              // this layer's keys and values [B][Hkv][Ncap][D]
     const char* V;
@@ -64,11 +65,15 @@ struct AttendCall : SplitParts {
     int64_t Ncap;
     int64_t walk;               // most keys a sequence's walk covers, whole pages
     int64_t sinks, window;      // window > 0: the first `sinks` and the newest `window` tokens alone
+    int64_t reach;              // tokens some query's window has: window + M - 1
+    void* out_rows;             // M > 0: [B][M][Hq][D] in the type of q (lse [B][M][Hq])
+    int M;                      // 0: one query per sequence
+    int rows;                   // of a key stream: G, or M G
     int B, Hq, Hkv, G, dtype;
     int chunk;                  // pages per split
     int join_later;             // the splits are put together in a launch of its own,
     int join_heads;             // by a workgroup per head (1) or per block of heads (16)
-    int row_blocks;             // blocks of 16 heads of a group
+    int row_blocks;             // blocks of 16 rows
     float scale_log2e;          // log2(e) / sqrt(D)
 };
 constexpr int kMassPerBlock = 1024;      // keys whose weights one workgroup adds up
@@ -78,12 +83,13 @@ inline int64_t attend_walk_wgs(const AttendCall& a) {
     return a.row_blocks > 1 ? (units + 7) / 8 * 8 * a.row_blocks : units;
 }
 inline int64_t attend_join_wgs(const AttendCall& a) {
-    return a.join_later && a.n_split > 1 ? (int64_t)a.B * a.Hkv * (a.join_heads == 1 ? a.G : a.row_blocks) : 0;
+    return a.join_later && a.n_split > 1 ? (int64_t)a.B * a.Hkv * (a.join_heads == 1 ? a.rows : a.row_blocks) : 0;
 }
 inline int64_t attend_mass_wgs(const AttendCall& a) {
     return a.mass ? (int64_t)a.B * a.Hkv * ((a.walk + kMassPerBlock - 1) / kMassPerBlock) : 0;
 }
 hipError_t launch_attend(const AttendCall& a, hipStream_t st);
+constexpr int kFewRows = 128;            // rows of a key stream that the kernels of single tokens take at most
 
 // Pages of the block-sparse decode.
 struct BlockCall {

@@ -37,7 +37,7 @@ struct PromptCall {
     int n_split, chunk;         // most splits of a row block's keys, tiles of 64 keys in each
     int row_blocks, block_rows;
 };
-constexpr int kPromptSplits = 64;
+constexpr int kPromptSplits = 64;      // (of 256 their joint takes 1.3 us more)
 // Tiles of 64 keys that the rows of the last block, which see most, see of a sequence of N tokens.
 inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int64_t window) {
     const int64_t oldest = N - last_queries - window, from = oldest < 0 ? 0 : oldest / 64, front = ((sinks < N ? sinks : N) + 63) / 64;
@@ -46,10 +46,11 @@ inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int6
 // Rows of a block, and the splits of its keys: runs of `chunk` tiles, as many as there are compute units, twice that where the matrix unit has
 // most of the time (512 queries at 32768 tokens: 340 and 291 us).  (room: bytes there are for partial sums.  Eight queries of four
 // sequences of 1k to 20k tokens in runs of 6 / 10 / 14 / 20 / 28 / 40 tiles, one of 20 to a compute unit: 65 / 54 / 57 / 45 / 52 / 62 us; in as many runs for every
-// sequence, the longest's of 20: 48.  64 queries of one sequence of 20000, 20 tiles to a compute unit: 55 / 47 / 47 / 41 / 48 / 61.)
+// sequence, the longest's of 20: 48.  64 queries of one sequence of 20000, 20 tiles to a compute unit: 55 / 47 / 47 / 41 / 48 / 61.  A wave of few rows has
+// a tile on its way, 32 KB at d = 128: of fewer channels as many more waves, d = 64, 8 sequences of 16000 tokens 62 and 48.)
 inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu) {
     const int64_t rows = a->M * a->G, streams = (int64_t)a->S * a->Hkv;
-    a->block_rows = rows <= 32 && a->format < 0 ? 32 : 128;          // (few rows of the 8-bit cache: coded_decode.hip)
+    a->block_rows = rows <= 32 && a->format < 0 && a->dtype != DT_F32 ? 32 : 128;          // (few rows of 32 bits or the 8-bit cache: dense.hip, coded_decode.hip)
     a->row_blocks = (int)((rows + a->block_rows - 1) / a->block_rows);
     int64_t longest = 1, all = 0;
     for (int b = 0; b < a->S; ++b) {
@@ -57,7 +58,7 @@ inline void plan_prompt(PromptCall* a, const int64_t* len, size_t room, int n_cu
         longest = n > longest ? n : longest;
         all += n;
     }
-    const int64_t wgs = streams * a->row_blocks, want = rows >= 512 ? 2 * n_cu : n_cu;
+    const int64_t wgs = streams * a->row_blocks, want = (rows >= 512 ? 2 : rows <= 32 && a->D < 128 ? 128 / a->D : 1) * n_cu;
     int64_t most = (int64_t)(room / ((size_t)wgs * a->block_rows * (a->D + 2) * sizeof(float)));     // splits
     if (most > kPromptSplits) most = kPromptSplits;
     int64_t chunk = wgs >= n_cu || most < 2 ? longest : (all * a->Hkv * a->row_blocks + want - 1) / want;
@@ -70,6 +71,13 @@ inline void place_prompt_parts(PromptCall* a, void* room) {
     a->part_acc = static_cast<float*>(room);
     a->part_lm = a->part_acc + (size_t)a->S * a->Hkv * a->row_blocks * a->n_split * a->block_rows * a->D;
 }
+// Rows of a key stream up to which tokens of a 32-bit cache go through the walk of single tokens (dense.hip), whose products take 16 rows and whose tiles
+// lie in registers; this kernel's take 32, and 64 KB to 256 KB of LDS leave a wave or four to a compute unit.  The two, in us, of 8 / 16 / 32 / 48 / 64 rows:
+//   d = 128, 8 KV heads, 30000 tokens           44 / 46 / 54 / 77 / 95       and 140 / 141 / 141 / 203 / 203
+//   d = 64, 8 KV heads, 4 sequences of 8000     27 / 29 / 42 / 48 / 72       and 82 / 82 / 82 / 82 / 82
+//   d = 256, the same                           100 / 104 / 152 / 235 / 270  and 342 / 342 / 344 / 472 / 473
+// 16 bits stay here (d = 128, 24000 tokens, 16 / 32 / 64 rows 25 / 26 / 40 and 25 / 26 / 29; 4 sequences of 1000 to 20000 46 / 50 / 75 and 41 / 41 / 52).
+constexpr int kFewRowsF32 = 64;
 constexpr int64_t kMostPromptRows = 1 << 30;      // of a stream: counted in 32 bits
 hipError_t launch_prompt(const PromptCall& a, hipStream_t st);
 hipError_t launch_prompt_coded(const PromptCall& a, hipStream_t st);

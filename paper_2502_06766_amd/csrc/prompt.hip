@@ -81,8 +81,13 @@ hipError_t launch_prompt(const PromptCall& a, hipStream_t st) {
     const dim3 grid((unsigned)((int64_t)a.S * a.Hkv * a.n_split * a.row_blocks));
 #define TKA_PROMPT(DT_, D_)                                                                                               \
     do {                                                                                                                  \
-        if (a.block_rows == 32) hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, 1>), grid, dim3(64), 0, st, a);              \
-        else hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, 4>), grid, dim3(256), 0, st, a);                               \
+        if constexpr (DT_ != DT_F32) {                                                                                    \
+            if (a.block_rows == 32) {                                                                                     \
+                hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, 1>), grid, dim3(64), 0, st, a);                            \
+                break;                                                                                                    \
+            }                                                                                                             \
+        }                                                                                                                 \
+        hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, 4>), grid, dim3(256), 0, st, a);                               \
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_PROMPT, a.dtype, a.D);
 #undef TKA_PROMPT

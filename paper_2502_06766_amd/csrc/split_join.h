@@ -1,5 +1,7 @@
 // Partial sums of the splits of a head's keys, put together: out = sum_i f_i acc_i / sum_i f_i l_i with f_i = 2^(m_i - max m).
 #pragma once
+#include <type_traits>
+
 #include "device_utils.h"
 #include "internal.h"
 #include "ops.h"
@@ -52,6 +54,25 @@ struct JoinedHeads {
     }
     __device__ __forceinline__ void lse(int h, float v) const { if (a.lse) a.lse[head0 + h] = v; }
 };
+// Where rows of a key stream go, from the row0-th on, if they are those of a prompt's tokens: row m G + g is head g of the group of token m.
+template <int DT, typename Call> struct JoinedRows {
+    const Call& a;
+    int stream, row0;
+    __device__ __forceinline__ int64_t at(int h) const {
+        const int row = row0 + h, m = row / a.G, b = stream / a.Hkv;
+        return ((int64_t)b * a.M + m) * a.Hq + (stream - b * a.Hkv) * a.G + (row - m * a.G);
+    }
+    __device__ __forceinline__ void one(int h, int c, float v) const {
+        using E = typename std::conditional<DT == DT_F32, float, typename std::conditional<DT == DT_F16, _Float16, __bf16>::type>::type;
+        static_cast<E*>(a.out_rows)[at(h) * a.D + c] = (E)v;
+    }
+    __device__ __forceinline__ void sum(int h, int c, f32x4 v) const {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) one(h, c + y, v[y]);
+    }
+    __device__ __forceinline__ void lse(int h, float v) const { if (a.lse) a.lse[at(h)] = v; }
+};
+
 // Weighted sum of the splits of `quads` groups of four channels.  Four sums, by split modulo four, whichever thread takes them: the result does
 // not depend on how many heads are joined at a time.
 template <int NT, int SHARES, typename To>

@@ -104,6 +104,17 @@ static void check_prompt(const PromptCall& a, size_t room) {
         CHECK(within(a.part_acc, slots * a.D * 4, ws, room) && within(a.part_lm, slots * 8, ws, room));
     }
 }
+hipError_t launch_attend(const AttendCall& a, hipStream_t) {
+    ++launches;
+    CHECK(a.M >= 1 && a.rows == a.M * a.G && a.rows <= kFewRowsF32 && a.dtype == TOPK_ATTN_F32 && a.row_blocks == (a.rows + 15) / 16 && a.chunk >= 1 && a.n_split >= 1 && a.n_split <= kMaxSplits);
+    int64_t pages = 0;
+    for (int64_t n : lens) pages = std::max(pages, tka::WindowWalk(n, walk_sinks, a.reach).pages());
+    CHECK((int64_t)a.n_split * a.chunk >= pages && (int64_t)(a.n_split - 1) * a.chunk < pages);
+    const double heads = (double)a.B * a.Hkv * a.rows * a.n_split;
+    CHECK(within(a.part_acc, heads * a.D * 4, ws, prompt_room) && within(a.part_lm, heads * 8, ws, prompt_room));
+    CHECK((char*)a.part_lm == (char*)a.part_acc + (size_t)a.B * a.Hkv * a.rows * a.n_split * a.D * 4);
+    return hipSuccess;
+}
 hipError_t launch_prompt(const PromptCall& a, hipStream_t) { check_prompt(a, prompt_room); return hipSuccess; }
 hipError_t launch_prompt_coded(const PromptCall& a, hipStream_t) { check_prompt(a, cfg.workspace_bytes); return hipSuccess; }
 }  // namespace tka

@@ -343,3 +343,50 @@ def test_keys_of_minus_infinity_have_no_weight(dtype, coded, d):
         tol = tol + (0 if token else HALF[dtype]) * np.abs(w_out[:, keep])
         assert np.isfinite(w_out[:, keep]).all() and (np.abs(o - w_out)[:, keep] <= tol).all()
         assert (np.abs(l - w_lse)[:, keep] <= weight_error(wide(q, dtype)[0], K0, d) + (n / 16 + 64) * U + 8 * U * (1 + np.abs(w_lse[:, keep]))).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+def test_few_rows_do_not_notice_what_they_do_not_see(dtype, d):
+    """The last eight tokens' rows: values and keys that are no numbers ahead of some of them or behind their windows."""
+    Hq, n, M = 4, 139, 8
+    g = np.random.default_rng(3)
+    K, V = (draw(g, 1, n, d, dtype=dtype) for _ in range(2))
+    bad = wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    q = up(draw(g, 1, M, Hq, d, dtype=dtype), dtype)
+    clean, _ = filled([n], Hq, 1, d, 200, dtype, rows=[(K, V)])
+    for at, value, keys in (((130, 5), 0, False), ((136, 7), 1, False), ((133, 0), 2, False), ((135, 9), 0, True), ((127, 3), 0, False), ((66, 31), 1, False)):
+        Kb, Vb = K.copy(), V.copy()
+        (Kb if keys else Vb)[0, at[0], at[1]] = bad[value]
+        dirty, _ = filled([n], Hq, 1, d, 200, dtype, rows=[(Kb, Vb)])
+        for sinks, window in ((0, 3), (0, 8), (0, 70), (0, None), (3, 6), (67, 2), (128, 5)):
+            a, b = (c.prompt(0, q, window=window, sinks=sinks) for c in (clean, dirty))
+            touched = torch.from_numpy(ref.seen(n, M, sinks, window or n)).to(DEV)[:, at[0]]
+            assert torch.equal(a[0][0][~touched], b[0][0][~touched]) and torch.equal(a[1][0][~touched], b[1][0][~touched]), (at, sinks, window)
+            if not touched.any():
+                continue
+            if keys:
+                assert torch.isnan(b[0][0][touched]).all(), (at, sinks, window)
+            else:
+                one = b[0][0][touched][..., at[1]].float()
+                # (an infinity that all rows of a tile see may come out as NaN)
+                assert not torch.isfinite(one).any() and (value == 1 or not (one == float("inf")).any()), (at, sinks, window)
+                rest = [c for c in range(d) if c != at[1]]
+                assert torch.equal(a[0][0][..., rest], b[0][0][..., rest]) and torch.equal(a[1], b[1]), (at, sinks, window)
+        dirty.close()
+    clean.close()
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,M", [(wl.F32, 8, 2, 128, 16), (wl.F32, 8, 2, 128, 17), (wl.F32, 3, 1, 64, 21), (wl.F32, 3, 1, 64, 22), (wl.F32, 2, 2, 256, 64),
+                                              (wl.F32, 2, 2, 256, 65), (wl.F32, 16, 1, 32, 4), (wl.F16, 8, 2, 128, 8), (wl.F16, 8, 2, 128, 9), (wl.BF16, 20, 1, 64, 1)])
+def test_rows_at_the_change_of_kernels(dtype, Hq, Hkv, d, M):
+    """As many rows as one kernel takes, and some more; sequences that end in a tile, at its end, and shortly behind it."""
+    lens = [max(n, M) for n in (M, 700, 128, 65 + M, 1985)]
+    cache, got = filled(lens, Hq, Hkv, d, max(lens), dtype, seed=M)
+    q = draw(np.random.default_rng(M + 1), len(lens), M, Hq, d, dtype=dtype)
+    for sinks, window in ((0, None), (0, 1), (5, 70), (70, 64), (0, 200)):
+        out, lse = cache.prompt(0, up(q, dtype), window=window, sinks=sinks)
+        for b, n in enumerate(lens):
+            check(out[b].double().cpu().numpy(), lse[b].double().cpu().numpy(), wide(q[b], dtype), *got[b], sinks, window or n, dtype, False,
+                  f"sequence {b} ({n} tokens), {sinks} and {window}")
+    cache.close()
