@@ -5,7 +5,8 @@
 //   e4m3   scale = the smallest power of two with amax <= 448 scale: x / scale is exact, and rounding it to e4m3 the only rounding.
 // Blocks whose amax is below 2^-100 are zeros; a block with a NaN or an infinity has a scale of NaN, and all of it reads as NaN.
 //
-// Bound by the rows read and the codes written, 3 bytes an element of 16 bits; reading back 3 as well.
+// Bound by the rows read and the codes written, 3 bytes an element of 16 bits; reading back 3 as well.  8 KV heads of d = 128: 8191 tokens into the cache
+// 17 us, back 13.9 (3.6 TB/s); 48000 tokens 72.6 and 60.4 (4.1 and 4.9 TB/s; a copy reaches 4.9); one token of 16 sequences 2.8, of a step's 7.9 with the call.
 #include "coded.h"
 
 namespace tka {
