@@ -276,7 +276,7 @@ int topk_attn_decode_sinks(topk_attn_t* h, int layer, const void* q, int64_t sin
  *   q    device [S, n_queries, Hq, d] in the cache dtype, 16-byte aligned (S: sequences of the call)
  *   out  device [S, n_queries, Hq, d] in the cache dtype, 16-byte aligned;  lse  device [S, n_queries, Hq] fp32 or NULL
  * seq: one sequence of the layer, or -1: all B of them (their lengths may differ).  Softmax statistics and sums are held in 32 bits; the weights of
- * 16-bit caches are rounded to the cache dtype once, as the output is.  What a token does not see (NaN and infinities too) has no effect on its output.
+ * 16-bit caches are rounded to the cache dtype once, as the output is (fp16: below 2^-27 of the row's largest in steps of 2^-37 of it).  What a token does not see (NaN and infinities too) has no effect on its output.
  * n_queries == 0 is a no-op.  Replays as topk_attn_decode_dense.
  * Errors: EINVAL (null h/q/out, range, misaligned, n_queries < 0 or beyond a sequence's length, sinks < 0, window < 1), EUNSUPPORTED (2^24 or more
  * workgroups: 128 rows of queries times heads of a group each; 2^31 or more rows of a KV head). */

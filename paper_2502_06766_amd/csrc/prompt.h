@@ -8,8 +8,8 @@
 // times channels x rows, then channels x keys times keys x rows): a lane holds scores and weighted sums of one row, lane % 32, the running maximum is
 // a number per lane, and the scores come out of the first product in the order in which the second one takes the weights:
 //   score register i of a 32-key tile is key 8 (i / 4) + 4 (lane / 32) + i % 4; step x of 16 keys takes registers 8 x .. 8 x + 7.
-// Weights are rounded once to the type of the values (16 bits: what the second product takes; half a step of 2^-8 or 2^-11, as large as that of the output);
-// their sum is of the unrounded ones.
+// Weights are rounded once to the type of the values (16 bits: what the second product takes; half a step of 2^-8 or 2^-11, as large as that of the output;
+// what of fp16's range they use: WeightRange); their sum is of the unrounded ones.
 //
 // Bound by the matrix unit, and behind it by the vector instructions of the weights, which only the other wave of a SIMD's products cover.  8 KV heads, 32 heads, d = 128:
 // a prompt of 8192 tokens, bf16, 532 us (1.03 PFLOP/s; a library product of 8192^3 has 1.23, MFMA alone on random numbers 1.5 to 1.8); 16384 tokens in a
@@ -164,6 +164,13 @@ template <int CT> __device__ __forceinline__ bool has_no_number(uint32_t w) {
 // The maximum that the weights are relative to follows the scores' only when those are more than 2^kSlack above: the weighted sums are scaled seldom
 // (scores of a normal distribution, 8192 tokens, 32 rows: after the first tile at none of the others, with no slack at 32 of 127), and a weight stays below 2^kSlack.
 constexpr float kSlack = 8.f, kSumSlack = 5.f, kSumShift = 10.f;       // (of weights times a value scale: below 2^15 in fp16)
+// fp16 has whole steps of its bits down to 2^-14 and nothing below 2^-25, and weights of that size may be many: one key 17 nats above 65536 others is 400 of
+// them, and without a shift nothing of those was left.  Weights are held times 2^13 with 2 powers of slack, below 2^15: all of the type's bits down to 2^-27 of the
+// largest and steps of 2^-37 below, as in the single token's decode.  (8 powers of slack and a shift of 7 would leave steps of 2^-31, 2^-6 of a weight 18 nats below.  They scale the
+// sums at none of 127 tiles of normal scores, 2 at ten of them: 8192 tokens, 32 heads over 8, d = 128, 590 us against 582.)
+template <int CT, bool VSCALE> struct WeightRange {
+    static constexpr float slack = CT == DT_F16 && !VSCALE ? 2.f : kSlack, shift = CT == DT_F16 && !VSCALE ? 13.f : 0.f;
+};
 
 // Whether some of a lane's words has an infinity or a NaN: the largest magnitudes, two halves at a time.
 template <int CT, int N>
@@ -252,8 +259,9 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     top = other_half_max(top);
     const bool none = top == -INFINITY;                              // (also of nothing but NaN: the weights are NaN then)
     const float bm = none ? -INFINITY : ceilf(top * f);
-    const float m_new = bm > st.m + kSlack || st.m == -INFINITY ? bm : st.m, ref = m_new == -INFINITY ? 0.f : m_new;
-    float turn = __builtin_amdgcn_exp2f(st.m - ref), e_new = 0.f;
+    using Range = WeightRange<CT, VSCALE>;
+    const float m_new = bm > st.m + Range::slack || st.m == -INFINITY ? bm : st.m, whole = m_new == -INFINITY ? 0.f : m_new, ref = whole - Range::shift;
+    float turn = __builtin_amdgcn_exp2f(st.m - whole), e_new = 0.f;
     int ke = 0;
     st.l *= turn;
     if (VSCALE) {                                                    // (the weighted sum goes by its own)
@@ -680,7 +688,7 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
         }
     }
     // ---- what the rows leave ----
-    float l = st.l, m = st.m;
+    float l = st.l, m = st.m - WeightRange<CT, CODED>::shift;
     {
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(x[0]) + __uint_as_float(x[1]);

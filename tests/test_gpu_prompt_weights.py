@@ -1,0 +1,77 @@
+"""Attention of a prompt's tokens where many small weights make up the result, on the GPU through the binding, against closed forms in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_06766_amd import topk_attn as ta
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda", 0) if torch.cuda.is_available() else None
+U = 2.0 ** -24                                                   # half a step of fp32 relative to the value
+HALF = {ta.F32: 2.0 ** -24, ta.F16: 2.0 ** -11, ta.BF16: 2.0 ** -8}
+TORCH = {ta.F32: torch.float32, ta.F16: torch.float16, ta.BF16: torch.bfloat16}
+
+
+def cache_of(K, V, Hq, dtype, fmt):
+    """A cache of one sequence that holds K, V [Hkv, n, d]; fmt None: in its own type."""
+    Hkv, n, d = K.shape
+    K, V = (x.to(TORCH[dtype]) for x in (K, V))
+    if fmt is None:
+        cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, n, 64, dtype)
+        cache.append(0, 0, K, V, head_major=True)
+    else:
+        cache = ta.TopkAttnCodedCache(1, 1, Hq, Hkv, d, n, dtype, format=fmt)
+        cache.append(0, K.transpose(0, 1)[None], V.transpose(0, 1)[None])
+    return cache
+
+
+def decode(cache, fmt, q):
+    return cache.decode_dense(0, q) if fmt is None else cache.decode(0, q)
+
+
+# ---- one key far above many others ---------------------------------------------------------------------------------------
+def check_small_weights(dtype, fmt, n, nats):
+    """A first token that scores `nats` above all others and whose value is zero: the output is made of the others' weights alone.  Rows that are walked whole, and
+    few rows whose keys are split.
+
+    The first token's key is 16 in one channel, a number that e4m3 holds as it is and int8 as 127 times the block's scale."""
+    d, G = 64, 4
+    K, V = torch.zeros((1, n, d), device=DEV), torch.ones((1, n, d), device=DEV)
+    K[0, 0, 0], V[0, 0] = 16.0, 0.0
+    cache = cache_of(K, V, G, dtype, fmt)
+    try:
+        top = 16.0
+        if fmt == ta.CODED_INT8:
+            m, e = math.frexp(float(np.float32(16) / np.float32(127)))
+            top = 127 * math.ldexp(float(np.rint(m * 65536)) / 65536, e)
+        top *= nats / 16
+        for M in (8192, 2):
+            q = torch.zeros((1, M, G, d), device=DEV, dtype=TORCH[dtype])
+            q[..., 0] = nats / 2                                 # times 16 over sqrt(64)
+            out, lse = cache.prompt(0, q)
+            one, _ = decode(cache, fmt, q[:, -1].contiguous())
+            p = torch.arange(n - M, n, device=DEV, dtype=torch.float64)
+            total = math.exp(top) + p
+            want = (p / total)[:, None, None]
+            # the exponent is a product with a factor of 32 bits and a difference (3 u of it and of its integer reference, which is 13 more in fp16), the exponential
+            # 4 u; a weight's rounding and the output's; sums one after the other, 16 keys at a time
+            exponent = 3 * U * (top * 1.4427 + 14) + 4 * U
+            tol = (2 * HALF[dtype] + 2 * exponent + (n / 16 + 64) * U) * want
+            off = (out[0].double() - want).abs()
+            assert bool((off <= tol).all()), f"{M} rows: off by {(off / want).max():.3g} of the output, {(tol / want).max():.3g} allowed"
+            off = (lse[0].double() - torch.log(total)[:, None]).abs().max().item()
+            assert off <= exponent + (n / 16 + 64) * U + 4 * U * math.log(total.max()), f"{M} rows: lse off by {off:.3g}"
+        # the single token's decode holds weights in two parts, with steps of 2^-37 of the largest where they are small: half of one is 2^-10.9 of a weight 18.75 nats below
+        off = (one[0].double() - want[-1]).abs().max().item() / want[-1].item()
+        assert off <= 2.0 ** -10.9 + 2 * exponent + (n / 16 + 64) * U
+    finally:
+        cache.close()
+
+
+@pytest.mark.parametrize("nats", [14, 16, 17, 18, 18.75])
+@pytest.mark.parametrize("n", [65537, 131073])
+@pytest.mark.parametrize("dtype", [ta.F16, ta.BF16])
+def test_small_weights_add_up(dtype, n, nats):
+    check_small_weights(dtype, None, n, nats)
