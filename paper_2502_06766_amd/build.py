@@ -21,8 +21,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 # Accumulators of the prompt kernels' matrix instructions in vector registers: the vector unit scales them now and then, and from the accumulation registers
-# each of them would be moved over and back (prompt of 4096 tokens, head dimension 256: 183 us against 258).
-SOURCE_FLAGS = {"prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# each of them would be moved over and back, for which head dimension 256 has no registers left.  d = 256, 16 heads over 4, with and without: a prompt of 4096 tokens,
+# bf16, 183 and 258 us; 2048 tokens at the end of 24000 of the 8-bit cache, bf16, int8 951 and 1705, e4m3 943 and 1441, fp32 2010 and 5150 (d = 128, fp32, 855 and 927).
+SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("prompt.hip", "coded_prompt.hip")}
 
 
 def source_hash() -> str:
