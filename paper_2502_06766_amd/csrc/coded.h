@@ -105,12 +105,18 @@ struct CodedDecodeCall : SplitParts {
     int row_blocks;             // blocks of 16 rows
 };
 // Rows of a key stream (kFewRows at most) up to which a prompt's tokens go through the kernel of single tokens, which takes the codes from memory to the products in
-// registers, 16 rows at a time; the prompt kernel widens them into LDS once for 128 rows.  The two, in us, of 16 / 32 / 48 / 64 / 96 / 128 rows:
-//   d = 128, bf16, 8 KV heads, 24000 tokens           20.9 / 24.4 / 31.6 / 36.8 / 49.6 / 58.5 and 38.2 / 38.8 / 31.3 / 32.4 / 33.2 / 34.4
-//   d = 64, fp16, 8 sequences of 16000                34.9 / 56.2 / 62.0 / 96.4 / 107 / 128   and 99.0 / 99.5 / 73.7 / 73.8 / 73.4 / 73.2
-//   d = 256, fp16, 4 sequences of 8000                36.2 / 42.3 / 55.9 / 58.7 / 75.5 / 87.9 and 211 / 208 / 98.2 / 99.2 / 111 / 128
-//   d = 128, fp32, 30000                              24.8 / 30.4 / 38.2 / 43.9 / 62.4 / 75.8 and 57.2 / 57.9 / 51.0 / 52.1 / 53.4 / 55.2
-inline int few_rows(int dtype, int D) { return D == 256 ? kFewRows : dtype == DT_F32 ? 64 : 32; }
+// registers, 16 rows at a time; the prompt kernel widens them into LDS once for 128 rows.  The two, in us, of 16 / 32 / 48 / 64 / 96 / 128 rows (8 KV heads, groups of 4):
+//   d = 256, fp16, 4 sequences of 8000                41.1 / 49.5 / 64.4 / 72.8 / 88.0 / 112  and 59.8 / 60.6 / 63.2 / 64.0 / 66.5 / 69.3
+//   d = 256, fp16, 16 sequences of 8000               113 / 124 / 165 / 187 / 260 / 325       and 192 / 193 / 199 / 200 / 205 / 215
+//   d = 256, fp16, 4 sequences of up to 32000         82.2 / 97.6 / 135 / 141 / 182 / 217     and 188 / 190 / 195 / 196 / 201 / 206
+//   d = 256, bf16, e4m3, 24000 tokens                 32.0 / 36.3 / 45.4 / 50.5 / 68.4 / 82.9 and 44.7 / 45.5 / 46.8 / 48.0 / 50.6 / 53.3
+//   d = 256, fp32, 4 sequences of 8000                42.8 / 54.5 / 92.8 / 80.5 / 133 / 126   and 118 / 119 / 127 / 128 / 136 / 143
+//   d = 128, bf16, 24000 tokens                       21.4 / 24.8 / 32.3 / 37.7 / 50.1 / 59.0 and 29.8 / 30.3 / 31.3 / 31.9 / 33.6 / 34.8
+//   d = 128, fp32, 30000                              24.6 / 30.2 / 39.2 / 44.4 / 63.1 / 76.4 and 45.4 / 46.1 / 47.8 / 48.4 / 50.3 / 52.7
+//   d = 64, fp32, 4 sequences of 16000                23.7 / 35.0 / 38.8 / 57.5 / 64.4 / 97.8 and 38.2 / 38.8 / 60.4 / 60.9 / 61.6 / 62.6
+//   d = 64, fp16, 8 sequences of 16000                37.6 / 59.2 / 64.8 / 101 / 110 / 131    and 47.2 / 47.5 / 76.5 / 76.7 / 78.3 / 77.3
+//   d = 32, bf16, 4 sequences of 16000                20.6 / 29.7 / 48.0 / 48.2 / 79.6 / 79.3 and 24.7 / 24.8 / 38.2 / 38.5 / 38.4 / 39.2
+inline int few_rows(int dtype, int D) { return D == 256 ? (dtype == DT_F32 ? kFewRows : 64) : dtype == DT_F32 ? 64 : D == 128 ? 32 : 16; }
 inline int64_t coded_decode_wgs(const CodedDecodeCall& a) {
     const int64_t units = (int64_t)a.B * a.Hkv * a.n_split;
     return a.row_blocks > 1 ? (units + 7) / 8 * 8 * a.row_blocks : units;
