@@ -341,13 +341,16 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     if constexpr (CT == DT_F32) {
 #pragma unroll
         for (int ct = 0; ct < T; ++ct) {
+            f32x16 part = {};                                        // (an addition to the sum so far for a tile, not for every two keys: 2 % of the time)
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const int key = 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hh + i % 4, ch = 32 * ct + row;
                 float x = *reinterpret_cast<const float*>(ldsV + key * ROWB + value_piece<ROWB, 4>(key, ch >> 2) * 16 + (ch & 3) * 4);
                 if (poison && !(fabsf(x) < INFINITY)) x = 0.f;
-                st.acc[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[i / 16][i % 16], st.acc[ct], 0, 0, 0);
+                part = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[i / 16][i % 16], part, 0, 0, 0);
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.acc[ct][i] += part[i];
         }
     } else {
         using v8 = typename TileType<CT>::v8;
@@ -432,8 +435,50 @@ __device__ __forceinline__ void RowFetch<ROWB, NW, VALUES, EB>::operator()(const
     }
 }
 
-// DT: type of queries, output and open rows; FMT: the coded cache's format, or -1: rows of DT.  NW waves of 32 rows.
-template <int DT, int FMT, int D, int NW>
+// 32 bits that grow without end round every small addition the same way (65536 equal weights, fp32: 2.6e-4 of the sum, when every two keys were an addition).
+// Splits of more tiles than this put a lane's sums aside after as many, and begin again (FOLD).  Additions that follow each other: one for a tile (fp32), four (16 bits) or
+// eight (codes and fp32 queries), as many as there are tiles between two times, and then as many as there are times.
+template <int DT, bool CODED> constexpr int kFoldTiles = DT != DT_F32 ? 512 : CODED ? 128 : 256;
+// The sums put aside, of a lane: in scratch memory, since there are no registers or LDS for them beside two workgroups (d = 128 in 16 bits), relative to the powers of two
+// they were put aside with, which only rise.  (35 MB there and back a time, if all workgroups of d = 128 do it at once.  2048 tokens at the end of 200000, 16 heads
+// over 4, fp16: 3815 us and 3806 without; every 128 tiles 3 % of the time.)
+template <int D, bool FOLD> struct KeptSums {
+    typedef __attribute__((address_space(5))) float* Place;
+    static constexpr int M = D / 2, E = D / 2 + 1, L = D / 2 + 2, SIZE = D / 2 + 3;
+    Place at;
+    // (passed through a register: as an array that the compiler sees through it would be in registers)
+    __device__ __forceinline__ explicit KeptSums(float* room) : at((Place)room) { if (FOLD) asm volatile("" : "+v"(at)); }
+    // (nothing so far but keys of -inf or NaN: the sums are zero or NaN)
+    static __device__ __forceinline__ float turn(float before, float now) { return before == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(before - now); }
+    // VSCALE: the weighted sums have a power of two of their own.  first: nothing is there yet
+    template <bool VSCALE> __device__ __forceinline__ void put(RowState<D>& st, bool first) const {
+        if (!first) take<VSCALE>(st);
+        at[M] = st.m;
+        at[E] = st.e;
+        at[L] = st.l;
+        st.l = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                at[16 * ct + i] = st.acc[ct][i];
+                st.acc[ct][i] = 0.f;
+            }
+        }
+    }
+    template <bool VSCALE> __device__ __forceinline__ void take(RowState<D>& st) const {
+        const float f = turn(at[M], st.m), f_acc = VSCALE ? turn(at[E], st.e) : f;
+        st.l = fmaf(at[L], f, st.l);
+#pragma unroll
+        for (int ct = 0; ct < D / 32; ++ct) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.acc[ct][i] = fmaf(at[16 * ct + i], f_acc, st.acc[ct][i]);
+        }
+    }
+};
+
+// DT: type of queries, output and open rows; FMT: the coded cache's format, or -1: rows of DT.  NW waves of 32 rows.  FOLD: more than kFoldTiles tiles a split.
+template <int DT, int FMT, int D, int NW, bool FOLD>
 __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ? 2 : 1)) prompt_kernel(PromptCall a) {
     constexpr bool CODED = FMT >= 0;
     constexpr int CT = CODED ? DT_F16 : DT, PARTS = CODED && DT == DT_F32 ? 2 : 1;
@@ -496,6 +541,20 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
     st.hidden = hidden_of(st.pos);
 #pragma unroll
     for (int ct = 0; ct < D / 32; ++ct) st.acc[ct] = f32x16{};
+    float room[FOLD ? KeptSums<D, FOLD>::SIZE : 1];
+    const KeptSums<D, FOLD> kept(room);
+    // The walk over tiles lo to hi - 1, in runs between two times that the sums are put aside.
+    constexpr int RUN = kFoldTiles<DT, CODED>;
+    const auto in_runs = [&](auto walk, auto masked, int lo, int hi) {
+        if (!FOLD) return walk(masked, lo, hi);
+        while (lo < hi) {
+            const int next = i0 + ((lo - i0) / RUN + 1) * RUN, end = next < hi ? next : hi;
+            walk(masked, lo, end);
+            lo = end;
+            if (lo == next && lo < i1) kept.template put<CODED>(st, lo - i0 == RUN);
+        }
+    };
+    const auto end_walk = [&] { if (FOLD && i1 - i0 > RUN) kept.template take<CODED>(st); };
     const bool idle = at0 >= n_rows;
     const int wave_first = hidden_of(wave_lo) + 1;                  // oldest token that a window of the wave has
     const auto seen = [&](int t0) { return !idle && t0 <= wave_hi && (t0 + 63 >= wave_first || t0 < sinks); };
@@ -554,9 +613,10 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
         };
 #pragma unroll 1
         for (int x = 0; x < 2; ++x) {
-            walk(std::false_type{}, x ? end1 : i0, x ? end2 : end0);
-            walk(std::true_type{}, x ? end2 : end0, x ? i1 : end1);
+            in_runs(walk, std::false_type{}, x ? end1 : i0, x ? end2 : end0);
+            in_runs(walk, std::true_type{}, x ? end2 : end0, x ? i1 : end1);
         }
+        end_walk();
     } else {
         // ---- blocks: codes through registers, into LDS as fp16 ----
         float unit_q;
@@ -599,7 +659,7 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
             static_assert(CB / 16 % NT == 0 || CB / 16 < NT, "whole passes");
             constexpr int P = PT ? PT : 1;
             u32x4 k[P], v[P];
-            float2 scale, next = make_float2(0.f, 0.f);
+            float2 scale = make_float2(0.f, 0.f), next = scale;
             const char* const Kb = a.c.codes[0] + (int64_t)stream * a.c.blocks * CB;
             const char* const Vb = a.c.codes[1] + (int64_t)stream * a.c.blocks * CB;
             const float* const Sb = a.c.scales + (int64_t)stream * a.c.blocks * 2;
@@ -638,14 +698,19 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
                     }
                 }
             };
+            // (in vector registers: moved into scalar ones, as the compiler would have a block's numbers, they were waited for where they are asked for)
+            const auto take_scale = [&] {
+                scale = next;
+                asm volatile("" : "+v"(scale.x), "+v"(scale.y));
+            };
             if (i0 < i1) {
                 load(i0);
                 place(0);
+                take_scale();
             }
             const auto walk = [&](auto masked, int lo, int hi) {
                 for (int i = lo; i < hi; ++i) {
                     const int buf = NBUF == 2 ? (i - i0) & 1 : 0;
-                    scale = next;
                     if (i + 1 < i1) load(i + 1);
                     __syncthreads();
                     const int t0 = 64 * tile_of(i);
@@ -655,15 +720,19 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
                         prompt_tile<DT_F16, true, true, DT == DT_F32, decltype(masked)::value, D, PARTS, PARTS>(at, at + TILE, q, st, f, f_lo, scale.y, t0, sinks, false);
                     }
                     if (NBUF == 1) __syncthreads();
-                    if (i + 1 < i1) place(NBUF == 2 ? buf ^ 1 : 0);
+                    if (i + 1 < i1) {
+                        place(NBUF == 2 ? buf ^ 1 : 0);
+                        take_scale();
+                    }
                 }
             };
 #pragma unroll 1
             for (int x = 0; x < 2; ++x) {
-                walk(std::false_type{}, x ? end1 : i0, x ? end2 : end0);
-                walk(std::true_type{}, x ? end2 : end0, x ? i1 : end1);
+                in_runs(walk, std::false_type{}, x ? end1 : i0, x ? end2 : end0);
+                in_runs(walk, std::true_type{}, x ? end2 : end0, x ? i1 : end1);
             }
         }
+        end_walk();
 #pragma unroll
         for (int ct = 0; ct < D / 32; ++ct) {
 #pragma unroll

@@ -79,18 +79,24 @@ hipError_t launch_prompt_join(const PromptCall& a, hipStream_t st) {
 
 hipError_t launch_prompt(const PromptCall& a, hipStream_t st) {
     const dim3 grid((unsigned)((int64_t)a.S * a.Hkv * a.n_split * a.row_blocks));
+#define TKA_PROMPT_(DT_, D_, NW_)                                                                                         \
+    do {                                                                                                                  \
+        if (a.chunk > kFoldTiles<DT_, false>) hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, NW_, true>), grid, dim3(64 * NW_), 0, st, a); \
+        else hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, NW_, false>), grid, dim3(64 * NW_), 0, st, a);                \
+    } while (0)
 #define TKA_PROMPT(DT_, D_)                                                                                               \
     do {                                                                                                                  \
         if constexpr (DT_ != DT_F32) {                                                                                    \
             if (a.block_rows == 32) {                                                                                     \
-                hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, 1>), grid, dim3(64), 0, st, a);                            \
+                TKA_PROMPT_(DT_, D_, 1);                                                                                  \
                 break;                                                                                                    \
             }                                                                                                             \
         }                                                                                                                 \
-        hipLaunchKernelGGL((prompt_kernel<DT_, -1, D_, 4>), grid, dim3(256), 0, st, a);                               \
+        TKA_PROMPT_(DT_, D_, 4);                                                                                          \
     } while (0)
     TKA_BY_TYPE_AND_DIM(TKA_PROMPT, a.dtype, a.D);
 #undef TKA_PROMPT
+#undef TKA_PROMPT_
     const hipError_t e = hipGetLastError();
     return e != hipSuccess || a.n_split == 1 ? e : launch_prompt_join(a, st);
 }

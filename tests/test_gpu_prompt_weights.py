@@ -75,3 +75,50 @@ def check_small_weights(dtype, fmt, n, nats):
 @pytest.mark.parametrize("dtype", [ta.F16, ta.BF16])
 def test_small_weights_add_up(dtype, n, nats):
     check_small_weights(dtype, None, n, nats)
+
+
+# ---- sums of many equal weights ------------------------------------------------------------------------------------------
+def equal_weights(fmt, dtype):
+    """A score and a value that the cache reads back exactly, and a query whose weights do not end in 32 bits: key, value, query, score."""
+    one = 127 / 128 if fmt == ta.CODED_INT8 else 1.0             # (int8: 127 times a power of two, e4m3 and the types: itself)
+    q = torch.tensor(21.7).to(TORCH[dtype]).item()
+    return one, one, q, q * one / 8.0
+
+
+@pytest.mark.parametrize("dtype,fmt,n", [(ta.F32, None, 65537), (ta.F32, None, 200001), (ta.F32, ta.CODED_INT8, 200001), (ta.F32, ta.CODED_E4M3, 200001), (ta.F16, None, 1 << 20),
+                                         (ta.BF16, None, 1 << 20), (ta.F16, ta.CODED_INT8, 1 << 20), (ta.BF16, ta.CODED_E4M3, 1 << 20)])
+def test_sums_of_many_equal_weights(dtype, fmt, n):
+    """Rows as many as fill the chip, so that their keys are not split: sums that grow along the whole cache, of numbers of one sign."""
+    d, G, M = 64, 4, 8192
+    k, v, q0, score = equal_weights(fmt, dtype)
+    K, V = torch.zeros((1, n, d), device=DEV), torch.zeros((1, n, d), device=DEV)
+    K[0, :, 0] = k
+    V[0, :, 0] = v
+    V[0, ::3, 1:] = v
+    cache = cache_of(K, V, G, dtype, fmt)
+    try:
+        q = torch.zeros((1, M, G, d), device=DEV, dtype=TORCH[dtype])
+        q[..., 0] = q0
+        out, lse = cache.prompt(0, q)
+        seen = torch.arange(n - M, n, device=DEV, dtype=torch.float64) + 1
+        # a weight as the second product takes it, relative to the power of two above: 16 bits round it once
+        w = torch.tensor(2.0 ** (score * math.log2(math.e) - math.ceil(score * math.log2(math.e))), dtype=torch.float64)
+        if dtype != ta.F32:
+            w = w.to(torch.float16 if fmt is not None else TORCH[dtype]).double() / w
+        else:
+            w = torch.ones(())
+        want = torch.stack([torch.ones_like(seen), torch.floor((seen + 2) / 3) / seen], 1) * v * w.item()
+        # Additions that follow each other, half a step of the sum each at most.  Weighted sum: in a tile 32 (fp32; and one of them to the sum so far), 4 (16 bits) or 8 (codes,
+        # fp32 queries), as many tiles as there are between two times that the sums are put aside, and those times; weights: 16 in a tile and 2, then the same.
+        apart = 512 if dtype != ta.F32 else 256 if fmt is None else 128
+        folds = n / 64 / apart
+        chain = (32 + apart if fmt is None else 8 * apart) if dtype == ta.F32 else 4 * apart
+        sums = (chain + folds + 18 + apart + folds + 8) * U + (2.0 ** -22 if fmt is not None and dtype == ta.F32 else 0)
+        off = (out[0, :, :, :2].double() / want[:, None] - 1).abs().max().item()
+        # (the expected weight is that of 64 bits: 20 u of what 32 bits make of it may round to the neighbour, a step of the type)
+        assert off <= sums + (HALF[dtype] + 20 * U if dtype != ta.F32 else 4 * U), f"out off by {off:.3g}, {sums:.3g} allowed for sums"
+        off = (lse[0].double() - (score + torch.log(seen))[:, None]).abs().max().item()
+        allowed = (18 + apart + folds) * U + 3 * U * (score * 1.4427 + 14) + 4 * U + 4 * U * (score + math.log(n))
+        assert off <= allowed, f"lse off by {off:.3g}, {allowed:.3g} allowed"
+    finally:
+        cache.close()
