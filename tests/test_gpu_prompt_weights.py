@@ -122,3 +122,32 @@ def test_sums_of_many_equal_weights(dtype, fmt, n):
         assert off <= allowed, f"lse off by {off:.3g}, {allowed:.3g} allowed"
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("fmt", [ta.CODED_INT8, ta.CODED_E4M3])
+def test_sums_of_few_rows_of_many_streams(fmt):
+    """512 sequences of 2^20 tokens, 64 rows each: as many partial sums as the workspace has room for, and the walks between them of a length that does not
+    grow with the cache.  (Every sequence holds the same rows.)"""
+    d, n, B, M, dtype = 32, 1 << 20, 512, 64, ta.F32
+    _, v, q0, _ = equal_weights(fmt, dtype)
+    score = q0 * v / math.sqrt(d)                                # (the keys are the values, whose first channel alone meets the query)
+    V = torch.zeros((n, d), device=DEV)
+    V[:, 0] = v
+    V[::3, 1:] = v
+    cache = ta.TopkAttnCodedCache(1, B, 1, 1, d, n, dtype, format=fmt)
+    try:
+        ta.topk_attn_coded_append(cache.h, 0, -1, V.data_ptr(), V.data_ptr(), n, 0, d, d, torch.cuda.current_stream().cuda_stream)
+        q = torch.zeros((B, M, 1, d), device=DEV)
+        q[..., 0] = q0
+        out, lse = cache.prompt(0, q)
+        seen = torch.arange(n - M, n, device=DEV, dtype=torch.float64) + 1
+        want = torch.stack([torch.ones_like(seen), torch.floor((seen + 2) / 3) / seen], 1) * v
+        # additions that follow each other: four of a block, at most 256 blocks of a wave, then waves and splits; the weights' sum keeps what its additions round off
+        sums = (4 * 256 + 4 + 16 + 32 + 8) * U + 2.0 ** -22
+        off = (out[:, :, 0, :2].double() / want - 1).abs().max().item()
+        assert off <= sums + 4 * U, f"out off by {off:.3g}, {sums:.3g} allowed for sums"
+        off = (lse[:, :, 0].double() - (score + torch.log(seen))).abs().max().item()
+        allowed = 60 * U + 3 * U * (score * 1.4427 + 1) + 4 * U + 4 * U * (score + math.log(n))
+        assert off <= allowed, f"lse off by {off:.3g}, {allowed:.3g} allowed"
+    finally:
+        cache.close()
