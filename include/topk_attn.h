@@ -397,7 +397,9 @@ int topk_attn_coded_read(topk_attn_coded_t* h, int layer, int seq, int64_t first
 int topk_attn_coded_decode(topk_attn_coded_t* h, int layer, const void* q, int64_t sinks, int64_t window, float* out, float* lse,
                            void* hip_stream);
 
-/* topk_attn_prompt over the rows as they read: the same arguments, masks, output types and errors. */
+/* topk_attn_prompt over the rows as they read: the same arguments, masks, output types and errors.  Weights: up to 16 rows (n_queries times heads of a group) of 16 bits, 32 at
+ * head_dim 128, 64 at 256, and fp32 queries hold 2^-22 of them; more rows of 16 bits are rounded once, to fp16 over full blocks and to `dtype` over the rows behind them.  Those far
+ * below a row's largest in steps of 2^-36 of it. */
 int topk_attn_coded_prompt(topk_attn_coded_t* h, int layer, int seq, const void* q, int64_t n_queries, int64_t sinks, int64_t window, void* out,
                            float* lse, void* hip_stream);
 

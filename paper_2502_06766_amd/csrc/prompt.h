@@ -162,14 +162,17 @@ template <int CT> __device__ __forceinline__ bool has_no_number(uint32_t w) {
 }
 
 // The maximum that the weights are relative to follows the scores' only when those are more than 2^kSlack above: the weighted sums are scaled seldom
-// (scores of a normal distribution, 8192 tokens, 32 rows: after the first tile at none of the others, with no slack at 32 of 127), and a weight stays below 2^kSlack.
-constexpr float kSlack = 8.f, kSumSlack = 5.f, kSumShift = 10.f;       // (of weights times a value scale: below 2^15 in fp16)
+// (scores of a normal distribution, 8192 tokens, 32 rows: after the first tile at none of the others, with 2 powers of slack at ten of 127, with none at 33), and a
+// weight stays below 2^kSlack.
+constexpr float kSlack = 8.f;
 // fp16 has whole steps of its bits down to 2^-14 and nothing below 2^-25, and weights of that size may be many: one key 17 nats above 65536 others is 400 of
-// them, and without a shift nothing of those was left.  Weights are held times 2^13 with 2 powers of slack, below 2^15: all of the type's bits down to 2^-27 of the
-// largest and steps of 2^-37 below, as in the single token's decode.  (8 powers of slack and a shift of 7 would leave steps of 2^-31, 2^-6 of a weight 18 nats below.  They scale the
-// sums at none of 127 tiles of normal scores, 2 at ten of them: 8192 tokens, 32 heads over 8, d = 128, 590 us against 582.)
+// them, and without a shift nothing of those was left.  Weights of fp16 are held times 2^13 with 2 powers of slack, below 2^15: all of the type's bits down to 2^-27 of the
+// largest and steps of 2^-37 below, as in the single token's decode.  (8 powers of slack and a shift of 7 would leave steps of 2^-31, 2^-6 of a weight 18 nats below: 8192 tokens,
+// 32 heads over 8, d = 128, 590 us against 582.)  Over codes that goes for the product with a block's value scale, relative to a power of two that is up to twice the
+// largest: steps of 2^-36 (5 powers and 10 left 2^-33, 0.8 % of weights 18.75 nats below: a prompt of 8192 tokens, int8, bf16, 619 us against 616).
+constexpr float kSlack16 = 2.f, kShift16 = 13.f;
 template <int CT, bool VSCALE> struct WeightRange {
-    static constexpr float slack = CT == DT_F16 && !VSCALE ? 2.f : kSlack, shift = CT == DT_F16 && !VSCALE ? 13.f : 0.f;
+    static constexpr float slack = CT == DT_F16 && !VSCALE ? kSlack16 : kSlack, shift = CT == DT_F16 && !VSCALE ? kShift16 : 0.f;
 };
 
 // Whether some of a lane's words has an infinity or a NaN: the largest magnitudes, two halves at a time.
@@ -267,7 +270,7 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     if (VSCALE) {                                                    // (the weighted sum goes by its own)
         ke = (int)(__float_as_uint(sv) >> 23) - 126;                 // sv < 2^ke
         const float e_tile = bm + (float)ke;
-        e_new = sv > 0.f && !none && (e_tile > st.e + kSumSlack || st.e == -INFINITY) ? e_tile : st.e;
+        e_new = sv > 0.f && !none && (e_tile > st.e + kSlack16 || st.e == -INFINITY) ? e_tile : st.e;
         turn = st.e == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.e - e_new);
     }
     if (__any(turn != 1.f)) {
@@ -289,7 +292,7 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     st.l += sum[0] + sum[1];
     if (VSCALE) {
         float g = sv;
-        if (sv > 0.f) g = ldexpf(sv, (int)fmaxf(fminf(ref - e_new + kSumShift, (float)(127 - ke)), -300.f));
+        if (sv > 0.f) g = ldexpf(sv, (int)fmaxf(fminf(ref - e_new + kShift16, (float)(127 - ke)), -300.f));
         if (none) g = 0.f;                                           // (a block of NaN that the row does not see)
         st.e = e_new;
 #pragma unroll
@@ -764,7 +767,7 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
     }
     const int at = 32 * wave + (lane & 31);
     float by = 1.f;                                                 // brings the weighted sum to 2^m
-    if (CODED) by = st.e == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e - kSumShift - (m == -INFINITY ? 0.f : m));
+    if (CODED) by = st.e == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e - kShift16 - (m == -INFINITY ? 0.f : m));
     if (row0 + at >= n_rows) return;
     if (a.n_split == 1) {
         const float inv = by / l;

@@ -58,7 +58,10 @@ def check_small_weights(dtype, fmt, n, nats):
             # the exponent is a product with a factor of 32 bits and a difference (3 u of it and of its integer reference, which is 13 more in fp16), the exponential
             # 4 u; a weight's rounding and the output's; sums one after the other, 16 keys at a time
             exponent = 3 * U * (top * 1.4427 + 14) + 4 * U
-            tol = (2 * HALF[dtype] + 2 * exponent + (n / 16 + 64) * U) * want
+            # (over codes: half a step of 2^-37 of the largest weight, times a value scale that is at least half of the power of two it is relative to; fp32 queries: two
+            # parts, 2^-22)
+            weight = max(HALF[dtype] if dtype != ta.F32 else 2.0 ** -22, 0.0 if fmt is None else 2.0 ** -37 * math.exp(top))
+            tol = (weight + HALF[dtype] + 2 * exponent + (n / 16 + 64) * U) * want
             off = (out[0].double() - want).abs()
             assert bool((off <= tol).all()), f"{M} rows: off by {(off / want).max():.3g} of the output, {(tol / want).max():.3g} allowed"
             off = (lse[0].double() - torch.log(total)[:, None]).abs().max().item()
@@ -75,6 +78,14 @@ def check_small_weights(dtype, fmt, n, nats):
 @pytest.mark.parametrize("dtype", [ta.F16, ta.BF16])
 def test_small_weights_add_up(dtype, n, nats):
     check_small_weights(dtype, None, n, nats)
+
+
+@pytest.mark.parametrize("nats", [14, 16, 17, 18, 18.75])
+@pytest.mark.parametrize("n", [65537, 131073])
+@pytest.mark.parametrize("fmt", [ta.CODED_INT8, ta.CODED_E4M3])
+@pytest.mark.parametrize("dtype", [ta.F16, ta.BF16, ta.F32])
+def test_small_weights_over_codes_add_up(dtype, fmt, n, nats):
+    check_small_weights(dtype, fmt, n, nats)
 
 
 # ---- sums of many equal weights ------------------------------------------------------------------------------------------
