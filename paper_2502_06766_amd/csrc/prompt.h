@@ -47,7 +47,7 @@ struct PromptCall {
 constexpr int kPromptSplits = 64;      // (of 256 their joint takes 1.3 us more)
 // Tiles of 64 keys that the rows of the last block, which see most, see of a sequence of N tokens.
 inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int64_t window) {
-    const int64_t oldest = N - last_queries - window, from = oldest < 0 ? 0 : oldest / 64, front = ((sinks < N ? sinks : N) + 63) / 64;
+    const int64_t before = N - last_queries, from = window < before ? (before - window) / 64 : 0, front = ((sinks < N ? sinks : N) + 63) / 64;
     return (N + 63) / 64 - from + (front < from ? front : from);
 }
 // Rows of a block, and the splits of its keys: runs of `chunk` tiles, as many as there are compute units, twice that where the matrix unit has
