@@ -261,10 +261,11 @@ __device__ __forceinline__ void prompt_tile(const char* ldsK, const char* ldsV, 
     for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
     top = other_half_max(top);
     const bool none = top == -INFINITY;                              // (also of nothing but NaN: the weights are NaN then)
-    const float bm = none ? -INFINITY : ceilf(top * f);
+    // A whole number that the largest exponent is not above, and the product of 32 bits, which from 2^23 on is off by ones, is not below.
+    const float product = top * f, bm = none ? -INFINITY : ceilf(product) + floorf(fabsf(product) * 0x1p-23f);
     using Range = WeightRange<CT, VSCALE>;
-    const float m_new = bm > st.m + Range::slack || st.m == -INFINITY ? bm : st.m, whole = m_new == -INFINITY ? 0.f : m_new, ref = whole - Range::shift;
-    float turn = __builtin_amdgcn_exp2f(st.m - whole), e_new = 0.f;
+    const float to = bm - Range::shift, m_new = to > st.m + Range::slack || st.m == -INFINITY ? to : st.m, ref = m_new == -INFINITY ? 0.f : m_new;
+    float turn = __builtin_amdgcn_exp2f(st.m - ref), e_new = 0.f;
     int ke = 0;
     st.l *= turn;
     if (VSCALE) {                                                    // (the weighted sum goes by its own)
@@ -760,14 +761,14 @@ __global__ void __launch_bounds__(64 * NW, (NW > 1 && D <= 128 && DT != DT_F32 ?
         }
     }
     // ---- what the rows leave ----
-    float l = st.l, m = st.m - WeightRange<CT, CODED>::shift;
+    float l = st.l, m = st.m;
     {
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
     }
     const int at = 32 * wave + (lane & 31);
     float by = 1.f;                                                 // brings the weighted sum to 2^m
-    if (CODED) by = st.e == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e - kShift16 - (m == -INFINITY ? 0.f : m));
+    if (CODED) by = st.e == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.e - (m == -INFINITY ? 0.f : m) - kShift16);       // (beyond 2^24 one of them less 13 is no number)
     if (row0 + at >= n_rows) return;
     if (a.n_split == 1) {
         const float inv = by / l;

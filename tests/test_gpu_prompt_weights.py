@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import coded_cache_ref as ref
 from paper_2502_06766_amd import topk_attn as ta
 
 pytestmark = pytest.mark.gpu
@@ -86,6 +87,35 @@ def test_small_weights_add_up(dtype, n, nats):
 @pytest.mark.parametrize("dtype", [ta.F16, ta.BF16, ta.F32])
 def test_small_weights_over_codes_add_up(dtype, fmt, n, nats):
     check_small_weights(dtype, fmt, n, nats)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype,fmt", [(ta.F16, None), (ta.BF16, None), (ta.F16, ta.CODED_INT8), (ta.BF16, ta.CODED_E4M3)])
+def test_scores_beyond_2_24(dtype, fmt, d):
+    """Equal scores whose exponents of two lie between 2^24 and 2^27, where numbers of 32 bits are 2 to 8 apart: the weights stay in the type's range, and the output is
+    the values' mean; also where later keys' scores are a little higher."""
+    n, G, M = 333 if fmt is None else 320, 2, 100                 # (over codes: full blocks, whose keys all read as one number)
+    V = torch.rand((1, n, d), device=DEV) + 0.5
+    for q0 in (16384.0, 19968.0, 24576.0):
+        for k0 in range(4096, 32768, 1024):
+            if not 2 ** 24 <= q0 * k0 / math.sqrt(d) * math.log2(math.e) < 2 ** 27:
+                continue
+            K = torch.zeros((1, n, d), device=DEV)
+            K[0, :, 0] = k0
+            cache = cache_of(K, V, G, dtype, fmt)
+            try:
+                q = torch.zeros((1, M, G, d), device=DEV, dtype=TORCH[dtype])
+                q[..., 0] = q0
+                out, lse = cache.prompt(0, q)
+                rows = V[0].to(TORCH[dtype]).double()
+                if fmt is not None:
+                    rows = torch.from_numpy(ref.held(rows.cpu().numpy(), fmt)).to(DEV)
+                want = (rows.cumsum(0) / torch.arange(1, n + 1, device=DEV, dtype=torch.float64)[:, None])[n - M:]
+                # (all weights alike, rounded once; the output)
+                assert bool(((out[0].double() - want[:, None]).abs() <= (2 * HALF[dtype] + 1024 * U) * want[:, None]).all()), (q0, k0)
+                assert bool(torch.isfinite(lse).all())
+            finally:
+                cache.close()
 
 
 # ---- sums of many equal weights ------------------------------------------------------------------------------------------
