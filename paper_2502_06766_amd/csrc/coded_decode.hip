@@ -26,6 +26,8 @@ __device__ __forceinline__ float top_of_rows(float v) {        // largest of lan
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// A whole number that is not below x, and that the product which x is the rounding of is not above: from 2^23 on it is off by ones.
+__device__ __forceinline__ float whole_above(float x) { return ceilf(x) + floorf(fminf(fabsf(x), 0x1p120f) * 0x1p-23f); }      // (-inf stays)
 // 2^x for a whole number x (0 for -inf)
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -108,7 +110,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
             there[i] = 16 * wave + 4 * j + i < rows && sees(t0 + i);
             if (there[i]) top = fmaxf(top, s[i] * kScaleHi);
         }
-        m = ceilf(top_of_rows(top));
+        m = whole_above(top_of_rows(top));
         const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -235,7 +237,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
                 p[x] = v;
                 top = fmaxf(top, v);
             }
-            const float bm = ceilf(top_of_rows(top));
+            const float bm = whole_above(top_of_rows(top));
             const float m_new = fmaxf(m, bm), ref = m_new == -INFINITY ? 0.f : m_new;
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
@@ -320,7 +322,6 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
 #pragma unroll
             for (int r = 0; r < 4; ++r) red[wave][n][16 * c + 4 * j + r] = acc[c][r] * CodeUnit<FMT>::value;
         }
-        e_w -= kShift;
     }
     l = add_lanes_32(add_lanes_16(l));
     // A maximum passes over NaN: a wave of nothing but NaN would count as one without a key.  (With a maximum of +inf its factor is NaN.)
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
     if (j == 0) { red_m[wave][n] = m; red_l[wave][n] = l; red_e[wave][n] = e_w; }
     __syncthreads();
     const bool alone = ns == 1;
+    const float shift = split < open ? 0.f : kShift;                 // (of blocks' weighted sums; beyond 2^24 a power less 13 is no number)
     for (int i = (int)threadIdx.x; i < heads * D; i += NT) {
         const int h = i / D, c = i - h * D;
         float top = -INFINITY;
@@ -337,7 +339,7 @@ __global__ void __launch_bounds__(256, (DT == DT_F32 && D == 256 ? 1 : 2)) coded
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const float f = red_m[w][h] == -INFINITY ? 0.f : power2(red_m[w][h] - top);
-            const float f_w = red_e[w][h] == -INFINITY ? 0.f : power2(red_e[w][h] - top);
+            const float f_w = red_e[w][h] == -INFINITY ? 0.f : power2(red_e[w][h] - top - shift);
             sum = fmaf(f_w, red[w][h][c], sum);
             if (f != 0.f) total = fmaf(f, red_l[w][h], total);
         }

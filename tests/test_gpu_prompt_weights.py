@@ -89,33 +89,61 @@ def test_small_weights_over_codes_add_up(dtype, fmt, n, nats):
     check_small_weights(dtype, fmt, n, nats)
 
 
+def large_scores(d):
+    """Queries and keys of one channel whose exponents of two lie between 2^24 and 2^27, where numbers of 32 bits are 2 to 8 apart."""
+    for q0 in (16384.0, 19968.0, 24576.0):
+        for k0 in range(4096, 32768, 1024):
+            if 2 ** 24 <= q0 * k0 / math.sqrt(d) * math.log2(math.e) < 2 ** 27:
+                yield q0, k0
+
+
 @pytest.mark.parametrize("d", [32, 64, 128, 256])
 @pytest.mark.parametrize("dtype,fmt", [(ta.F16, None), (ta.BF16, None), (ta.F16, ta.CODED_INT8), (ta.BF16, ta.CODED_E4M3)])
 def test_scores_beyond_2_24(dtype, fmt, d):
-    """Equal scores whose exponents of two lie between 2^24 and 2^27, where numbers of 32 bits are 2 to 8 apart: the weights stay in the type's range, and the output is
-    the values' mean; also where later keys' scores are a little higher."""
+    """Equal scores that large: the weights stay in the type's range, and the output is the values' mean."""
     n, G, M = 333 if fmt is None else 320, 2, 100                 # (over codes: full blocks, whose keys all read as one number)
     V = torch.rand((1, n, d), device=DEV) + 0.5
-    for q0 in (16384.0, 19968.0, 24576.0):
-        for k0 in range(4096, 32768, 1024):
-            if not 2 ** 24 <= q0 * k0 / math.sqrt(d) * math.log2(math.e) < 2 ** 27:
-                continue
-            K = torch.zeros((1, n, d), device=DEV)
-            K[0, :, 0] = k0
-            cache = cache_of(K, V, G, dtype, fmt)
-            try:
-                q = torch.zeros((1, M, G, d), device=DEV, dtype=TORCH[dtype])
-                q[..., 0] = q0
-                out, lse = cache.prompt(0, q)
-                rows = V[0].to(TORCH[dtype]).double()
-                if fmt is not None:
-                    rows = torch.from_numpy(ref.held(rows.cpu().numpy(), fmt)).to(DEV)
-                want = (rows.cumsum(0) / torch.arange(1, n + 1, device=DEV, dtype=torch.float64)[:, None])[n - M:]
-                # (all weights alike, rounded once; the output)
-                assert bool(((out[0].double() - want[:, None]).abs() <= (2 * HALF[dtype] + 1024 * U) * want[:, None]).all()), (q0, k0)
-                assert bool(torch.isfinite(lse).all())
-            finally:
-                cache.close()
+    for q0, k0 in large_scores(d):
+        K = torch.zeros((1, n, d), device=DEV)
+        K[0, :, 0] = k0
+        cache = cache_of(K, V, G, dtype, fmt)
+        try:
+            q = torch.zeros((1, M, G, d), device=DEV, dtype=TORCH[dtype])
+            q[..., 0] = q0
+            out, lse = cache.prompt(0, q)
+            rows = V[0].to(TORCH[dtype]).double()
+            if fmt is not None:
+                rows = torch.from_numpy(ref.held(rows.cpu().numpy(), fmt)).to(DEV)
+            want = (rows.cumsum(0) / torch.arange(1, n + 1, device=DEV, dtype=torch.float64)[:, None])[n - M:]
+            # (all weights alike, rounded once; the output)
+            assert bool(((out[0].double() - want[:, None]).abs() <= (2 * HALF[dtype] + 1024 * U) * want[:, None]).all()), (q0, k0)
+            assert bool(torch.isfinite(lse).all())
+        finally:
+            cache.close()
+
+
+@pytest.mark.parametrize("fmt", [ta.CODED_INT8, ta.CODED_E4M3])
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("dtype", [ta.F16, ta.BF16, ta.F32])
+def test_single_tokens_and_few_rows_over_codes_beyond_2_24(dtype, d, fmt):
+    """The same of the kernel of single tokens: one token, and the last two."""
+    n, G = 320, 2
+    V = torch.rand((1, n, d), device=DEV) + 0.5
+    for q0, k0 in large_scores(d):
+        K = torch.zeros((1, n, d), device=DEV)
+        K[0, :, 0] = k0
+        cache = cache_of(K, V, G, dtype, fmt)
+        try:
+            q = torch.zeros((1, 2, G, d), device=DEV, dtype=TORCH[dtype])
+            q[..., 0] = q0
+            rows = torch.from_numpy(ref.held(V[0].to(TORCH[dtype]).double().cpu().numpy(), fmt)).to(DEV)
+            # (weights alike, in two parts of fp16: their reference is up to 24 powers above them, 13 are shifted, and the second part of 2^-11 has steps of 2^-24; 80 blocks)
+            weight = 2.0 ** -13
+            for out, m, half in ((cache.decode(0, q[:, -1].contiguous())[0][:, None], 1, 0.0), (cache.prompt(0, q)[0], 2, HALF[dtype])):
+                want = (rows.cumsum(0) / torch.arange(1, n + 1, device=DEV, dtype=torch.float64)[:, None])[n - m:]
+                assert bool(((out[0].double() - want[:, None]).abs() <= (weight + half + 600 * U) * want[:, None]).all()), (q0, k0, m)
+        finally:
+            cache.close()
 
 
 # ---- sums of many equal weights ------------------------------------------------------------------------------------------
