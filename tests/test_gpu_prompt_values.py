@@ -146,3 +146,41 @@ def test_prompt_over_codes(fmt, dtype, Hq, Hkv, d, n, M, sinks, window, few):
         check(cache, dtype, fmt, held(K, fmt), held(V, fmt), Hq, M, sinks, window, few, n)
     finally:
         cache.close()
+
+
+@pytest.mark.parametrize("fmt", [None, ta.CODED_E4M3])
+@pytest.mark.parametrize("dtype,n", [(ta.BF16, 34000), (ta.F32, 17000)])
+def test_captured_long_prompts_replay(dtype, n, fmt):
+    """Walks whose sums are put aside, recorded before any such call was made eagerly, replayed with other queries and eager calls between, on another stream beside them."""
+    Hq, Hkv, d, M = 4, 1, 64, 8192
+    K, V = rows_of(Hkv, n, d, dtype, n)
+    caches = []
+    for _ in range(2):
+        if fmt is None:
+            caches.append(ta.TopkAttnCache(1, 1, Hq, Hkv, d, n, 64, dtype))
+            caches[-1].append(0, 0, K, V, head_major=True)
+        else:
+            caches.append(ta.TopkAttnCodedCache(1, 1, Hq, Hkv, d, n, dtype, format=fmt))
+            caches[-1].append(0, K.transpose(0, 1)[None], V.transpose(0, 1)[None])
+    try:
+        g = torch.Generator(device=DEV)
+        g.manual_seed(3)
+        q = torch.empty((1, M, Hq, d), device=DEV, dtype=TORCH[dtype])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            recorded = caches[0].prompt(0, q)
+        side = torch.cuda.Stream()
+        for _ in range(3):
+            q.copy_(torch.randn(q.shape, generator=g, device=DEV))
+            side.wait_stream(torch.cuda.current_stream())
+            graph.replay()
+            with torch.cuda.stream(side):
+                beside = caches[1].prompt(0, q)
+            torch.cuda.synchronize()
+            got = [x.clone() for x in recorded]
+            eager = caches[0].prompt(0, q)
+            assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(got, eager, beside))
+    finally:
+        for cache in caches:
+            cache.close()
