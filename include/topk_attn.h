@@ -276,10 +276,11 @@ int topk_attn_decode_sinks(topk_attn_t* h, int layer, const void* q, int64_t sin
  *   q    device [S, n_queries, Hq, d] in the cache dtype, 16-byte aligned (S: sequences of the call)
  *   out  device [S, n_queries, Hq, d] in the cache dtype, 16-byte aligned;  lse  device [S, n_queries, Hq] fp32 or NULL
  * seq: one sequence of the layer, or -1: all B of them (their lengths may differ).  Softmax statistics and sums are held in 32 bits; the weights of
- * 16-bit caches are rounded to the cache dtype once, as the output is (fp16: below 2^-27 of the row's largest in steps of 2^-37 of it).  What a token does not see (NaN and infinities too) has no effect on its output.
- * n_queries == 0 is a no-op.  Replays as topk_attn_decode_dense.
- * Errors: EINVAL (null h/q/out, range, misaligned, n_queries < 0 or beyond a sequence's length, sinks < 0, window < 1), EUNSUPPORTED (2^24 or more
- * workgroups: 128 rows of queries times heads of a group each; 2^31 or more rows of a KV head). */
+ * 16-bit caches are rounded to the cache dtype once, as the output is (fp16: below 2^-27 of the row's largest in steps of 2^-37 of it).  What a token does not see (NaN and infinities too) has no effect on its output;
+ * an infinity among the values that it does see may come out as NaN.  n_queries == 0 is a no-op.  Replays as topk_attn_decode_dense.
+ * Errors: EINVAL (null h/q/out, range, misaligned, n_queries < 0 or beyond a sequence's length, sinks < 0, window < 1), EUNSUPPORTED (more than
+ * 2^30 rows, queries times heads of a group, of a KV head; 2^24 or more workgroups: one for every 128 rows of a sequence and KV head, 16 where fp32 has at most 64 of them, times
+ * the runs that keys are split in, where there would be less than one for every compute unit). */
 int topk_attn_prompt(topk_attn_t* h, int layer, int seq, const void* q, int64_t n_queries, int64_t sinks, int64_t window, void* out, float* lse,
                      void* hip_stream);
 
@@ -352,7 +353,8 @@ int topk_attn_decode_layers(topk_attn_t* h, int layer0, int n_layers, const void
  *         within 2^-10 scale where x is below 2^-6 scale.  For rows with a few channels far above the others.
  * A row reads as code * scale, in 32 bits or more; amax below 2^-100 reads as zeros; a block with a NaN or an infinity reads as NaN, all of it.  (E4M3: a number within
  * 2^-4 of the largest one of `dtype` may be rounded beyond it, and read back as an infinity.)
- * The handle is one of its own beside topk_attn_t, with the same rules: caller-owned memory, nothing allocated or synchronised after create, calls on a handle must not
+ * The handle is one of its own beside topk_attn_t, for dense and windowed layers: the top-k and block-sparse decodes, append_rotary, add_mass and evict do not take it (rows that
+ * are to be normalised and rotated come in that way from the caller, or by append_rotary into a topk_attn_t and its storage from there).  The same rules: caller-owned memory, nothing allocated or synchronised after create, calls on a handle must not
  * overlap, argument errors leave it unchanged, appends and resets are not to be replayed from a HIP graph, reads,
  * decodes and prompts as topk_attn_decode_dense. */
 typedef struct topk_attn_coded topk_attn_coded_t;

@@ -10,7 +10,7 @@
 //
 // Bound by the read of the codes: 16 KB per 64 keys and KV head (d = 128).  A million tokens, 8 KV heads, int8, fp16 queries: 373 us (5.8 TB/s; plain
 // reads reach 6.0 to 6.1); 16 sequences of up to 32768, e4m3: 127 (4.5 TB/s: their splits end unevenly); 500 tokens 11.2, all latency; eight tokens of 4 sequences
-// of 1000 to 20000 (32 rows) 51.  Two tiles a wave in registers, two workgroups to a compute unit: the next block is on its way during this one's products.
+// of 1000 to 20000 (32 rows) 46.  Two tiles a wave in registers, two workgroups to a compute unit: the next block is on its way during this one's products.
 #include "coded.h"
 #include "scan_tiles.h"
 #include "split_join.h"

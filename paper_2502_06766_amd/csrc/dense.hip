@@ -81,8 +81,6 @@ __device__ __forceinline__ int attend_splits(const AttendCall& a, int64_t pages)
     const int64_t splits = (pages + a.chunk - 1) / a.chunk;
     return (int)(splits < a.n_split ? splits : a.n_split);
 }
-// FOLD: for splits of more than kFold steps a wave.  (Shorter ones without the code for it, which takes registers: 32 sequences of 800 to 16384
-// tokens of d = 64 with mass 167 us, 176 with it.)
 // Whether some value of the wave's step (32 bits) is an infinity or a NaN.
 template <int D> __device__ __forceinline__ bool any_odd(const AttendTile<DT_F32, D>& t) {
     uint32_t top = 0;
@@ -94,6 +92,8 @@ template <int D> __device__ __forceinline__ bool any_odd(const AttendTile<DT_F32
     return __any(top >= 0x7F800000u);
 }
 
+// FOLD: for splits of more than kFold steps a wave.  (Shorter ones without the code for it, which takes registers: 32 sequences of 800 to 16384
+// tokens of d = 64 with mass 167 us, 176 with it.)
 template <int DT, int D, int WALK, bool MASS, bool FOLD>
 __global__ void __launch_bounds__(256, (AttendTile<DT, D>::ROW <= 512 ? 2 : 1)) attend_kernel(AttendCall a) {
     using Tile = AttendTile<DT, D>;

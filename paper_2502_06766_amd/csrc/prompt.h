@@ -8,14 +8,16 @@
 // times channels x rows, then channels x keys times keys x rows): a lane holds scores and weighted sums of one row, lane % 32, the running maximum is
 // a number per lane, and the scores come out of the first product in the order in which the second one takes the weights:
 //   score register i of a 32-key tile is key 8 (i / 4) + 4 (lane / 32) + i % 4; step x of 16 keys takes registers 8 x .. 8 x + 7.
-// Weights are rounded once to the type of the values (16 bits: what the second product takes; half a step of 2^-8 or 2^-11, as large as that of the output;
-// what of fp16's range they use: WeightRange); their sum is of the unrounded ones.
+// Weights are rounded once to the type of the values (16 bits: what the second product takes; half a step of 2^-8 or 2^-11, as large as that of the output, which is 1.4 times as
+// far off with both; what of fp16's range they use: WeightRange); their sum is of the unrounded ones.  Two parts of a weight take 1.4 times as long (the prompt of 8192
+// tokens below 751 us).
 //
-// Bound by the matrix unit, and behind it by the vector instructions of the weights, which only the other wave of a SIMD's products cover.  8 KV heads, 32 heads, d = 128:
-// a prompt of 8192 tokens, bf16, 532 us (1.03 PFLOP/s; a library product of 8192^3 has 1.23, MFMA alone on random numbers 1.5 to 1.8); 16384 tokens in a
-// window of 2048, fp16, 303 (0.84); 2048 tokens behind 24000 of the 8-bit cache 842 (0.92: the codes are widened on the way); eight tokens of four sequences of up to
-// 20000, bf16, 44.5, 34.4 of it this kernel (4.8 TB/s), 5.4 the joint.
-// Tiles go to LDS in two buffers by loads that pass no register; their reads meet no bank twice.  Two waves a SIMD with 32 rows each: one with 64 spilled.
+// Bound by the matrix unit, and behind it by the vector instructions of the weights, which only the other wave of a SIMD's products cover.  32 heads over 8, d = 128:
+// a prompt of 8192 tokens, bf16, 533 us (1.03 PFLOP/s; a library product of 8192^3 has 1.23, MFMA alone on random numbers 1.5 to 1.8); the last 2048 of 24000 tokens of the 8-bit
+// cache 861 (0.90: the codes are widened on the way); eight tokens of four sequences of up to 20000, bf16, 44.7, 34.4 of it this kernel (4.8 TB/s), 5.4 the joint.  16 heads over 4,
+// 16001 tokens in a window of 2048, fp16: 313 (0.81).
+// Tiles go to LDS in two buffers (16 bits up to d = 128) by loads that pass no register; their reads meet no bank twice.  Two waves a SIMD with 32 rows each, in 16 bits up to
+// d = 128, else one: one with 64 spilled.
 #pragma once
 #include <type_traits>
 
@@ -50,8 +52,8 @@ inline int64_t prompt_tiles(int64_t N, int64_t last_queries, int64_t sinks, int6
     const int64_t before = N - last_queries, from = window < before ? (before - window) / 64 : 0, front = ((sinks < N ? sinks : N) + 63) / 64;
     return (N + 63) / 64 - from + (front < from ? front : from);
 }
-// Rows of a block, and the splits of its keys: runs of `chunk` tiles, as many as there are compute units, twice that where the matrix unit has
-// most of the time (512 queries at 32768 tokens: 340 and 291 us).  (room: bytes there are for partial sums.  Eight queries of four
+// Rows of a block, and the splits of its keys, where there are fewer blocks than compute units: runs of `chunk` tiles, as many as there are compute units, twice that where the
+// matrix unit has most of the time (512 queries at 32768 tokens, 32 heads over 8: 340 and 291 us).  (room: bytes there are for partial sums.  Eight queries of four
 // sequences of 1k to 20k tokens in runs of 6 / 10 / 14 / 20 / 28 / 40 tiles, one of 20 to a compute unit: 65 / 54 / 57 / 45 / 52 / 62 us; in as many runs for every
 // sequence, the longest's of 20: 48.  64 queries of one sequence of 20000, 20 tiles to a compute unit: 55 / 47 / 47 / 41 / 48 / 61.  A wave of few rows has
 // a tile on its way, 32 KB at d = 128: of fewer channels as many more waves, d = 64, 8 sequences of 16000 tokens 62 and 48.)
