@@ -74,8 +74,9 @@ Workspace workspace_of(const topk_attn_coded_config* c) {
     // splits that fill the chip, and no more than 256 blocks a split (64 a wave, whose sums follow each other); one of open rows
     w.max_splits = std::min<int64_t>(kMaxSplits, 1 + std::min<int64_t>(std::max<int64_t>(blocks, 1), std::max<int64_t>(4096 / units, blocks / 256) + 1));
     size_t parts = (size_t)c->n_seqs * c->n_q_heads * (size_t)w.max_splits * (c->head_dim + 2) * sizeof(float);
-    // few rows of every stream: splits of at most 1024 blocks (256 a wave, whose sums follow each other), and one of open rows; a thousandth of the cache
-    parts = std::max(parts, (size_t)c->n_seqs * c->n_kv_heads * (size_t)few_rows(c->dtype, c->head_dim) * (size_t)(blocks / 1024 + 2) * (c->head_dim + 2) * sizeof(float));
+    // few rows of every stream of a long cache: splits of at most 1024 blocks (256 a wave, whose sums follow each other), and one of open rows; a hundredth of the cache at most
+    if (blocks >= 1024)
+        parts = std::max(parts, (size_t)c->n_seqs * c->n_kv_heads * (size_t)few_rows(c->dtype, c->head_dim) * (size_t)(blocks / 1024 + 2) * (c->head_dim + 2) * sizeof(float));
     // chunks of few rows whose keys are split: two workgroups of 128 rows on each of 256 compute units
     if (blocks >= 8) parts = std::max(parts, (size_t)512 * 128 * (c->head_dim + 2) * sizeof(float));
     w.parts = take(w.parts_bytes = parts);
@@ -295,7 +296,7 @@ int topk_attn_coded_prompt(topk_attn_coded_t* h, int layer, int seq, const void*
     if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return TOPK_ATTN_EINVAL;
     const Workspace ws = workspace_of(&c);
     const int64_t rows = n_queries * (c.n_q_heads / c.n_kv_heads);
-    if (rows <= few_rows(c.dtype, c.head_dim)) {
+    if (rows <= few_rows(c.dtype, c.head_dim) && split_room(c, ws, S, rows) >= 2) {      // (blocks and open rows)
         CodedDecodeCall a{};
         a.q = q; a.out_rows = out; a.lse = lse; a.sinks = sinks; a.window = window;
         a.reach = std::min(window, (int64_t)1 << 40) + n_queries - 1;
