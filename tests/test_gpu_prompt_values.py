@@ -184,3 +184,28 @@ def test_captured_long_prompts_replay(dtype, n, fmt):
     finally:
         for cache in caches:
             cache.close()
+
+
+@pytest.mark.parametrize("fmt", [None, ta.CODED_INT8])
+@pytest.mark.parametrize("dtype", [ta.F32, ta.F16, ta.BF16])
+def test_prompts_without_lse_and_without_tokens(dtype, fmt):
+    """Few rows, split and whole walks give the same output when nothing but it is asked for; no queries are no call."""
+    Hq, Hkv, d, n = 4, 2, 64, 1500
+    K, V = rows_of(Hkv, n, d, dtype, n)
+    if fmt is None:
+        cache = ta.TopkAttnCache(1, 1, Hq, Hkv, d, n, 64, dtype)
+        cache.append(0, 0, K, V, head_major=True)
+    else:
+        cache = ta.TopkAttnCodedCache(1, 1, Hq, Hkv, d, n, dtype, format=fmt)
+        cache.append(0, K.transpose(0, 1)[None], V.transpose(0, 1)[None])
+    try:
+        q = torch.randn((1, n, Hq, d), device=DEV).to(TORCH[dtype])
+        for M in (1, 3, 100, n):
+            last = q[:, n - M:].contiguous()
+            out, lse = cache.prompt(0, last)
+            alone, none = cache.prompt(0, last, want_lse=False)
+            assert none is None and torch.equal(out, alone) and lse.shape == (1, M, Hq)
+        out, lse = cache.prompt(0, q[:, :0])
+        assert out.shape == (1, 0, Hq, d) and lse.shape == (1, 0, Hq)
+    finally:
+        cache.close()
